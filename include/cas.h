@@ -22,8 +22,8 @@
  *     dQ = scale * sum_j dS_j k_j,  dK_j += scale * dS_j q,  dV_j += P_j dO,
  *   summed over every query (all heads of the group) that sees key j.
  *
- * Keys and queries are taken as given (post-RoPE); no positional operation is
- * applied. All calls are asynchronous on the caller's HIP stream; results are
+ * The attention takes keys and queries as given (post-RoPE): cas_rope and
+ * cas_paged_append apply the positions before it. All calls are asynchronous on the caller's HIP stream; results are
  * valid once the stream reaches them.
  *
  * Thread safety: calls may be made from several host threads; the error
@@ -384,6 +384,113 @@ cas_status_t cas_paged_decode_run(const cas_decode_plan_t *plan, const void *q, 
 cas_status_t cas_paged_decode_plan_destroy(cas_decode_plan_t *plan);
 /* Whether plan is one of problem p as its values and tables are now (1) or not (0). */
 int32_t cas_paged_decode_plan_matches(const cas_decode_plan_t *plan, const cas_decode_problem_t *p);
+
+/*
+ * Rotary positions (paper: paragraph "Pool rotation", the queries' positions
+ * are offset by the tokens of the active cartridges ahead of them; Su et al.
+ * 2021 for the rotation). Of every head's first rotary_dim channels, pair i <
+ * rotary_dim / 2 at position t is turned by the angle a = 2 pi t turns[i]:
+ *   (x, y) -> scale (x cos a - y sin a, x sin a + y cos a).
+ * The pair is channels (i, rotary_dim/2 + i) in the HALF layout and (2i, 2i+1)
+ * in the INTERLEAVED one; the channels from rotary_dim on are copied. The
+ * angle is taken modulo a turn in double precision (far positions lose
+ * nothing); cos, sin and the products are fp32, rounded once to the dtype.
+ *
+ * turns: device array of rotary_dim / 2 doubles, 8-byte aligned, which
+ *   cas_rope_frequencies fills in host memory, or any others.
+ */
+typedef enum { CAS_ROPE_HALF = 0, CAS_ROPE_INTERLEAVED = 1 } cas_rope_layout_t;
+
+typedef struct {
+  int32_t layout;       /* cas_rope_layout_t */
+  int32_t rotary_dim;   /* a multiple of 16, 16 .. head_dim */
+  const double *turns;
+  float scale;          /* finite and > 0: 1, or a long-context scaling's factor */
+} cas_rope_t;
+
+/*
+ * Frequencies for long contexts, with f_i = base^(-2i / rotary_dim) radians
+ * per position:
+ *   NONE      f_i
+ *   LINEAR    f_i / factor (Chen et al. 2023, position interpolation)
+ *   NTK       f_i with base * factor^(rotary_dim / (rotary_dim - 2))
+ *   BY_PARTS  (1 - w) f_i / factor + w f_i, where a pair that turns r times
+ *             within original_len tokens has w = (r - low) / (high - low),
+ *             clamped to [0, 1] (Peng et al. 2023, "NTK-by-parts")
+ * Host only: writes f_i / (2 pi) to turns[0 .. rotary_dim / 2).
+ */
+typedef enum { CAS_ROPE_NONE = 0, CAS_ROPE_LINEAR = 1, CAS_ROPE_NTK = 2, CAS_ROPE_BY_PARTS = 3 } cas_rope_scaling_t;
+
+cas_status_t cas_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_len,
+                                  double low, double high, double *turns);
+
+/*
+ * One rotated tensor: x is read, y written, [tokens, heads, head_dim] with unit
+ * channel stride (element (t, h, c) at base + t*stride_tok + h*stride_head +
+ * c). y == x with equal strides rotates in place. Tokens and heads of x may
+ * have stride 0 (one that several share); those of y are distinct.
+ */
+typedef struct {
+  const void *x;
+  void *y;
+  int64_t x_stride_tok, x_stride_head;
+  int64_t y_stride_tok, y_stride_head;
+  int32_t heads;
+} cas_rope_tensor_t;
+
+/*
+ * Rotates n (1 .. 4) tensors of the same tokens (a layer's queries and keys)
+ * in one launch. positions: device array of `tokens` int32 (any sign).
+ * inverse != 0 gives the gradient: the same with -a, so that for y = R x and a
+ * gradient dy the call returns dx = R^T dy. head_dim is 64 or 128; x and y are
+ * 16-byte aligned with strides of multiples of 16 bytes. An output may overlap
+ * no other tensor of the call. Nothing is allocated and no workspace is used,
+ * so the call can be captured into a HIP graph.
+ */
+cas_status_t cas_rope(const cas_rope_t *rope, cas_dtype_t dtype, int32_t head_dim, int64_t tokens, const int32_t *positions,
+                      const cas_rope_tensor_t *tensors, int32_t n, int32_t inverse, void *hip_stream);
+
+/*
+ * Appending to the paged cache. The requests, pages and counts are those of
+ * the paged attention (cas_decode_problem_t) with the new tokens counted in:
+ * request b's n_b = q_offsets[b+1] - q_offsets[b] new tokens (0 allowed here)
+ * are the last n_b of its kv_lens[b] keys, and the call writes them to those
+ * places of its pages: token t of k and v, rows of [Tq, num_kv_heads, head_dim],
+ * t counted over the requests. With a rope the keys are rotated on the way, by
+ * the position that their request's first new token has in `starts` (host,
+ * batch entries; NULL: its place among the keys) and the ones that follow;
+ * with q and q_out the queries are too ([Tq, Hq, head_dim], q_out contiguous).
+ * Every other row of the pools stays as it is. The values equal those that
+ * cas_rope gives.
+ *
+ * A row that the call writes may not be a key of another request, or a key
+ * twice in its own (pages of cartridges are shared by reference; a request
+ * whose last page is shared needs a copy of it first): such tables are refused.
+ * Strides as for cas_rope (16 bytes aligned). q may be NULL (no query is
+ * rotated); rope may be NULL if q is. q_out == q is allowed where q is
+ * contiguous. No workspace; nothing is allocated on the device, and the call
+ * can be captured (a replay writes the same places).
+ */
+typedef struct {
+  const void *k, *v;
+  int64_t k_stride_tok, k_stride_head, v_stride_tok, v_stride_head;
+  const void *q;
+  int64_t q_stride_tok, q_stride_head;
+  void *q_out;
+  const int32_t *starts;
+} cas_append_t;
+
+/* In two steps, as with cas_paged_decode_plan_create: the plan (with copies of the tables) is checked once for all the
+ * layers of a step. */
+typedef struct cas_append_plan cas_append_plan_t;
+
+cas_status_t cas_paged_append(const cas_decode_problem_t *p, const cas_rope_t *rope, const cas_append_t *t, void *k_pages,
+                              void *v_pages, void *hip_stream);
+cas_status_t cas_paged_append_plan_create(const cas_decode_problem_t *p, cas_append_plan_t **plan);
+cas_status_t cas_paged_append_run(const cas_append_plan_t *plan, const cas_rope_t *rope, const cas_append_t *t, void *k_pages,
+                                  void *v_pages, void *hip_stream);
+int32_t cas_paged_append_plan_matches(const cas_append_plan_t *plan, const cas_decode_problem_t *p);
+cas_status_t cas_paged_append_plan_destroy(cas_append_plan_t *plan);
 
 /*
  * Budget manager (paper: paragraphs "Budget Manager" and "Pool rotation";

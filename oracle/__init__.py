@@ -23,3 +23,4 @@ from .attention import (  # noqa: F401
 )
 from . import adam  # noqa: F401,E402
 from . import pool  # noqa: F401,E402
+from . import rope  # noqa: F401,E402

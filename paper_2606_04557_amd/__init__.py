@@ -7,8 +7,10 @@ is missing, or a call fails, an exception is raised.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import dataclasses
+import math
 import struct
 from typing import List, Optional, Sequence, Tuple
 
@@ -19,7 +21,8 @@ __all__ = ["Segment", "Problem", "CasError", "load", "prefix_attn_fwd", "prefix_
            "prefix_attn_bwd",
            "workspace_size", "plan_info", "set_tuning", "get_tuning", "cartridge_stage",
            "timing_enable", "timing_reset", "timing_read", "AdamCartridge", "adam_lr_scale",
-           "cartridge_adam", "DecodeProblem", "paged_decode_fwd", "decode_plan", "plan_rotation", "CartridgePool"]
+           "cartridge_adam", "DecodeProblem", "paged_decode_fwd", "decode_plan", "plan_rotation", "CartridgePool",
+           "Rope", "RopeScaling", "rope_fwd", "rope_bwd", "paged_append"]
 
 
 class CasError(RuntimeError):
@@ -323,11 +326,25 @@ class _DecodePlan:
             self._destroy(self.handle)
 
 
+class _AppendPlan:
+    """Where a problem's new tokens go (cas_append_plan_t)."""
+
+    def __init__(self, problem: DecodeProblem):
+        lib, handle = load(), ctypes.c_void_p()
+        _check(lib.cas_paged_append_plan_create(ctypes.byref(problem.c), ctypes.byref(handle)))
+        self.handle = handle
+        self._destroy = lib.cas_paged_append_plan_destroy
+
+    def __del__(self):
+        if hasattr(self, "_destroy"):
+            self._destroy(self.handle)
+
+
 class DecodeProblem:
-    """Host tables of a paged decode call (cas_decode_problem_t): per request its
-    query count, key count and page list (pages of [page_size, Hkv, d]). The
-    first call on them plans its launches, for every further one too while they
-    stay as they are."""
+    """Host tables of the paged calls (cas_decode_problem_t): per request its
+    query (new token) count, key count and page list (pages of [page_size, Hkv,
+    d]). The first call of each kind on them plans its launches, for every
+    further one too while they stay as they are."""
 
     def __init__(self, q_counts: Sequence[int], kv_lens: Sequence[int], page_lists: Sequence[Sequence[int]],
                  num_pages: int, page_size: int, num_kv_heads: int, group_size: int, head_dim: int,
@@ -347,7 +364,7 @@ class DecodeProblem:
         self._kv = (ctypes.c_int32 * max(B, 1))(*[int(x) for x in kv_lens])
         self._po = (ctypes.c_int32 * (B + 1))(*po)
         self._ids = (ctypes.c_int32 * max(len(ids), 1))(*ids)
-        self._plan = None
+        self._plan = self._append_plan = None
         I = ctypes.POINTER(ctypes.c_int32)
         self.c = _lib.DecodeProblem(B, num_kv_heads, group_size, head_dim, float(softmax_scale), page_size,
                                     int(num_pages), ctypes.cast(self._qo, I), ctypes.cast(self._kv, I),
@@ -358,6 +375,12 @@ class DecodeProblem:
         plan = self._plan
         if plan is None or not load().cas_paged_decode_plan_matches(plan.handle, ctypes.byref(self.c)):
             plan = self._plan = _DecodePlan(self)
+        return plan
+
+    def append_plan(self) -> _AppendPlan:
+        plan = self._append_plan
+        if plan is None or not load().cas_paged_append_plan_matches(plan.handle, ctypes.byref(self.c)):
+            plan = self._append_plan = _AppendPlan(self)
         return plan
 
 
@@ -384,6 +407,221 @@ def paged_decode_fwd(q, k_pages, v_pages, q_counts: Sequence[int], kv_lens: Sequ
     _check(load().cas_paged_decode_run(plan.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), o.data_ptr(),
                                        _ptr(lse), ws.data_ptr(), ws.numel(), _stream_handle(q.device, stream)))
     return o, lse
+
+
+# ---------------------------------------------------------------------------
+# Rotary positions, and appending to the paged cache
+# ---------------------------------------------------------------------------
+@dataclasses.dataclass(frozen=True)
+class RopeScaling:
+    """Frequencies for contexts longer than the model was trained on
+    (cas_rope_frequencies). kind "linear": every frequency divided by factor;
+    "ntk": the base raised; "by_parts": pairs that turn at most ``low`` times
+    within original_len tokens are divided by factor, from ``high`` times on left
+    alone, in proportion between, and cos and sin are multiplied by
+    attention_factor (None: 0.1 ln factor + 1 for a factor above 1)."""
+    kind: str
+    factor: float
+    original_len: float = 4096
+    low: float = 1.0
+    high: float = 32.0
+    attention_factor: Optional[float] = None
+
+
+class Rope:
+    """Rotary positions of the first rotary_dim channels of every head
+    (cas_rope_t). ``layout`` "half" pairs channels i and rotary_dim/2 + i,
+    "interleaved" 2i and 2i + 1. ``frequencies`` (rotary_dim/2 radians per
+    position) and ``scale`` (on cos and sin) stand in for what base and scaling
+    give. The frequencies are copied to a GPU by the first call there (before a
+    graph is captured: call it, or device_turns, once)."""
+
+    _LAYOUTS = {"half": _lib.CAS_ROPE_HALF, "interleaved": _lib.CAS_ROPE_INTERLEAVED}
+    _KINDS = {"linear": _lib.CAS_ROPE_LINEAR, "ntk": _lib.CAS_ROPE_NTK, "by_parts": _lib.CAS_ROPE_BY_PARTS}
+
+    def __init__(self, rotary_dim: int, base: float = 10000.0, layout: str = "half", scaling: Optional[RopeScaling] = None,
+                 frequencies: Optional[Sequence[float]] = None, scale: Optional[float] = None):
+        if layout not in self._LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(self._LAYOUTS)}")
+        if scaling is not None and scaling.kind not in self._KINDS:
+            raise ValueError(f"scaling kind must be one of {sorted(self._KINDS)}")
+        self.rotary_dim, self.layout = int(rotary_dim), layout
+        out = (ctypes.c_double * max(self.rotary_dim // 2, 1))()
+        if scaling is None:
+            _check(load().cas_rope_frequencies(self.rotary_dim, float(base), _lib.CAS_ROPE_NONE, 1.0, 1.0, 0.0, 1.0, out))
+        else:
+            _check(load().cas_rope_frequencies(self.rotary_dim, float(base), self._KINDS[scaling.kind], float(scaling.factor),
+                                               float(scaling.original_len), float(scaling.low), float(scaling.high), out))
+        self.turns = list(out)   # turns per position
+        if frequencies is not None:
+            if len(frequencies) != self.rotary_dim // 2:
+                raise ValueError("frequencies must have rotary_dim / 2 entries")
+            self.turns = [float(f) / (2.0 * math.pi) for f in frequencies]
+        if scale is None:
+            scale = 1.0
+            if scaling is not None and scaling.attention_factor is not None:
+                scale = scaling.attention_factor
+            elif scaling is not None and scaling.kind == "by_parts" and scaling.factor > 1:
+                scale = 0.1 * math.log(scaling.factor) + 1.0
+        self.scale = float(scale)
+        self._device = {}
+
+    def device_turns(self, device):
+        """The frequencies on a GPU (float64 [rotary_dim/2])."""
+        return self._on(device)[1]
+
+    def _on(self, device):
+        import torch
+        got = self._device.get(device)
+        if got is None:
+            t = torch.tensor(self.turns, dtype=torch.float64, device=device)
+            got = self._device[device] = (_lib.Rope(self._LAYOUTS[self.layout], self.rotary_dim, t.data_ptr(), self.scale), t)
+        return got
+
+
+def _on_device(device, call):
+    """call() with ``device`` the current one, as launches need it."""
+    import torch
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, not on {device}")
+    if device.index is None or device.index == torch.cuda.current_device():
+        return call()
+    with torch.cuda.device(device):
+        return call()
+
+
+def _empty(stream, shape, dtype, device):
+    """A tensor whose memory belongs to the stream that the call runs on."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _same_kind(what: str, t, shape, dtype, device) -> None:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {list(shape)}, is {list(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, is {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{what} is on {t.device}, not on {device}")
+
+
+def _token_strides(what: str, t) -> Tuple[int, int, int, int]:
+    """(tokens, heads, token stride, head stride) of a [.., tokens, heads, d] tensor; 0 for a stride that nothing uses."""
+    shape, st = t.shape, t.stride()
+    if len(shape) < 3:
+        raise ValueError(f"{what} must be [.., tokens, heads, d]")
+    n = 1
+    step = st[-3]
+    for size, stride in zip(reversed(shape[:-2]), reversed(st[:-2])):
+        if size != 1:
+            if n == 1:
+                step = stride
+            elif stride != n * step:
+                raise ValueError(f"{what}: the leading dimensions have no common token stride")
+        n *= size
+    if shape[-1] > 1 and st[-1] != 1:
+        raise ValueError(f"{what}: channel stride must be 1")
+    return n, shape[-2], step if n > 1 else 0, st[-2] if shape[-2] > 1 else 0
+
+
+def _rope(xs, positions, rope: Rope, outs, stream, inverse: int) -> List[object]:
+    import torch
+    xs = list(xs)
+    if not 1 <= len(xs) <= 4:
+        raise ValueError("1 to 4 tensors")
+    x0 = xs[0]
+    dev, D = x0.device, x0.shape[-1]
+    outs = [None] * len(xs) if outs is None else list(outs)
+    if len(outs) != len(xs):
+        raise ValueError("outs must have an entry per tensor")
+    tens = (_lib.RopeTensor * len(xs))()
+    T = None
+    for i, x in enumerate(xs):
+        n, heads, st, sh = _token_strides(f"tensor {i}", x)
+        if T is None:
+            T = n
+        if n != T or x.shape[-1] != D:
+            raise ValueError("the tensors must have the same tokens and head_dim")
+        if x.dtype != x0.dtype or x.device != dev:
+            raise ValueError("the tensors must have one dtype and device")
+        if outs[i] is None:
+            outs[i] = _empty(stream, x.shape, x.dtype, dev)
+        y = outs[i]
+        if y is not x:
+            _same_kind(f"output {i}", y, x.shape, x.dtype, dev)
+        _, _, yt, yh = _token_strides(f"output {i}", y)
+        tens[i] = _lib.RopeTensor(x.data_ptr(), y.data_ptr(), st, sh, yt, yh, heads)
+    if positions.dtype != torch.int32:
+        raise TypeError("positions must be int32")
+    if positions.numel() != T or not positions.is_contiguous() or positions.device != dev:
+        raise ValueError("positions must be contiguous, one per token, on the tensors' device")
+    code = _dtype_code(x0)
+    _on_device(dev, lambda: _check(load().cas_rope(ctypes.byref(rope._on(dev)[0]), code, D, T, positions.data_ptr(), tens,
+                                                   len(xs), inverse, _stream_handle(dev, stream))))
+    return outs
+
+
+def rope_fwd(xs: Sequence[object], positions, rope: Rope, outs: Optional[Sequence[object]] = None, stream=None) -> List[object]:
+    """Rotates 1 to 4 tensors of the same tokens ([.., tokens, heads, d]; a layer's
+    queries and keys) by int32 ``positions``, one per token. Any token and head
+    strides, as of slices of one projection's output; outs=xs rotates in place."""
+    return _rope(xs, positions, rope, outs, stream, 0)
+
+
+def rope_bwd(grads: Sequence[object], positions, rope: Rope, outs: Optional[Sequence[object]] = None,
+             stream=None) -> List[object]:
+    """The gradients of rope_fwd's inputs from those of its outputs."""
+    return _rope(grads, positions, rope, outs, stream, 1)
+
+
+def paged_append(k, v, k_pages, v_pages, problem: DecodeProblem, rope: Optional[Rope] = None, q=None, q_out=None,
+                 starts: Optional[Sequence[int]] = None, stream=None):
+    """Writes the problem's new tokens, k and v ([Tq, Hkv, d] bf16, packed by
+    request, any token and head strides), to their places in the page pools:
+    request b's are the last of its kv_lens[b] keys. With ``rope`` the keys are
+    rotated on the way, and ``q`` ([Tq, Hq, d]) into ``q_out``, which is
+    returned; a request's first new token has position starts[b], by default its
+    place among the keys. Rows of k, v and q behind the last request's are not
+    read, and no other row of the pools is written."""
+    import torch
+    c = problem.c
+    Tq, Hkv, D, Hq, dev, dt = problem.Tq, c.num_kv_heads, c.head_dim, c.num_kv_heads * c.group_size, k.device, torch.bfloat16
+    for what, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        _same_kind(what, t, (c.num_pages, c.page_size, Hkv, D), dt, dev)
+        if not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+    a = _lib.Append()
+    for what, t, heads in (("k", k, Hkv), ("v", v, Hkv), ("q", q, Hq)):
+        if t is None:
+            continue
+        n, h, st, sh = _token_strides(what, t)
+        if n < Tq:
+            raise ValueError(f"{what} has {n} tokens, the problem {Tq}")
+        _same_kind(what, t, (*t.shape[:-2], heads, D), dt, dev)
+        setattr(a, what, t.data_ptr())
+        setattr(a, what + "_stride_tok", st)
+        setattr(a, what + "_stride_head", sh)
+    if q is not None:
+        if q_out is None:
+            q_out = _empty(stream, (Tq, Hq, D), dt, dev)
+        if q_out.numel() < Tq * Hq * D or not q_out.is_contiguous() or q_out.shape[-2:] != (Hq, D) or q_out.dtype != dt \
+                or q_out.device != dev:
+            raise ValueError("q_out must be a contiguous bf16 [Tq, Hq, d] on the tensors' device")
+        a.q_out = q_out.data_ptr()
+    if starts is not None:
+        if len(starts) != c.batch:
+            raise ValueError("starts must have an entry per request")
+        a.starts = (ctypes.c_int32 * c.batch).from_buffer(array.array("i", starts))
+
+    def call():
+        plan = problem.append_plan()
+        _check(load().cas_paged_append_run(plan.handle, None if rope is None else ctypes.byref(rope._on(dev)[0]), ctypes.byref(a),
+                                           k_pages.data_ptr(), v_pages.data_ptr(), _stream_handle(dev, stream)))
+    _on_device(dev, call)
+    return q_out
 
 
 def plan_rotation(steps: Sequence[int], active: Sequence[bool], budget: int, swap_fraction: float):

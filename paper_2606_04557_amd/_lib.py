@@ -30,8 +30,16 @@ EXPORTS = [
     "cas_paged_decode_plan_info", "cas_paged_decode_plan_create", "cas_paged_decode_run", "cas_paged_decode_plan_destroy",
     "cas_paged_decode_plan_matches", "cas_pool_plan_rotation", "cas_pool_create", "cas_pool_destroy", "cas_pool_host_cartridge",
     "cas_pool_load", "cas_pool_active", "cas_pool_end_step", "cas_pool_flush",
-    "cas_prefix_attn_fwd_noalloc", "cas_pool_read_moments",
+    "cas_prefix_attn_fwd_noalloc", "cas_pool_read_moments", "cas_rope_frequencies", "cas_rope", "cas_paged_append",
+    "cas_paged_append_plan_create", "cas_paged_append_run", "cas_paged_append_plan_matches", "cas_paged_append_plan_destroy",
 ]
+
+CAS_ROPE_HALF = 0
+CAS_ROPE_INTERLEAVED = 1
+CAS_ROPE_NONE = 0
+CAS_ROPE_LINEAR = 1
+CAS_ROPE_NTK = 2
+CAS_ROPE_BY_PARTS = 3
 
 
 class Segment(ctypes.Structure):
@@ -74,6 +82,24 @@ class DecodePlanInfo(ctypes.Structure):
     _fields_ = [("key_tiles", ctypes.c_int64), ("workgroups", ctypes.c_int32), ("num_rows", ctypes.c_int32),
                 ("row_blocks", ctypes.c_int32), ("max_partials", ctypes.c_int32), ("shared_runs", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("ws_bytes", ctypes.c_size_t)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("turns", ctypes.c_void_p),
+                ("scale", ctypes.c_float)]
+
+
+class RopeTensor(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("x_stride_tok", ctypes.c_int64),
+                ("x_stride_head", ctypes.c_int64), ("y_stride_tok", ctypes.c_int64), ("y_stride_head", ctypes.c_int64),
+                ("heads", ctypes.c_int32)]
+
+
+class Append(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_stride_tok", ctypes.c_int64),
+                ("k_stride_head", ctypes.c_int64), ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
+                ("q", ctypes.c_void_p), ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
+                ("q_out", ctypes.c_void_p), ("starts", ctypes.POINTER(ctypes.c_int32))]
 
 
 class PoolConfig(ctypes.Structure):
@@ -148,6 +174,15 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cas_paged_decode_plan_destroy.argtypes = [vp]
     lib.cas_paged_decode_plan_matches.argtypes = [vp, P(DecodeProblem)]
     lib.cas_paged_decode_plan_matches.restype = i32
+    f64 = ctypes.c_double
+    lib.cas_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, P(f64)]
+    lib.cas_rope.argtypes = [P(Rope), ctypes.c_int, i32, ctypes.c_int64, vp, P(RopeTensor), i32, i32, vp]
+    lib.cas_paged_append.argtypes = [P(DecodeProblem), P(Rope), P(Append), vp, vp, vp]
+    lib.cas_paged_append_plan_create.argtypes = [P(DecodeProblem), P(vp)]
+    lib.cas_paged_append_run.argtypes = [vp, P(Rope), P(Append), vp, vp, vp]
+    lib.cas_paged_append_plan_matches.argtypes = [vp, P(DecodeProblem)]
+    lib.cas_paged_append_plan_matches.restype = i32
+    lib.cas_paged_append_plan_destroy.argtypes = [vp]
     u8p = P(ctypes.c_uint8)
     lib.cas_pool_plan_rotation.argtypes = [P(i32), u8p, i32, i32, ctypes.c_float, P(i32), P(i32), P(i32)]
     lib.cas_pool_create.argtypes = [P(PoolConfig), P(vp)]
@@ -172,7 +207,9 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                  "cas_paged_decode_workspace_size", "cas_paged_decode_fwd", "cas_paged_decode_plan_info",
                  "cas_paged_decode_plan_create", "cas_paged_decode_run", "cas_paged_decode_plan_destroy",
                  "cas_pool_plan_rotation", "cas_pool_create", "cas_pool_destroy", "cas_pool_host_cartridge", "cas_pool_load",
-                 "cas_pool_active", "cas_pool_end_step", "cas_pool_flush", "cas_pool_read_moments"):
+                 "cas_pool_active", "cas_pool_end_step", "cas_pool_flush", "cas_pool_read_moments",
+                 "cas_rope_frequencies", "cas_rope", "cas_paged_append", "cas_paged_append_plan_create", "cas_paged_append_run",
+                 "cas_paged_append_plan_destroy"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib

@@ -31,8 +31,8 @@ SAN_LIB_PATH = os.path.join(SAN_DIR, "libcas_san.so")
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer",
              "-O1", "-g"]
-SOURCES = ["cas_api.cpp", "cas_pool.cpp", "cas_fwd.hip", "cas_bwd.hip", "cas_bf16.hip", "cas_adam.hip", "cas_decode.hip",
-           "cas_noalloc.hip"]
+SOURCES = ["cas_api.cpp", "cas_paged.cpp", "cas_pool.cpp", "cas_fwd.hip", "cas_bwd.hip", "cas_bf16.hip", "cas_adam.hip",
+           "cas_decode.hip", "cas_noalloc.hip", "cas_rope.hip"]
 ARCH = "gfx950"
 
 # -packed-fp32-ops: no packed fp32 ALU instructions are generated on gfx950.

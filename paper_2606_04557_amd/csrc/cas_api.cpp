@@ -44,12 +44,11 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
-struct Interval {
-  uintptr_t lo, hi;   // [lo, hi)
-  bool write;
-  uintptr_t owner;    // identical writes of one owner may coincide (aliased cartridge)
-  const char *what;
-};
+std::mutex g_topo_mu;
+std::map<int, Topology> g_topo;
+}  // namespace
+
+namespace cas {
 
 // Every write interval must be disjoint from every other interval (reads and
 // writes) of a different owner.
@@ -81,6 +80,41 @@ bool overlap_free(std::vector<Interval> &iv, std::string &msg) {
   }
   return true;
 }
+
+Topology device_topology() {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) {
+    (void)hipGetLastError();
+    return Topology{};
+  }
+  std::lock_guard<std::mutex> lk(g_topo_mu);
+  auto it = g_topo.find(dev);
+  if (it != g_topo.end()) return it->second;
+  Topology t;
+  int cus = 0;
+  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0) {
+    t.cus = cus;
+    t.xcds = std::max(1, cus / 32);
+  } else {
+    (void)hipGetLastError();
+  }
+  g_topo.emplace(dev, t);
+  return t;
+}
+
+cas_status_t check_workspace(void *ws, size_t have, size_t need) {
+  if (have < need || (need > 0 && !ws)) g_ws_needed = need;
+  if (need > 0 && !ws) return fail(CAS_ERR_WORKSPACE, "workspace is NULL");
+  if (have < need)
+    return fail(CAS_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes, have " +
+                                       std::to_string(have));
+  if (!aligned16(ws)) return fail(CAS_ERR_ALIGNMENT, "workspace must be 16-byte aligned");
+  return CAS_OK;
+}
+
+}  // namespace cas
+
+namespace {
 
 struct Plan {
   DType dt;
@@ -118,35 +152,6 @@ struct Plan {
   size_t off_part_o = 0, off_part_lse = 0, ws_fwd = 0;
   size_t off_nd = 0, off_lse2 = 0, off_part_dq = 0, off_qT = 0, off_doT = 0, ws_bwd = 0;
 };
-
-// Compute units and XCDs of the current device, looked up once per device.
-// gfx950 has 32 CUs per XCD (256 and 8 on a whole MI355X; a partition shows
-// fewer). Without a device (planning-only use) the whole MI355X is assumed.
-struct Topology {
-  int cus = 256, xcds = 8;
-};
-std::mutex g_topo_mu;
-std::map<int, Topology> g_topo;
-Topology device_topology() {
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) {
-    (void)hipGetLastError();
-    return Topology{};
-  }
-  std::lock_guard<std::mutex> lk(g_topo_mu);
-  auto it = g_topo.find(dev);
-  if (it != g_topo.end()) return it->second;
-  Topology t;
-  int cus = 0;
-  if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && cus > 0) {
-    t.cus = cus;
-    t.xcds = std::max(1, cus / 32);
-  } else {
-    (void)hipGetLastError();
-  }
-  g_topo.emplace(dev, t);
-  return t;
-}
 
 // Key-axis splits of the forward or dQ pass, for base_wgs workgroups unsplit
 // that walk avg_tiles key tiles on average and max_tiles at most, one
@@ -925,16 +930,6 @@ cas_status_t hip_fail(const char *what, hipError_t e) {
   return fail(CAS_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
 }
 
-cas_status_t check_workspace(void *ws, size_t have, size_t need) {
-  if (have < need || (need > 0 && !ws)) g_ws_needed = need;
-  if (need > 0 && !ws) return fail(CAS_ERR_WORKSPACE, "workspace is NULL");
-  if (have < need)
-    return fail(CAS_ERR_WORKSPACE, "workspace too small: need " + std::to_string(need) + " bytes, have " +
-                                       std::to_string(have));
-  if (!aligned16(ws)) return fail(CAS_ERR_ALIGNMENT, "workspace must be 16-byte aligned");
-  return CAS_OK;
-}
-
 // ---------------------------------------------------------------------------
 // Paged decode: validation, key-axis split planning and launch tables.
 // ---------------------------------------------------------------------------
@@ -1431,6 +1426,14 @@ namespace cas {
 cas_status_t set_error(cas_status_t s, const std::string &msg) { return fail(s, msg); }
 
 cas_status_t set_hip_error(const char *what, hipError_t e) { return hip_fail(what, e); }
+
+cas_status_t upload_launch_tables(size_t bytes, void *ws, hipStream_t stream, const std::function<void(char *)> &fill) {
+  return ring_upload(bytes, ws, stream, fill);
+}
+
+hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch) {
+  return timed(name, s, launch);
+}
 
 hipError_t enqueue_copies(const HostCopy *c, int n, hipMemcpyKind kind, hipStream_t s) {
   const char *run_src = nullptr;

@@ -3,7 +3,9 @@
 
 #include <hip/hip_runtime.h>
 
+#include <functional>
 #include <string>
+#include <vector>
 
 #include "../../include/cas.h"
 
@@ -13,6 +15,36 @@ namespace cas {
 cas_status_t set_error(cas_status_t s, const std::string &msg);
 // CAS_ERR_HIP with the HIP error's text.
 cas_status_t set_hip_error(const char *what, hipError_t e);
+
+// Byte range [lo, hi) of a tensor that a call reads or writes. Writes of one
+// owner may coincide.
+struct Interval {
+  uintptr_t lo, hi;
+  bool write;
+  uintptr_t owner;
+  const char *what;
+};
+// Whether every written interval is disjoint from all others; msg names a pair
+// that is not.
+bool overlap_free(std::vector<Interval> &iv, std::string &msg);
+
+// CAS_ERR_WORKSPACE (and the size that the call needs) unless ws holds `need` bytes.
+cas_status_t check_workspace(void *ws, size_t have, size_t need);
+
+// Copies `bytes` of launch tables, written by fill() into pinned memory, to ws
+// on the stream.
+cas_status_t upload_launch_tables(size_t bytes, void *ws, hipStream_t stream, const std::function<void(char *)> &fill);
+
+// launch(), bracketed by timing events while cas_timing_enable is on.
+hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch);
+
+// Compute units and XCDs of the current device, looked up once per device.
+// gfx950 has 32 CUs per XCD (256 and 8 on a whole MI355X; a partition shows
+// fewer). Without a device (planning-only use) the whole MI355X is assumed.
+struct Topology {
+  int cus = 256, xcds = 8;
+};
+Topology device_topology();
 
 // One host <-> device copy of a list; bytes == 0 entries are skipped.
 struct HostCopy {

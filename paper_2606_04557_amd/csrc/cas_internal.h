@@ -269,6 +269,48 @@ struct DecodeParams {
   float scale_log2;
 };
 
+// Rotary positions of up to four tensors of the same tokens. Workgroup (x, y,
+// z) takes tokens 256 / (head_dim / 16) / slots each from tensor z, heads y *
+// slots + i, and from there every gridDim.y * slots.
+struct DevRopeTensor {
+  const void *x;
+  void *y;
+  int64_t x_tok, x_head, y_tok, y_head;   // strides in elements
+  int32_t heads;
+  int32_t pad_;
+};
+struct DevRope {
+  const double *turns;
+  int32_t rotary;
+  float scale;
+  int32_t interleaved;
+  int32_t inverse;
+};
+struct RopeParams {
+  DevRope rope;
+  DevRopeTensor t[4];
+  const int32_t *positions;
+  int64_t tokens;
+  int32_t slots;            // threads' heads of one token at a time, a power of two
+};
+
+// Appending to the paged cache: n consecutive tokens, tok0 of the new ones, go
+// to rows row0 .. row0 + n - 1 of the pool's rows from page `page` on; the first
+// has position pos0. One item per workgroup (of each tensor and head group).
+struct DevAppendItem {
+  int32_t tok0, page, pos0;
+  int16_t row0, n;
+};
+constexpr int kAppendItems = 224;   // items in one launch's kernel arguments (4 KiB in all)
+struct AppendParams {
+  DevRope rope;             // turns null: nothing is rotated
+  const void *k, *v, *q;
+  void *k_pages, *v_pages, *q_out;
+  int64_t k_tok, k_head, v_tok, v_head, q_tok, q_head;
+  int32_t Hkv, g, page_size, slots;
+  DevAppendItem items[kAppendItems];
+};
+
 // Forward shared by cas_prefix_attn_fwd (scratch == nullptr: the caller's
 // workspace, tables through the pinned staging ring) and the no-allocation
 // forward (scratch != nullptr: after validation, scratch() yields the device
@@ -307,5 +349,7 @@ hipError_t launch_bwd_prologue_bf16(const PreParams &p, int D, hipStream_t s);
 hipError_t launch_adam_bf16(const AdamParams &p, int D, int n_chunks, hipStream_t s);
 hipError_t launch_decode_bf16(const DecodeParams &p, int D, int n_work, int row_blocks, hipStream_t s);
 hipError_t launch_decode_merge_bf16(const DecodeParams &p, int D, int max_split, hipStream_t s);
+hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_groups, hipStream_t s);
+hipError_t launch_append(const AppendParams &p, int D, int n_items, int head_groups, hipStream_t s);
 
 }  // namespace cas

@@ -1,0 +1,441 @@
+// Host side of the rotary positions and of appending to the paged cache:
+// argument validation, plans and launches. Validation is host code and runs
+// before any HIP call.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <exception>
+#include <memory>
+#include <string>
+#include <vector>
+
+#include "../../include/cas.h"
+#include "cas_host.h"
+#include "cas_internal.h"
+
+using namespace cas;
+
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+std::string str(int64_t x) { return std::to_string(x); }
+
+// No exception leaves a C entry (host memory for the plan's tables may run out).
+template <typename F>
+cas_status_t guarded(F &&f) {
+  try {
+    return f();
+  } catch (const std::exception &e) {
+    return set_error(CAS_ERR_UNSUPPORTED, std::string("host memory: ") + e.what());
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rotary positions
+// ---------------------------------------------------------------------------
+cas_status_t check_rope(const cas_rope_t *r, int head_dim) {
+  if (!r) return set_error(CAS_ERR_INVALID_ARGUMENT, "rope is NULL");
+  if (r->layout != CAS_ROPE_HALF && r->layout != CAS_ROPE_INTERLEAVED)
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "unknown rope layout");
+  if (r->rotary_dim < 16 || r->rotary_dim > head_dim || r->rotary_dim % 16)
+    return set_error(CAS_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16 in [16, head_dim]");
+  if (!std::isfinite(r->scale) || !(r->scale > 0.0f)) return set_error(CAS_ERR_INVALID_ARGUMENT, "rope scale must be finite and > 0");
+  if (!r->turns) return set_error(CAS_ERR_INVALID_ARGUMENT, "rope turns is NULL");
+  if ((uintptr_t)r->turns & 7u) return set_error(CAS_ERR_ALIGNMENT, "rope turns must be 8-byte aligned");
+  return CAS_OK;
+}
+
+DevRope dev_rope(const cas_rope_t *r, bool inverse) {
+  return DevRope{r->turns, r->rotary_dim, r->scale, r->layout == CAS_ROPE_INTERLEAVED, inverse};
+}
+
+// What a strided [tokens, heads, head_dim] tensor covers, in bytes: rows of
+// `ext` bytes (of one or several heads or tokens), `stride` apart.
+struct Footprint {
+  uintptr_t base, end;
+  uint64_t stride, ext;
+  bool distinct;   // no two elements share an address
+};
+
+Footprint footprint(const void *x, int64_t tokens, int64_t heads, int64_t st, int64_t sh, int D, int es) {
+  int64_t outer = st, n_outer = tokens, inner = sh, n_inner = heads;
+  if (n_outer == 1 || (n_inner > 1 && inner > outer)) {
+    std::swap(outer, inner);
+    std::swap(n_outer, n_inner);
+  }
+  const int64_t in = n_inner > 1 ? inner : 0, out = n_outer > 1 ? outer : 0;
+  Footprint f;
+  f.base = (uintptr_t)x;
+  f.ext = (uint64_t)((n_inner - 1) * in + D) * es;
+  f.stride = (uint64_t)out * es;
+  f.end = f.base + (uint64_t)(n_outer - 1) * f.stride + f.ext;
+  f.distinct = (n_inner == 1 || in >= D) && (n_outer == 1 || f.stride >= f.ext);
+  return f;
+}
+
+// Two tensors that share a range of addresses are still apart when their rows
+// interleave (slices of one projection's output).
+bool apart(const Footprint &a, const Footprint &b) {
+  if (a.end <= b.base || b.end <= a.base) return true;
+  if (a.stride != b.stride || a.stride == 0 || a.ext > a.stride || b.ext > a.stride) return false;
+  const uint64_t S = a.stride, delta = b.base >= a.base ? (b.base - a.base) % S : (S - (a.base - b.base) % S) % S;
+  return delta >= a.ext && delta + b.ext <= S;
+}
+
+constexpr int64_t kMaxStride = (int64_t)1 << 31;   // (with the limits on tokens and heads, spans fit 64 bits)
+constexpr int64_t kMaxRopeTokens = (int64_t)1 << 26;
+
+cas_status_t check_strides(const char *what, int64_t st, int64_t sh, int es) {
+  if (st < 0 || sh < 0 || st > kMaxStride || sh > kMaxStride)
+    return set_error(CAS_ERR_INVALID_ARGUMENT, std::string(what) + ": strides must be in [0, 2^31]");
+  if ((st * es) % 16 || (sh * es) % 16)
+    return set_error(CAS_ERR_ALIGNMENT, std::string(what) + ": strides must be multiples of 16 bytes");
+  return CAS_OK;
+}
+
+// Heads of one token that the threads of a workgroup take at a time. The
+// angles of a token are computed once for every thread that works on it, so few
+// slots save arithmetic and many spread a few tokens over more threads.
+int head_slots(int64_t tokens, int D, int heads) {
+  const int all = 256 / (D / 16);
+  int slots = tokens >= 1024 ? 8 : all;
+  while (slots > 1 && slots / 2 >= heads) slots /= 2;
+  return slots;
+}
+
+cas_status_t rope_call(const cas_rope_t *rope, cas_dtype_t dtype, int32_t D, int64_t tokens, const int32_t *positions,
+                       const cas_rope_tensor_t *ts, int32_t n, int32_t inverse, hipStream_t stream) {
+  if (dtype != CAS_DTYPE_BF16 && dtype != CAS_DTYPE_FP32) return set_error(CAS_ERR_UNSUPPORTED, "dtype must be bf16 or fp32");
+  if (D != 64 && D != 128) return set_error(CAS_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  cas_status_t s = check_rope(rope, D);
+  if (s != CAS_OK) return s;
+  if (tokens < 0) return set_error(CAS_ERR_INVALID_ARGUMENT, "tokens must be >= 0");
+  if (tokens > kMaxRopeTokens) return set_error(CAS_ERR_UNSUPPORTED, "more than 2^26 tokens");
+  if (n < 1 || n > 4 || !ts) return set_error(CAS_ERR_INVALID_ARGUMENT, "1 to 4 tensors");
+  if (tokens == 0) return CAS_OK;
+  if (!positions) return set_error(CAS_ERR_INVALID_ARGUMENT, "positions is NULL");
+  if ((uintptr_t)positions & 3u) return set_error(CAS_ERR_ALIGNMENT, "positions must be 4-byte aligned");
+  const int es = dtype == CAS_DTYPE_BF16 ? 2 : 4;
+  RopeParams p{};
+  std::vector<Footprint> in, out;
+  int heads = 1;
+  for (int i = 0; i < n; ++i) {
+    const cas_rope_tensor_t &t = ts[i];
+    const std::string name = "tensor " + str(i);
+    if (!t.x || !t.y) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": x and y must be non-NULL");
+    if (t.heads < 1 || t.heads > (1 << 16)) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": heads must be in [1, 2^16]");
+    if (!aligned16(t.x) || !aligned16(t.y)) return set_error(CAS_ERR_ALIGNMENT, name + ": x and y must be 16-byte aligned");
+    if ((s = check_strides((name + " x").c_str(), t.x_stride_tok, t.x_stride_head, es)) != CAS_OK) return s;
+    if ((s = check_strides((name + " y").c_str(), t.y_stride_tok, t.y_stride_head, es)) != CAS_OK) return s;
+    in.push_back(footprint(t.x, tokens, t.heads, t.x_stride_tok, t.x_stride_head, D, es));
+    out.push_back(footprint(t.y, tokens, t.heads, t.y_stride_tok, t.y_stride_head, D, es));
+    if (!out.back().distinct) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": y overlaps itself");
+    p.t[i] = DevRopeTensor{t.x, t.y, t.x_stride_tok, t.x_stride_head, t.y_stride_tok, t.y_stride_head, t.heads, 0};
+    heads = std::max(heads, t.heads);
+  }
+  const Footprint pos{(uintptr_t)positions, (uintptr_t)positions + (uintptr_t)tokens * 4, 0, (uint64_t)tokens * 4, true};
+  const Footprint turns{(uintptr_t)rope->turns, (uintptr_t)rope->turns + (uintptr_t)rope->rotary_dim * 4, 0,
+                        (uint64_t)rope->rotary_dim * 4, true};
+  for (int i = 0; i < n; ++i) {
+    const std::string name = "tensor " + str(i) + ": y overlaps ";
+    if (!apart(out[i], pos) || !apart(out[i], turns)) return set_error(CAS_ERR_INVALID_ARGUMENT, name + "positions or turns");
+    for (int j = 0; j < n; ++j) {
+      const bool in_place = i == j && ts[i].x == ts[i].y && (tokens == 1 || ts[i].x_stride_tok == ts[i].y_stride_tok) &&
+                            (ts[i].heads == 1 || ts[i].x_stride_head == ts[i].y_stride_head);
+      if (!in_place && !apart(out[i], in[j])) return set_error(CAS_ERR_INVALID_ARGUMENT, name + "the x of tensor " + str(j));
+      if (i != j && !apart(out[i], out[j])) return set_error(CAS_ERR_INVALID_ARGUMENT, name + "the y of tensor " + str(j));
+    }
+  }
+  p.rope = dev_rope(rope, inverse != 0);
+  p.positions = positions;
+  p.tokens = tokens;
+  p.slots = head_slots(tokens, D, heads);
+  const hipError_t e = timed_launch("rope", stream, [&] { return launch_rope(p, dtype == CAS_DTYPE_BF16 ? kBF16 : kFP32, D, n, 1, stream); });
+  return e == hipSuccess ? CAS_OK : set_hip_error("rope launch", e);
+}
+
+// ---------------------------------------------------------------------------
+// Tables of paged requests
+// ---------------------------------------------------------------------------
+// As the paged decode checks them, except that requests without new tokens (and
+// without keys) are allowed: a padded batch has some.
+cas_status_t check_paged(const cas_decode_problem_t *p) {
+  if (!p) return set_error(CAS_ERR_INVALID_ARGUMENT, "problem is NULL");
+  if (p->batch < 1 || p->num_kv_heads < 1 || p->group_size < 1)
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "batch, num_kv_heads and group_size must be >= 1");
+  if (p->head_dim != 64 && p->head_dim != 128) return set_error(CAS_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  const int P = p->page_size;
+  if (P != 16 && P != 32 && P != 64 && P != 128) return set_error(CAS_ERR_UNSUPPORTED, "page_size must be 16, 32, 64 or 128");
+  const int64_t Hq = (int64_t)p->num_kv_heads * p->group_size;
+  if (Hq > (1 << 16)) return set_error(CAS_ERR_UNSUPPORTED, "num_kv_heads*group_size above 2^16");
+  if ((int64_t)P * p->num_kv_heads * p->head_dim * 2 >= ((int64_t)1 << 31))
+    return set_error(CAS_ERR_UNSUPPORTED, "page larger than 2 GiB");
+  if (p->num_pages < 1) return set_error(CAS_ERR_INVALID_ARGUMENT, "num_pages must be >= 1");
+  if (!p->q_offsets || !p->kv_lens || !p->page_offsets || !p->page_ids)
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "q_offsets, kv_lens, page_offsets and page_ids must be non-NULL");
+  if (p->q_offsets[0] != 0 || p->page_offsets[0] != 0)
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "q_offsets[0] and page_offsets[0] must be 0");
+  for (int b = 0; b < p->batch; ++b) {
+    const int64_t n = (int64_t)p->q_offsets[b + 1] - p->q_offsets[b], L = p->kv_lens[b];
+    const std::string name = "request " + str(b);
+    if (n < 0) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": q_offsets decrease");
+    if (L < n) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": kv_len below its new tokens");
+    if (L > (1 << 30)) return set_error(CAS_ERR_UNSUPPORTED, name + ": more than 2^30 keys");
+    if ((int64_t)p->page_offsets[b + 1] - p->page_offsets[b] != ceil_div(L, P))
+      return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": page count must be ceil(kv_len / page_size)");
+  }
+  if ((int64_t)p->q_offsets[p->batch] * Hq > INT32_MAX) return set_error(CAS_ERR_UNSUPPORTED, "new tokens * heads above 2^31");
+  for (int32_t i = 0; i < p->page_offsets[p->batch]; ++i)
+    if (p->page_ids[i] < 0 || p->page_ids[i] >= p->num_pages)
+      return set_error(CAS_ERR_INVALID_ARGUMENT, "page id " + str(i) + " out of range");
+  return CAS_OK;
+}
+
+// A problem with copies of its tables.
+struct OwnedProblem {
+  cas_decode_problem_t p;
+  std::vector<int32_t> tables;   // q_offsets, kv_lens, page_offsets, page_ids
+
+  void assign(const cas_decode_problem_t &o) {
+    const size_t B = (size_t)o.batch, ids = (size_t)o.page_offsets[B];
+    tables.clear();
+    tables.reserve(3 * B + 2 + ids);
+    auto copy = [&](const int32_t *src, size_t n) {
+      const int32_t *at = tables.data() + tables.size();
+      tables.insert(tables.end(), src, src + n);
+      return at;
+    };
+    p = o;
+    p.q_offsets = copy(o.q_offsets, B + 1);
+    p.kv_lens = copy(o.kv_lens, B);
+    p.page_offsets = copy(o.page_offsets, B + 1);
+    p.page_ids = copy(o.page_ids, ids);
+  }
+  bool matches(const cas_decode_problem_t *q) const {
+    if (!q || !q->q_offsets || !q->kv_lens || !q->page_offsets || !q->page_ids) return false;
+    if (q->batch != p.batch || q->num_kv_heads != p.num_kv_heads || q->group_size != p.group_size || q->head_dim != p.head_dim ||
+        q->softmax_scale != p.softmax_scale || q->page_size != p.page_size || q->num_pages != p.num_pages)
+      return false;
+    auto same = [](const int32_t *a, const int32_t *b, size_t n) { return std::memcmp(a, b, n * sizeof(int32_t)) == 0; };
+    const size_t B = (size_t)p.batch;
+    return same(q->q_offsets, p.q_offsets, B + 1) && same(q->kv_lens, p.kv_lens, B) &&
+           same(q->page_offsets, p.page_offsets, B + 1) && same(q->page_ids, p.page_ids, (size_t)p.page_offsets[B]);
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Appending to the paged cache
+// ---------------------------------------------------------------------------
+// n new tokens of request b from its off-th on that go to consecutive rows of
+// the pool from row `row0` of page `page` on.
+struct AppendRun {
+  int32_t b, off, n, page, row0;
+};
+
+// The runs of every request's new tokens; refuses tables that write a row which
+// is someone else's key, or a key twice.
+cas_status_t build_append(const cas_decode_problem_t *p, std::vector<AppendRun> &runs) {
+  cas_status_t s = check_paged(p);
+  if (s != CAS_OK) return s;
+  const int P = p->page_size, B = p->batch;
+  struct Write {
+    int32_t page, lo, hi, entry;   // rows [lo, hi) of a page, named by page_ids[entry]
+  };
+  std::vector<Write> w;
+  for (int b = 0; b < B; ++b) {
+    const int32_t n = p->q_offsets[b + 1] - p->q_offsets[b], L = p->kv_lens[b], e0 = p->page_offsets[b];
+    for (int32_t k = L - n; k < L;) {
+      const int32_t j = k / P, lo = k % P, hi = (int32_t)std::min<int64_t>(P, lo + (int64_t)(L - k)), page = p->page_ids[e0 + j];
+      w.push_back({page, lo, hi, e0 + j});
+      AppendRun *r = runs.empty() ? nullptr : &runs.back();
+      if (r && r->b == b && lo == 0 && (int64_t)r->page * P + r->row0 + r->n == (int64_t)page * P) r->n += hi - lo;
+      else runs.push_back({b, k - (L - n), hi - lo, page, lo});
+      k += hi - lo;
+    }
+  }
+  if (w.empty()) return CAS_OK;
+  std::sort(w.begin(), w.end(), [](const Write &a, const Write &b) { return a.page != b.page ? a.page < b.page : a.lo < b.lo; });
+  auto refuse = [&](int32_t page) {
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "page " + str(page) + ": new tokens would overwrite a key that the tables name elsewhere");
+  };
+  for (size_t i = 1; i < w.size(); ++i)
+    if (w[i].page == w[i - 1].page && w[i].lo < w[i - 1].hi) return refuse(w[i].page);
+  // Every other place that names a written page. A bit for the low 16 bits of
+  // each written id passes over nearly all entries at once.
+  std::vector<uint64_t> bits(1024, 0);
+  for (const Write &x : w) bits[(x.page & 0xffff) >> 6] |= 1ull << (x.page & 63);
+  for (int b = 0; b < B; ++b)
+    for (int32_t e = p->page_offsets[b]; e < p->page_offsets[b + 1]; ++e) {
+      const int32_t id = p->page_ids[e];
+      if (!(bits[(id & 0xffff) >> 6] >> (id & 63) & 1)) continue;
+      const int64_t seen = std::min<int64_t>(P, (int64_t)p->kv_lens[b] - (int64_t)(e - p->page_offsets[b]) * P);
+      auto it = std::lower_bound(w.begin(), w.end(), id, [](const Write &a, int32_t v) { return a.page < v; });
+      for (; it != w.end() && it->page == id; ++it)
+        if (it->entry != e && it->lo < seen) return refuse(id);
+    }
+  return CAS_OK;
+}
+
+cas_status_t run_append(const cas_decode_problem_t *p, const std::vector<AppendRun> &runs, const cas_rope_t *rope,
+                        const cas_append_t *t, void *k_pages, void *v_pages, hipStream_t stream) {
+  if (!t) return set_error(CAS_ERR_INVALID_ARGUMENT, "append tensors are NULL");
+  const int D = p->head_dim, Hkv = p->num_kv_heads, Hq = Hkv * p->group_size;
+  const int64_t Tq = p->q_offsets[p->batch];
+  cas_status_t s;
+  if (rope && (s = check_rope(rope, D)) != CAS_OK) return s;
+  if (!rope && t->q) return set_error(CAS_ERR_INVALID_ARGUMENT, "q without a rope");
+  if (Tq == 0) return CAS_OK;
+  if (!t->k || !t->v || !k_pages || !v_pages) return set_error(CAS_ERR_INVALID_ARGUMENT, "k, v, k_pages and v_pages must be non-NULL");
+  if (t->q && !t->q_out) return set_error(CAS_ERR_INVALID_ARGUMENT, "q without q_out");
+  if (!aligned16(t->k) || !aligned16(t->v) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(t->q) ||
+      (t->q && !aligned16(t->q_out)))
+    return set_error(CAS_ERR_ALIGNMENT, "tensors must be 16-byte aligned");
+  if ((s = check_strides("k", t->k_stride_tok, t->k_stride_head, 2)) != CAS_OK) return s;
+  if ((s = check_strides("v", t->v_stride_tok, t->v_stride_head, 2)) != CAS_OK) return s;
+  if (t->q && (s = check_strides("q", t->q_stride_tok, t->q_stride_head, 2)) != CAS_OK) return s;
+  auto span = [&](const void *x, int64_t heads, int64_t st, int64_t sh) {
+    return (uintptr_t)x + (uintptr_t)((Tq - 1) * st + (heads - 1) * sh + D) * 2;
+  };
+  const uintptr_t pool = (uintptr_t)p->num_pages * p->page_size * Hkv * D * 2;
+  std::vector<Interval> iv;
+  iv.push_back({(uintptr_t)t->k, span(t->k, Hkv, t->k_stride_tok, t->k_stride_head), false, 0, "k"});
+  iv.push_back({(uintptr_t)t->v, span(t->v, Hkv, t->v_stride_tok, t->v_stride_head), false, 0, "v"});
+  iv.push_back({(uintptr_t)k_pages, (uintptr_t)k_pages + pool, true, 1, "k_pages"});
+  iv.push_back({(uintptr_t)v_pages, (uintptr_t)v_pages + pool, true, 2, "v_pages"});
+  if (t->q) {
+    const bool in_place = t->q == t->q_out && (Hq == 1 || t->q_stride_head == D) && (Tq == 1 || t->q_stride_tok == (int64_t)Hq * D);
+    if (!in_place) iv.push_back({(uintptr_t)t->q, span(t->q, Hq, t->q_stride_tok, t->q_stride_head), false, 0, "q"});
+    iv.push_back({(uintptr_t)t->q_out, (uintptr_t)t->q_out + (uintptr_t)Tq * Hq * D * 2, true, 3, "q_out"});
+  }
+  if (rope) iv.push_back({(uintptr_t)rope->turns, (uintptr_t)rope->turns + (uintptr_t)rope->rotary_dim * 4, false, 0, "turns"});
+  std::string msg;
+  if (!overlap_free(iv, msg)) return set_error(CAS_ERR_INVALID_ARGUMENT, msg);
+  for (int b = 0; b < p->batch && t->starts; ++b) {
+    const int64_t n = p->q_offsets[b + 1] - p->q_offsets[b];
+    if ((int64_t)t->starts[b] + n > INT32_MAX) return set_error(CAS_ERR_INVALID_ARGUMENT, "request " + str(b) + ": position above 2^31");
+  }
+  AppendParams a{};
+  if (rope) a.rope = dev_rope(rope, false);
+  a.k = t->k;
+  a.v = t->v;
+  a.q = t->q;
+  a.k_pages = k_pages;
+  a.v_pages = v_pages;
+  a.q_out = t->q_out;
+  a.k_tok = t->k_stride_tok;
+  a.k_head = t->k_stride_head;
+  a.v_tok = t->v_stride_tok;
+  a.v_head = t->v_stride_head;
+  a.q_tok = t->q_stride_tok;
+  a.q_head = t->q_stride_head;
+  a.Hkv = Hkv;
+  a.g = p->group_size;
+  a.page_size = p->page_size;
+  const int rows = 256 / (D / 16);
+  a.slots = Tq >= 1024 ? 2 : rows;
+  const int per_wg = rows / a.slots;
+  const int head_groups = (int)std::min<int64_t>(64, ceil_div(t->q ? Hq : Hkv, 4 * a.slots));
+  int n_items = 0;
+  auto flush = [&]() -> hipError_t {
+    const int n = n_items;
+    n_items = 0;
+    return n ? timed_launch("append", stream, [&] { return launch_append(a, D, n, head_groups, stream); }) : hipSuccess;
+  };
+  for (const AppendRun &r : runs) {
+    const int32_t n_new = p->q_offsets[r.b + 1] - p->q_offsets[r.b];
+    const int32_t start = t->starts ? t->starts[r.b] : p->kv_lens[r.b] - n_new;
+    for (int32_t i = 0; i < r.n; i += per_wg) {
+      const int64_t row = (int64_t)r.row0 + i;
+      a.items[n_items++] = DevAppendItem{p->q_offsets[r.b] + r.off + i, r.page + (int32_t)(row / p->page_size), start + r.off + i,
+                                         (int16_t)(row % p->page_size), (int16_t)std::min(per_wg, r.n - i)};
+      if (n_items == kAppendItems) {
+        const hipError_t e = flush();
+        if (e != hipSuccess) return set_hip_error("append launch", e);
+      }
+    }
+  }
+  const hipError_t e = flush();
+  return e == hipSuccess ? CAS_OK : set_hip_error("append launch", e);
+}
+
+}  // namespace
+
+struct cas_append_plan {
+  OwnedProblem own;
+  std::vector<AppendRun> runs;
+};
+
+extern "C" {
+
+cas_status_t cas_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor, double original_len,
+                                  double low, double high, double *turns) {
+  if (!turns) return set_error(CAS_ERR_INVALID_ARGUMENT, "turns is NULL");
+  if (rotary_dim < 16 || rotary_dim > 128 || rotary_dim % 16)
+    return set_error(CAS_ERR_UNSUPPORTED, "rotary_dim must be a multiple of 16 in [16, 128]");
+  if (!std::isfinite(base) || !(base > 0.0)) return set_error(CAS_ERR_INVALID_ARGUMENT, "base must be finite and > 0");
+  if (scaling < CAS_ROPE_NONE || scaling > CAS_ROPE_BY_PARTS) return set_error(CAS_ERR_INVALID_ARGUMENT, "unknown scaling");
+  if (scaling != CAS_ROPE_NONE && (!std::isfinite(factor) || !(factor > 0.0)))
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "factor must be finite and > 0");
+  if (scaling == CAS_ROPE_BY_PARTS &&
+      (!std::isfinite(original_len) || !(original_len > 0.0) || !std::isfinite(low) || !std::isfinite(high) || !(low < high)))
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "by parts: original_len must be > 0 and low < high");
+  const double R = rotary_dim, two_pi = 6.283185307179586477;
+  if (scaling == CAS_ROPE_NTK) base *= std::pow(factor, R / (R - 2.0));
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / R) / two_pi;   // turns per position
+    if (scaling == CAS_ROPE_LINEAR) f /= factor;
+    if (scaling == CAS_ROPE_BY_PARTS) {
+      const double w = std::min(1.0, std::max(0.0, (original_len * f - low) / (high - low)));
+      f = (1.0 - w) * f / factor + w * f;
+    }
+    turns[i] = f;
+  }
+  return CAS_OK;
+}
+
+cas_status_t cas_rope(const cas_rope_t *rope, cas_dtype_t dtype, int32_t head_dim, int64_t tokens, const int32_t *positions,
+                      const cas_rope_tensor_t *tensors, int32_t n, int32_t inverse, void *hip_stream) {
+  return guarded([&] { return rope_call(rope, dtype, head_dim, tokens, positions, tensors, n, inverse, (hipStream_t)hip_stream); });
+}
+
+cas_status_t cas_paged_append(const cas_decode_problem_t *p, const cas_rope_t *rope, const cas_append_t *t, void *k_pages,
+                              void *v_pages, void *hip_stream) {
+  return guarded([&] {
+    std::vector<AppendRun> runs;
+    const cas_status_t s = build_append(p, runs);
+    return s == CAS_OK ? run_append(p, runs, rope, t, k_pages, v_pages, (hipStream_t)hip_stream) : s;
+  });
+}
+
+cas_status_t cas_paged_append_plan_create(const cas_decode_problem_t *p, cas_append_plan_t **plan) {
+  if (!plan) return set_error(CAS_ERR_INVALID_ARGUMENT, "plan is NULL");
+  *plan = nullptr;
+  return guarded([&] {
+    auto pl = std::make_unique<cas_append_plan>();
+    const cas_status_t s = build_append(p, pl->runs);
+    if (s != CAS_OK) return s;
+    pl->own.assign(*p);
+    *plan = pl.release();
+    return CAS_OK;
+  });
+}
+
+cas_status_t cas_paged_append_run(const cas_append_plan_t *plan, const cas_rope_t *rope, const cas_append_t *t, void *k_pages,
+                                  void *v_pages, void *hip_stream) {
+  if (!plan) return set_error(CAS_ERR_INVALID_ARGUMENT, "plan is NULL");
+  return guarded([&] { return run_append(&plan->own.p, plan->runs, rope, t, k_pages, v_pages, (hipStream_t)hip_stream); });
+}
+
+int32_t cas_paged_append_plan_matches(const cas_append_plan_t *plan, const cas_decode_problem_t *p) {
+  return plan && p && plan->own.matches(p);
+}
+
+cas_status_t cas_paged_append_plan_destroy(cas_append_plan_t *plan) {
+  delete plan;
+  return CAS_OK;
+}
+
+}  // extern "C"
