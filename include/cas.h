@@ -493,6 +493,55 @@ int32_t cas_paged_append_plan_matches(const cas_append_plan_t *plan, const cas_d
 cas_status_t cas_paged_append_plan_destroy(cas_append_plan_t *plan);
 
 /*
+ * Attention of a chunk of new tokens over the paged cache: prompts that are
+ * prefilled piece by piece behind their cartridges, and single decode tokens
+ * mixed with them in one step (paper: Section "Inference", several cartridges
+ * concatenated in order ahead of the prompt; ordinary causal masking of the
+ * tokens that follow). The problem, tensors and results are those of
+ * cas_paged_decode_fwd (the new tokens' K/V already in their pages:
+ * cas_paged_append); requests without new tokens are allowed. That call streams
+ * the keys once for every 32 rows (tokens x heads of a group) and is for steps
+ * of a few tokens per request; this one takes 256 rows at a time on the matrix
+ * cores. Rows of q and o behind the last request's are neither read nor
+ * written; lse is [Hq, Tq]. Keys past a query's own position do not reach it,
+ * whatever they and their values hold (NaN and infinities included).
+ *
+ * Under stream capture the launch tables travel as kernel arguments; a captured
+ * call uses its workspace at every replay, so graphs that may run at the same
+ * time need one each.
+ */
+cas_status_t cas_paged_chunk_workspace_size(const cas_decode_problem_t *p, size_t *bytes);
+cas_status_t cas_paged_chunk_fwd(const cas_decode_problem_t *p, const void *q, const void *k_pages, const void *v_pages,
+                                 void *o, float *lse, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/* In two steps, as with cas_paged_decode_plan_create: planned once for a step's size and its layers. */
+typedef struct cas_chunk_plan cas_chunk_plan_t;
+
+cas_status_t cas_paged_chunk_plan_create(const cas_decode_problem_t *p, cas_chunk_plan_t **plan, size_t *ws_bytes);
+cas_status_t cas_paged_chunk_run(const cas_chunk_plan_t *plan, const void *q, const void *k_pages, const void *v_pages,
+                                 void *o, float *lse, void *workspace, size_t ws_bytes, void *hip_stream);
+int32_t cas_paged_chunk_plan_matches(const cas_chunk_plan_t *plan, const cas_decode_problem_t *p);
+cas_status_t cas_paged_chunk_plan_destroy(cas_chunk_plan_t *plan);
+
+/*
+ * A plan's launch tables (host only; for tests and profiling tools). items may
+ * be NULL; otherwise it receives 9 values per workgroup in dispatch order: first
+ * token and token count of the request, its key count, its first entry of
+ * page_ids, the block's first row (tokens x group heads), KV head, first and one
+ * past the last 64-key tile, and the partial that it writes (-1: the result).
+ */
+typedef struct {
+  int32_t workgroups;
+  int32_t partials;
+  int32_t max_partials;   /* most of one block of rows (1: no merge) */
+  int32_t reserved;
+  int64_t key_tiles;      /* 64-key tiles walked by all workgroups */
+  size_t ws_bytes;
+} cas_chunk_plan_info_t;
+
+cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items);
+
+/*
  * Budget manager (paper: paragraphs "Budget Manager" and "Pool rotation";
  * hyperparameter table: budget B = 20, rotation interval R = 10, swap
  * fraction phi = 0.5, least-trained cartridges first, Adam moments of

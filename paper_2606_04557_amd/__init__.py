@@ -22,7 +22,8 @@ __all__ = ["Segment", "Problem", "CasError", "load", "prefix_attn_fwd", "prefix_
            "workspace_size", "plan_info", "set_tuning", "get_tuning", "cartridge_stage",
            "timing_enable", "timing_reset", "timing_read", "AdamCartridge", "adam_lr_scale",
            "cartridge_adam", "DecodeProblem", "paged_decode_fwd", "decode_plan", "plan_rotation", "CartridgePool",
-           "Rope", "RopeScaling", "rope_fwd", "rope_bwd", "paged_append"]
+           "Rope", "RopeScaling", "rope_fwd", "rope_bwd", "paged_append", "paged_chunk_fwd",
+           "paged_chunk_workspace_size", "chunk_plan"]
 
 
 class CasError(RuntimeError):
@@ -340,6 +341,20 @@ class _AppendPlan:
             self._destroy(self.handle)
 
 
+class _ChunkPlan:
+    """A launch plan of the chunk attention (cas_chunk_plan_t)."""
+
+    def __init__(self, problem: DecodeProblem):
+        lib, handle, n = load(), ctypes.c_void_p(), ctypes.c_size_t(0)
+        _check(lib.cas_paged_chunk_plan_create(ctypes.byref(problem.c), ctypes.byref(handle), ctypes.byref(n)))
+        self.handle, self.ws_bytes = handle, n.value
+        self._destroy = lib.cas_paged_chunk_plan_destroy
+
+    def __del__(self):
+        if hasattr(self, "_destroy"):
+            self._destroy(self.handle)
+
+
 class DecodeProblem:
     """Host tables of the paged calls (cas_decode_problem_t): per request its
     query (new token) count, key count and page list (pages of [page_size, Hkv,
@@ -364,7 +379,7 @@ class DecodeProblem:
         self._kv = (ctypes.c_int32 * max(B, 1))(*[int(x) for x in kv_lens])
         self._po = (ctypes.c_int32 * (B + 1))(*po)
         self._ids = (ctypes.c_int32 * max(len(ids), 1))(*ids)
-        self._plan = self._append_plan = None
+        self._plan = self._append_plan = self._chunk_plan = None
         I = ctypes.POINTER(ctypes.c_int32)
         self.c = _lib.DecodeProblem(B, num_kv_heads, group_size, head_dim, float(softmax_scale), page_size,
                                     int(num_pages), ctypes.cast(self._qo, I), ctypes.cast(self._kv, I),
@@ -381,6 +396,12 @@ class DecodeProblem:
         plan = self._append_plan
         if plan is None or not load().cas_paged_append_plan_matches(plan.handle, ctypes.byref(self.c)):
             plan = self._append_plan = _AppendPlan(self)
+        return plan
+
+    def chunk_plan(self) -> _ChunkPlan:
+        plan = self._chunk_plan
+        if plan is None or not load().cas_paged_chunk_plan_matches(plan.handle, ctypes.byref(self.c)):
+            plan = self._chunk_plan = _ChunkPlan(self)
         return plan
 
 
@@ -622,6 +643,60 @@ def paged_append(k, v, k_pages, v_pages, problem: DecodeProblem, rope: Optional[
                                            k_pages.data_ptr(), v_pages.data_ptr(), _stream_handle(dev, stream)))
     _on_device(dev, call)
     return q_out
+
+
+def paged_chunk_workspace_size(problem: DecodeProblem) -> int:
+    """Workspace bytes of paged_chunk_fwd on the problem, with the device current that will run it."""
+    return problem.chunk_plan().ws_bytes
+
+
+def paged_chunk_fwd(q, k_pages, v_pages, problem: DecodeProblem, o=None, lse=None, need_lse: bool = True, stream=None,
+                    workspace=None):
+    """Attention of each request's new tokens (q: [Tq, Hq, d] bf16, contiguous,
+    packed by request), chunks of prompts and single tokens mixed, over all its
+    keys in the pages: paged_decode_fwd for more than a few tokens per request.
+    Requests may have no new token. Returns O (as q; rows behind the last
+    request's are neither read nor written) and LSE [Hq, Tq] (fp32)."""
+    import torch
+    c = problem.c
+    Tq, Hkv, D, Hq, dev, dt = problem.Tq, c.num_kv_heads, c.head_dim, c.num_kv_heads * c.group_size, q.device, torch.bfloat16
+    if q.dim() != 3 or q.shape[0] < Tq:
+        raise ValueError(f"q must be [Tq, Hq, d] with Tq >= {Tq}")
+    _same_kind("q", q, (q.shape[0], Hq, D), dt, dev)
+    for what, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        _same_kind(what, t, (c.num_pages, c.page_size, Hkv, D), dt, dev)
+    if o is None:
+        o = _empty(stream, q.shape, dt, dev)
+    if lse is None and need_lse:
+        lse = _empty(stream, (Hq, Tq), torch.float32, dev)
+    _same_kind("o", o, q.shape, dt, dev)
+    if lse is not None:
+        _same_kind("lse", lse, (Hq, Tq), torch.float32, dev)
+    for what, t in (("q", q), ("k_pages", k_pages), ("v_pages", v_pages), ("o", o), ("lse", lse)):
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+
+    def call():
+        plan = problem.chunk_plan()
+        ws = workspace
+        if ws is None or ws.numel() * ws.element_size() < plan.ws_bytes:
+            ws = _empty(stream, (max(plan.ws_bytes, 1),), torch.uint8, dev)
+        elif ws.device != dev or not ws.is_contiguous():
+            raise ValueError("workspace must be contiguous and on the tensors' device")
+        _check(load().cas_paged_chunk_run(plan.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), o.data_ptr(),
+                                          _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _stream_handle(dev, stream)))
+    _on_device(dev, call)
+    return o, lse
+
+
+def chunk_plan(problem: DecodeProblem):
+    """The launch plan of paged_chunk_fwd (cas_paged_chunk_plan_info): its counts
+    and its workgroups (a tuple each)."""
+    plan, info = problem.chunk_plan(), _lib.ChunkPlanInfo()
+    _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), None))
+    items = (ctypes.c_int32 * (9 * max(info.workgroups, 1)))()
+    _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), items))
+    return info, list(zip(*[iter(items)] * 9))[:info.workgroups]
 
 
 def plan_rotation(steps: Sequence[int], active: Sequence[bool], budget: int, swap_fraction: float):

@@ -32,6 +32,8 @@ EXPORTS = [
     "cas_pool_load", "cas_pool_active", "cas_pool_end_step", "cas_pool_flush",
     "cas_prefix_attn_fwd_noalloc", "cas_pool_read_moments", "cas_rope_frequencies", "cas_rope", "cas_paged_append",
     "cas_paged_append_plan_create", "cas_paged_append_run", "cas_paged_append_plan_matches", "cas_paged_append_plan_destroy",
+    "cas_paged_chunk_workspace_size", "cas_paged_chunk_fwd", "cas_paged_chunk_plan_create", "cas_paged_chunk_run",
+    "cas_paged_chunk_plan_matches", "cas_paged_chunk_plan_destroy", "cas_paged_chunk_plan_info",
 ]
 
 CAS_ROPE_HALF = 0
@@ -100,6 +102,11 @@ class Append(ctypes.Structure):
                 ("k_stride_head", ctypes.c_int64), ("v_stride_tok", ctypes.c_int64), ("v_stride_head", ctypes.c_int64),
                 ("q", ctypes.c_void_p), ("q_stride_tok", ctypes.c_int64), ("q_stride_head", ctypes.c_int64),
                 ("q_out", ctypes.c_void_p), ("starts", ctypes.POINTER(ctypes.c_int32))]
+
+
+class ChunkPlanInfo(ctypes.Structure):
+    _fields_ = [("workgroups", ctypes.c_int32), ("partials", ctypes.c_int32), ("max_partials", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("key_tiles", ctypes.c_int64), ("ws_bytes", ctypes.c_size_t)]
 
 
 class PoolConfig(ctypes.Structure):
@@ -183,6 +190,14 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cas_paged_append_plan_matches.argtypes = [vp, P(DecodeProblem)]
     lib.cas_paged_append_plan_matches.restype = i32
     lib.cas_paged_append_plan_destroy.argtypes = [vp]
+    lib.cas_paged_chunk_workspace_size.argtypes = [P(DecodeProblem), P(sz)]
+    lib.cas_paged_chunk_fwd.argtypes = [P(DecodeProblem), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cas_paged_chunk_plan_create.argtypes = [P(DecodeProblem), P(vp), P(sz)]
+    lib.cas_paged_chunk_run.argtypes = [vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cas_paged_chunk_plan_matches.argtypes = [vp, P(DecodeProblem)]
+    lib.cas_paged_chunk_plan_matches.restype = i32
+    lib.cas_paged_chunk_plan_destroy.argtypes = [vp]
+    lib.cas_paged_chunk_plan_info.argtypes = [vp, P(ChunkPlanInfo), P(i32)]
     u8p = P(ctypes.c_uint8)
     lib.cas_pool_plan_rotation.argtypes = [P(i32), u8p, i32, i32, ctypes.c_float, P(i32), P(i32), P(i32)]
     lib.cas_pool_create.argtypes = [P(PoolConfig), P(vp)]
@@ -209,7 +224,9 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                  "cas_pool_plan_rotation", "cas_pool_create", "cas_pool_destroy", "cas_pool_host_cartridge", "cas_pool_load",
                  "cas_pool_active", "cas_pool_end_step", "cas_pool_flush", "cas_pool_read_moments",
                  "cas_rope_frequencies", "cas_rope", "cas_paged_append", "cas_paged_append_plan_create", "cas_paged_append_run",
-                 "cas_paged_append_plan_destroy"):
+                 "cas_paged_append_plan_destroy", "cas_paged_chunk_workspace_size", "cas_paged_chunk_fwd",
+                 "cas_paged_chunk_plan_create", "cas_paged_chunk_run", "cas_paged_chunk_plan_destroy",
+                 "cas_paged_chunk_plan_info"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib

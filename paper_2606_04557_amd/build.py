@@ -32,7 +32,7 @@ SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=und
              "-Xarch_host", "-fno-sanitize-recover=undefined", "-Xarch_host", "-fno-omit-frame-pointer",
              "-O1", "-g"]
 SOURCES = ["cas_api.cpp", "cas_paged.cpp", "cas_pool.cpp", "cas_fwd.hip", "cas_bwd.hip", "cas_bf16.hip", "cas_adam.hip",
-           "cas_decode.hip", "cas_noalloc.hip", "cas_rope.hip"]
+           "cas_decode.hip", "cas_noalloc.hip", "cas_rope.hip", "cas_chunk.hip"]
 ARCH = "gfx950"
 
 # -packed-fp32-ops: no packed fp32 ALU instructions are generated on gfx950.

@@ -311,6 +311,33 @@ struct AppendParams {
   DevAppendItem items[kAppendItems];
 };
 
+// Chunk attention over pages. One workgroup: up to 256 packed rows from row0 on
+// (row r of a request is its token r / g, head r % g of the KV head's group) of
+// a request with `len` new tokens from tok0 on, its last of kv_len keys, in the
+// pages page_ids[page0 ..], over 64-key tiles [tile0, tile1). part: which
+// partial it writes, or -1: no other workgroup has these rows.
+struct DevChunkItem {
+  int32_t tok0, len, kv_len, page0, row0, kvh, tile0, tile1, part;
+};
+// A block of rows whose keys were split: partials part0 .. part0 + nparts - 1.
+struct DevChunkMerge {
+  int32_t tok0, len, row0, kvh, part0, nparts;
+};
+struct ChunkParams {
+  const void *q;
+  const void *k_pages;
+  const void *v_pages;
+  void *o;
+  float *lse;                  // [Hq][Tq] or null
+  const DevChunkItem *items;
+  const DevChunkMerge *merges;
+  const int32_t *page_ids;
+  float *part_o;               // [partial][256][D], normalised
+  float *part_lse;             // [partial][256]
+  int32_t Hkv, g, page_size, Tq;
+  float scale_log2;
+};
+
 // Forward shared by cas_prefix_attn_fwd (scratch == nullptr: the caller's
 // workspace, tables through the pinned staging ring) and the no-allocation
 // forward (scratch != nullptr: after validation, scratch() yields the device
@@ -350,6 +377,8 @@ hipError_t launch_adam_bf16(const AdamParams &p, int D, int n_chunks, hipStream_
 hipError_t launch_decode_bf16(const DecodeParams &p, int D, int n_work, int row_blocks, hipStream_t s);
 hipError_t launch_decode_merge_bf16(const DecodeParams &p, int D, int max_split, hipStream_t s);
 hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_groups, hipStream_t s);
+hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_items, hipStream_t s);
+hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int n_merges, hipStream_t s);
 hipError_t launch_append(const AppendParams &p, int D, int n_items, int head_groups, hipStream_t s);
 
 }  // namespace cas

@@ -1,5 +1,5 @@
-// Host side of the rotary positions and of appending to the paged cache:
-// argument validation, plans and launches. Validation is host code and runs
+// Host side of the rotary positions, of appending to the paged cache and of the
+// chunk attention over it: argument validation, plans and launches. Validation is host code and runs
 // before any HIP call.
 #include <hip/hip_runtime.h>
 
@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <functional>
 #include <memory>
 #include <string>
 #include <vector>
@@ -361,11 +362,227 @@ cas_status_t run_append(const cas_decode_problem_t *p, const std::vector<AppendR
   return e == hipSuccess ? CAS_OK : set_hip_error("append launch", e);
 }
 
+// ---------------------------------------------------------------------------
+// Chunk attention over the paged cache
+// ---------------------------------------------------------------------------
+constexpr int kChunkRows = 256;     // packed rows of a workgroup
+constexpr int kChunkTile = 64;
+constexpr int kMaxChunkParts = 64;  // pieces of one block of rows
+
+struct ChunkPlan {
+  std::vector<DevChunkItem> items;   // in dispatch order
+  std::vector<DevChunkMerge> merges;
+  int32_t parts = 0, max_parts = 1;
+  int64_t tiles = 0;
+  size_t off_merges = 0, off_pages = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
+};
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// Blocks of rows of every request and KV head, cut along the key axis where the
+// blocks alone would leave compute units without work. Costs are in key tiles;
+// one workgroup runs per compute unit at a time and costs about kWgTiles beside
+// its tiles (dispatch, first loads, epilogue), a merge kMergeTiles for its
+// launch, and the partials' bytes at kBytesPerTile.
+constexpr double kWgTiles = 8.0, kMergeTiles = 3.0, kBytesPerTile = 5e6;
+
+cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
+  cas_status_t s = check_paged(p);
+  if (s != CAS_OK) return s;
+  if (!std::isfinite(p->softmax_scale) || !(p->softmax_scale > 0.0f))
+    return set_error(CAS_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
+  const int B = p->batch, g = p->group_size, Hkv = p->num_kv_heads;
+  const Topology topo = device_topology();
+  struct Block {
+    int32_t b, row0, rows, tiles;
+  };
+  std::vector<Block> blocks;   // of one KV head
+  int32_t longest = 0;
+  int64_t total = 0;
+  for (int b = 0; b < B; ++b) {
+    const int64_t n = p->q_offsets[b + 1] - p->q_offsets[b], nrows = n * g, before = p->kv_lens[b] - n;
+    for (int64_t r = 0; r < nrows; r += kChunkRows) {
+      const int64_t r1 = std::min<int64_t>(nrows, r + kChunkRows);
+      const int32_t nt = (int32_t)((before + (r1 - 1) / g) / kChunkTile + 1);   // up to its last query's own key
+      blocks.push_back({b, (int32_t)r, (int32_t)(r1 - r), nt});
+      longest = std::max(longest, nt);
+      total += nt;
+    }
+  }
+  if ((int64_t)blocks.size() * Hkv > INT32_MAX / kMaxChunkParts) return set_error(CAS_ERR_UNSUPPORTED, "too many workgroups");
+  auto pieces = [&](const Block &x, int64_t per) { return std::min<int64_t>(kMaxChunkParts, ceil_div(x.tiles, per)); };
+  // An estimate of the step with pieces of at most `per` tiles: the work spread
+  // evenly, the longest workgroup, and what the k + 1 shortest of the k * cus + 1
+  // longest ones take, of which one unit gets k + 1.
+  const int64_t cus = topo.cus;
+  std::vector<double> cost;
+  auto step_cost = [&](int64_t per) {
+    double sum = 0.0, bytes = 0.0;
+    cost.clear();
+    int64_t n = 0;
+    for (const Block &x : blocks) n += pieces(x, per) * Hkv;
+    const bool few = n <= 4 * cus;
+    double most = 0.0;
+    for (const Block &x : blocks) {
+      const int64_t k = pieces(x, per);
+      const double c = kWgTiles + (double)ceil_div(x.tiles, k);
+      sum += (kWgTiles * k + x.tiles) * Hkv;
+      most = std::max(most, c);
+      if (k > 1) bytes += (double)k * x.rows * p->head_dim * 4 * Hkv;
+      for (int64_t i = 0; few && i < k * Hkv; ++i) cost.push_back(c);
+    }
+    double t = std::max(sum / (double)cus, most);
+    if (few) {
+      std::sort(cost.begin(), cost.end(), std::greater<double>());
+      for (int64_t k = 1; k * cus < (int64_t)cost.size(); ++k) {
+        double c = 0.0;
+        for (int64_t i = k * cus - k; i <= k * cus; ++i) c += cost[i];
+        t = std::max(t, c);
+      }
+    }
+    return bytes > 0.0 ? t + kMergeTiles + bytes / kBytesPerTile : t;
+  };
+  int64_t best = std::max<int32_t>(1, longest);
+  if (!blocks.empty()) {
+    double best_cost = step_cost(best);
+    // Lengths that give the units 1, 2, ... pieces each, and shorter and shorter ones.
+    std::vector<int64_t> tries;
+    for (int r = 1; r <= 4; ++r) tries.push_back(ceil_div(total * Hkv, cus * r));
+    for (int k = 2; k <= 32; k += k < 8 ? 1 : 8) tries.push_back(ceil_div(longest, k));
+    for (int64_t per : tries) {
+      per = std::max<int64_t>(per, std::max<int64_t>(2, ceil_div(longest, kMaxChunkParts)));
+      if (per >= best) continue;
+      const double c = step_cost(per);
+      if (c < best_cost) {
+        best_cost = c;
+        best = per;
+      }
+    }
+  }
+  // The items of one KV head; its blocks' partials lie together.
+  std::vector<std::vector<DevChunkItem>> by_head(Hkv);
+  for (int kvh = 0; kvh < Hkv; ++kvh)
+    for (const Block &x : blocks) {
+      const int32_t k = (int32_t)pieces(x, best), tok0 = p->q_offsets[x.b], len = p->q_offsets[x.b + 1] - tok0;
+      if (k > 1) pl.merges.push_back({tok0, len, x.row0, kvh, pl.parts, k});
+      for (int32_t i = 0; i < k; ++i)
+        by_head[kvh].push_back({tok0, len, p->kv_lens[x.b], p->page_offsets[x.b], x.row0, kvh,
+                                (int32_t)((int64_t)x.tiles * i / k), (int32_t)((int64_t)x.tiles * (i + 1) / k), k > 1 ? pl.parts++ : -1});
+      pl.max_parts = std::max(pl.max_parts, k);
+      pl.tiles += x.tiles;
+    }
+  // Dispatch order. Workgroup i goes to XCD i mod X, each with its own L2, so a KV
+  // head's workgroups stay on one XCD (or on X / Hkv of them), longest first.
+  auto longer = [](const DevChunkItem &a, const DevChunkItem &b) { return a.tile1 - a.tile0 > b.tile1 - b.tile0; };
+  const int X = std::max(1, topo.xcds);
+  std::vector<std::vector<DevChunkItem>> share;
+  if (Hkv % X == 0) {
+    share.resize(X);
+    for (int kvh = 0; kvh < Hkv; ++kvh) {
+      auto &v = share[kvh % X];
+      v.insert(v.end(), by_head[kvh].begin(), by_head[kvh].end());
+    }
+  } else if (X % Hkv == 0) {
+    share.resize(X);
+    for (int kvh = 0; kvh < Hkv; ++kvh) {
+      std::stable_sort(by_head[kvh].begin(), by_head[kvh].end(), longer);
+      for (size_t i = 0; i < by_head[kvh].size(); ++i) share[kvh + Hkv * (i % (X / Hkv))].push_back(by_head[kvh][i]);
+    }
+  } else {
+    share.resize(1);
+    for (auto &v : by_head) share[0].insert(share[0].end(), v.begin(), v.end());
+  }
+  size_t rounds = 0;
+  for (auto &v : share) {
+    std::stable_sort(v.begin(), v.end(), longer);
+    rounds = std::max(rounds, v.size());
+  }
+  for (size_t i = 0; i < rounds; ++i)
+    for (auto &v : share)
+      if (i < v.size()) pl.items.push_back(v[i]);
+  pl.off_merges = align256(pl.items.size() * sizeof(DevChunkItem));
+  pl.off_pages = align256(pl.off_merges + pl.merges.size() * sizeof(DevChunkMerge));
+  pl.table_bytes = align256(pl.off_pages + (size_t)p->page_offsets[B] * sizeof(int32_t));
+  pl.off_plse = pl.table_bytes;
+  pl.off_po = align256(pl.off_plse + (size_t)pl.parts * kChunkRows * 4);
+  pl.bytes = align256(pl.off_po + (size_t)pl.parts * kChunkRows * p->head_dim * 4);
+  return CAS_OK;
+}
+
+cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const void *q, const void *k_pages, const void *v_pages,
+                       void *o, float *lse, void *workspace, size_t ws_bytes, hipStream_t stream) {
+  if (pl.items.empty()) return CAS_OK;
+  if (!q || !k_pages || !v_pages || !o) return set_error(CAS_ERR_INVALID_ARGUMENT, "q, k_pages, v_pages and o must be non-NULL");
+  if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || ((uintptr_t)lse & 3u))
+    return set_error(CAS_ERR_ALIGNMENT, "tensors must be 16-byte aligned (lse 4-byte)");
+  const uintptr_t rows = (uintptr_t)p->q_offsets[p->batch] * p->num_kv_heads * p->group_size, qbytes = rows * p->head_dim * 2;
+  const uintptr_t pool = (uintptr_t)p->num_pages * p->page_size * p->num_kv_heads * p->head_dim * 2;
+  cas_status_t s = check_workspace(workspace, ws_bytes, pl.bytes);
+  if (s != CAS_OK) return s;
+  std::vector<Interval> iv;
+  iv.push_back({(uintptr_t)q, (uintptr_t)q + qbytes, false, 0, "q"});
+  iv.push_back({(uintptr_t)k_pages, (uintptr_t)k_pages + pool, false, 0, "k_pages"});
+  iv.push_back({(uintptr_t)v_pages, (uintptr_t)v_pages + pool, false, 0, "v_pages"});
+  iv.push_back({(uintptr_t)o, (uintptr_t)o + qbytes, true, 1, "o"});
+  iv.push_back({(uintptr_t)workspace, (uintptr_t)workspace + pl.bytes, true, 2, "workspace"});
+  if (lse) iv.push_back({(uintptr_t)lse, (uintptr_t)lse + rows * 4, true, 3, "lse"});
+  std::string msg;
+  if (!overlap_free(iv, msg)) return set_error(CAS_ERR_INVALID_ARGUMENT, msg);
+  char *ws = (char *)workspace;
+  auto fill = [&](char *h) {
+    std::memcpy(h, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
+    if (!pl.merges.empty()) std::memcpy(h + pl.off_merges, pl.merges.data(), pl.merges.size() * sizeof(DevChunkMerge));
+    std::memcpy(h + pl.off_pages, p->page_ids, (size_t)p->page_offsets[p->batch] * sizeof(int32_t));
+  };
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (stream && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
+  if (capture == hipStreamCaptureStatusActive) {
+    // A graph keeps kernel arguments, but not what the pinned ring holds now.
+    std::vector<char> h(pl.table_bytes, 0);
+    fill(h.data());
+    const hipError_t e = launch_table_args_upload(h.data(), pl.table_bytes, workspace, stream);
+    if (e != hipSuccess) return set_hip_error("table upload launch", e);
+  } else if ((s = upload_launch_tables(pl.table_bytes, workspace, stream, fill)) != CAS_OK) {
+    return s;
+  }
+  ChunkParams c{};
+  c.q = q;
+  c.k_pages = k_pages;
+  c.v_pages = v_pages;
+  c.o = o;
+  c.lse = lse;
+  c.items = (const DevChunkItem *)ws;
+  c.merges = (const DevChunkMerge *)(ws + pl.off_merges);
+  c.page_ids = (const int32_t *)(ws + pl.off_pages);
+  c.part_lse = (float *)(ws + pl.off_plse);
+  c.part_o = (float *)(ws + pl.off_po);
+  c.Hkv = p->num_kv_heads;
+  c.g = p->group_size;
+  c.page_size = p->page_size;
+  c.Tq = p->q_offsets[p->batch];
+  c.scale_log2 = p->softmax_scale * 1.4426950408889634f;
+  hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, (int)pl.items.size(), stream); });
+  if (e != hipSuccess) return set_hip_error("chunk launch", e);
+  // (A grid has at most 65,535 rows.)
+  for (size_t m = 0; m < pl.merges.size(); m += 65535) {
+    c.merges = (const DevChunkMerge *)(ws + pl.off_merges) + m;
+    const int n = (int)std::min<size_t>(65535, pl.merges.size() - m);
+    e = timed_launch("chunk_merge", stream, [&] { return launch_chunk_merge_bf16(c, p->head_dim, n, stream); });
+    if (e != hipSuccess) return set_hip_error("chunk_merge launch", e);
+  }
+  return CAS_OK;
+}
+
 }  // namespace
 
 struct cas_append_plan {
   OwnedProblem own;
   std::vector<AppendRun> runs;
+};
+
+struct cas_chunk_plan {
+  OwnedProblem own;
+  ChunkPlan plan;
 };
 
 extern "C" {
@@ -435,6 +652,70 @@ int32_t cas_paged_append_plan_matches(const cas_append_plan_t *plan, const cas_d
 
 cas_status_t cas_paged_append_plan_destroy(cas_append_plan_t *plan) {
   delete plan;
+  return CAS_OK;
+}
+
+cas_status_t cas_paged_chunk_workspace_size(const cas_decode_problem_t *p, size_t *bytes) {
+  if (!bytes) return set_error(CAS_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  return guarded([&] {
+    ChunkPlan pl;
+    const cas_status_t s = build_chunk(p, pl);
+    if (s == CAS_OK) *bytes = pl.bytes;
+    return s;
+  });
+}
+
+cas_status_t cas_paged_chunk_fwd(const cas_decode_problem_t *p, const void *q, const void *k_pages, const void *v_pages,
+                                 void *o, float *lse, void *workspace, size_t ws_bytes, void *hip_stream) {
+  return guarded([&] {
+    ChunkPlan pl;
+    const cas_status_t s = build_chunk(p, pl);
+    return s == CAS_OK ? run_chunk(p, pl, q, k_pages, v_pages, o, lse, workspace, ws_bytes, (hipStream_t)hip_stream) : s;
+  });
+}
+
+cas_status_t cas_paged_chunk_plan_create(const cas_decode_problem_t *p, cas_chunk_plan_t **plan, size_t *ws_bytes) {
+  if (!plan || !ws_bytes) return set_error(CAS_ERR_INVALID_ARGUMENT, "plan or ws_bytes is NULL");
+  *plan = nullptr;
+  return guarded([&] {
+    auto pl = std::make_unique<cas_chunk_plan>();
+    const cas_status_t s = build_chunk(p, pl->plan);
+    if (s != CAS_OK) return s;
+    pl->own.assign(*p);
+    *ws_bytes = pl->plan.bytes;
+    *plan = pl.release();
+    return CAS_OK;
+  });
+}
+
+cas_status_t cas_paged_chunk_run(const cas_chunk_plan_t *plan, const void *q, const void *k_pages, const void *v_pages,
+                                 void *o, float *lse, void *workspace, size_t ws_bytes, void *hip_stream) {
+  if (!plan) return set_error(CAS_ERR_INVALID_ARGUMENT, "plan is NULL");
+  return guarded([&] {
+    return run_chunk(&plan->own.p, plan->plan, q, k_pages, v_pages, o, lse, workspace, ws_bytes, (hipStream_t)hip_stream);
+  });
+}
+
+int32_t cas_paged_chunk_plan_matches(const cas_chunk_plan_t *plan, const cas_decode_problem_t *p) {
+  return plan && p && plan->own.matches(p);
+}
+
+cas_status_t cas_paged_chunk_plan_destroy(cas_chunk_plan_t *plan) {
+  delete plan;
+  return CAS_OK;
+}
+
+cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items) {
+  if (!plan || !info) return set_error(CAS_ERR_INVALID_ARGUMENT, "plan or info is NULL");
+  const ChunkPlan &pl = plan->plan;
+  *info = cas_chunk_plan_info_t{};
+  info->workgroups = (int32_t)pl.items.size();
+  info->partials = pl.parts;
+  info->max_partials = pl.max_parts;
+  info->key_tiles = pl.tiles;
+  info->ws_bytes = pl.bytes;
+  static_assert(sizeof(DevChunkItem) == 36, "a table of 32-bit values");
+  if (items && !pl.items.empty()) std::memcpy(items, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
   return CAS_OK;
 }
 
