@@ -6,105 +6,14 @@
 // operand reduced along its row axis comes from ds_read_b64_tr_b16 (V in the
 // forward, K in dQ) or, in dK/dV, from transposed copies of Q and dO that a
 // prologue kernel writes once per backward.
-#include <type_traits>
-#include <utility>
-
-#include "cas_device.h"
+#include "cas_bf16_pipe.h"
 
 namespace cas {
 
 namespace {
 
-constexpr int kNW = 8;                 // waves per workgroup
-constexpr int kFastThreads = kNW * 64;
-constexpr int kKT = 64;                // keys per tile (forward, dQ)
-constexpr int kFastRowsPerWave = 32;
-constexpr int kFastRowsPerWg = kNW * kFastRowsPerWave;   // 256
 constexpr int kDkdvLead = 6;           // dK/dV: LDS fragments in flight ahead of their MFMA
 constexpr int kDkdvPrio = 1;           // dK/dV: wave priority in a matrix phase (0 in VALU phases)
-constexpr int kRefMargin = 64;         // forward: row sums below 2^kRefMargin need no exact pass
-
-struct TileInfo {
-  const __bf16 *kp;
-  const __bf16 *vp;
-  int st;      // token stride in elements (the host keeps 128 rows within 32-bit offsets)
-  int nvalid;
-  int self0;   // first self key of the tile, or -1 for a cartridge tile
-};
-
-// f(integral_constant<int, 0>) ... f(integral_constant<int, N-1>), unrolled.
-template <typename F, int... Ks>
-__device__ __forceinline__ void static_for_impl(F &&f, std::integer_sequence<int, Ks...>) {
-  (f(std::integral_constant<int, Ks>{}), ...);
-}
-template <int N, typename F>
-__device__ __forceinline__ void static_for(F &&f) {
-  static_for_impl(f, std::make_integer_sequence<int, N>{});
-}
-
-// Scheduling groups: the next n MFMAs / LDS reads of the region, in order.
-template <int N>
-__device__ __forceinline__ void sched_mfma() { __builtin_amdgcn_sched_group_barrier(0x008, N, 0); }
-template <int N>
-__device__ __forceinline__ void sched_ds_read() { __builtin_amdgcn_sched_group_barrier(0x100, N, 0); }
-
-// Per-lane share of the direct-to-LDS copies of an R-row tile: the tile row
-// and element offset (swizzle applied) of each 16-byte chunk this lane moves
-// are fixed for the whole kernel, so a tile copy costs one multiply-add and
-// one copy instruction per chunk.
-template <int D, int R, int NW>
-struct CopyLanes {
-  static constexpr int CPR = D / 8;
-  static constexpr int NI = R * CPR / 64;             // 1 KiB wave instructions per tile
-  static constexpr int PER = (NI + NW - 1) / NW;      // instructions per wave
-  int row[PER];
-  int coff[PER];
-  __device__ __forceinline__ void init(int wave, int lane) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int pos = (wave + i * NW) * 64 + lane;
-      const int r = pos / CPR;
-      row[i] = r;
-      coff[i] = ((pos % CPR) ^ swz<D>(r)) * 8;
-    }
-  }
-  // Rows at or beyond nvalid (>= 1) re-read row nvalid-1 (finite; masked
-  // later). The copies go through a buffer resource spanning exactly the
-  // tile's rows (an out-of-range offset would read zeros, not fault), and
-  // as MUBUF LDS loads they are counted on vmcnt alone.
-  __device__ __forceinline__ void issue(char *tile, const __bf16 *base, int st, int nvalid, int wave) const {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) issue_one(tile, base, st, nvalid, wave, i);
-  }
-  // Instruction i (< PER) of this wave's share only.
-  __device__ __forceinline__ void issue_one(char *tile, const __bf16 *base, int st, int nvalid, int wave,
-                                            int i) const {
-    issue_rs(tile, make_rsrc(base, ((nvalid - 1) * st + D) * 2), st, nvalid, wave, i);
-  }
-  // The same through a given resource (an empty one writes zeros).
-  __device__ __forceinline__ void issue_rs(char *tile, BufRsrc rs, int st, int nvalid, int wave, int i) const {
-    const int inst = wave + i * NW;
-    if (NI % NW == 0 || inst < NI) dma16(rs, (min(row[i], nvalid - 1) * st + coff[i]) * 2, tile + inst * 1024);
-  }
-};
-
-// Pins register values at this point: the compiler may not move their
-// computation past it (e.g. across a barrier into the next phase).
-template <typename T, int N>
-__device__ __forceinline__ void fence_regs(T (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
-}
-
-// Workgroup barrier that orders LDS use: this wave's LDS reads have returned,
-// and the compiler moves no memory access across it. Outstanding direct
-// global->LDS copies are not waited for (wait_vmcnt does that).
-__device__ __forceinline__ void lds_barrier() {
-  __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0); vmcnt, expcnt untouched
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
 
 // The next dK/dV entry of a workgroup that has finished one (see DkdvParams):
 // `claimed` is what it drew from its own list's counter; past the list's end it
@@ -297,125 +206,27 @@ void fwd_bf16_kernel(FwdParams p) {
       return wave_active && !(s0_ >= 0 && s0_ > wave_t_hi);
     };
 
-    // Matrix phase as one software-pipelined sequence of MFMAs: the PV product
-    // of the previous tile (16 MFMAs, two transposed LDS reads per fragment),
-    // then the scores of this one (16 MFMAs, one LDS read per fragment). The
-    // fragment of MFMA k+LEAD is read while MFMA k runs, into a ring of LEAD+1
-    // registers, and the scheduling groups pin exactly that order, so the LDS
-    // latency hides behind the MFMA pipe across the PV -> S boundary too.
-    auto matrix = [&](auto DO_PV, auto DO_S, const char *kb, const char *vb) __attribute__((always_inline)) {
-      constexpr bool PV = decltype(DO_PV)::value, S = decltype(DO_S)::value;
-      constexpr int NPV = PV ? 4 * DT : 0;          // PV MFMAs
-      constexpr int N = NPV + (S ? 2 * NSTEP : 0);  // all MFMAs
-      constexpr int LEAD = 4, R = LEAD + 1;
-      // MFMA k < NPV: s = k / (2*DT), dt = (k / 2) % DT, key half hh = k % 2.
-      // MFMA k >= NPV: st = (k - NPV) / 2, score half hh = (k - NPV) % 2.
-      auto load = [&](auto K) __attribute__((always_inline)) {
-        constexpr int k = decltype(K)::value;
-        if constexpr (k < NPV) {
-          constexpr int s = k / (2 * DT), dt = (k / 2) % DT, hh = k % 2;
-          return tr_frag_at<D>(vb, to, 32 * hh + 16 * s, dt);
-        } else {
-          constexpr int st = (k - NPV) / 2, hh = (k - NPV) % 2;
-          return row_frag_at<D>(kb, ro, 32 * hh, st);
-        }
-      };
-      auto mma = [&](auto K, const bf16x8 &f) __attribute__((always_inline)) {
-        constexpr int k = decltype(K)::value;
-        if constexpr (k < NPV) {
-          constexpr int s = k / (2 * DT), dt = (k / 2) % DT, hh = k % 2;
-          oacc[dt] = Mma<__bf16>::run(f, pf[hh][s], oacc[dt]);
-        } else {
-          constexpr int st = (k - NPV) / 2, hh = (k - NPV) % 2;
-          if constexpr (hh == 0) s0 = Mma<__bf16>::run(f, qf[st], s0);
-          else s1 = Mma<__bf16>::run(f, qf[st], s1);
-        }
-      };
-      if constexpr (S) {
-        s0 = zero16();
-        s1 = zero16();
-      }
-      bf16x8 ring[R];
-      static_for<LEAD>([&](auto K) __attribute__((always_inline)) {
-        constexpr int k = decltype(K)::value;
-        if constexpr (k < N) ring[k % R] = load(K);
-      });
-      static_for<N>([&](auto K) __attribute__((always_inline)) {
-        constexpr int k = decltype(K)::value;
-        if constexpr (k + LEAD < N) ring[(k + LEAD) % R] = load(std::integral_constant<int, k + LEAD>{});
-        mma(K, ring[k % R]);
-      });
-      // Scheduling groups: the LEAD first fragments, then per MFMA k the reads
-      // of fragment k+LEAD.
-      static_for<LEAD>([&](auto K) __attribute__((always_inline)) {
-        constexpr int k = decltype(K)::value;
-        if constexpr (k < N) sched_ds_read<(k < NPV ? 2 : 1)>();
-      });
-      static_for<N>([&](auto K) __attribute__((always_inline)) {
-        constexpr int k = decltype(K)::value;
-        sched_mfma<1>();
-        if constexpr (k + LEAD < N) sched_ds_read<(k + LEAD < NPV ? 2 : 1)>();
-      });
-    };
     float alpha = 1.0f;   // exact pass: O rescale factor of the current tile
     // piece(n), n < kPieces: copy instruction n of the phase (group B's tile
     // copies), spread evenly over the exponentials.
     auto softmax = [&](auto MASK, int lim, auto &&piece) __attribute__((always_inline)) {
-      if constexpr (decltype(MASK)::value) {
-        // lim: last visible key of this lane's query within the tile. Register
-        // j of group G holds key crow(j, G) = crow(j, 0) + 4G, so comparing
-        // lim - 4G against compile-time constants needs no index registers.
-        const int limg = lim - 4 * G;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          s0[j] = crow(j, 0) <= limg ? s0[j] : -INFINITY;
-          s1[j] = 32 + crow(j, 0) <= limg ? s1[j] : -INFINITY;
-        }
-      }
-      auto tile_max = [&]() __attribute__((always_inline)) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < 16; j += 2) mx = fmaxf(fmaxf(mx, fmaxf(s0[j], s1[j])), fmaxf(s0[j + 1], s1[j + 1]));
-        return fmaxf(mx, xor32(mx)) * c;
-      };
+      if constexpr (decltype(MASK)::value) fwd_mask(lim, G, s0, s1);
       if constexpr (!kExact) {
         // Only until every row of the wave has seen a key.
         if (wave_any(m_run == -INFINITY)) {
-          const float mt = tile_max();
+          const float mt = fwd_tile_max(s0, s1, c);
           m_run = (m_run == -INFINITY) ? mt : m_run;
         }
       } else {
         // Running maximum; the sum is rescaled here, O by the caller (outside
         // its branches, so the accumulators are written in one place).
-        const float m_new = fmaxf(m_run, tile_max());
+        const float m_new = fmaxf(m_run, fwd_tile_max(s0, s1, c));
         alpha = (m_new == -INFINITY) ? 1.0f : fast_exp2(m_run - m_new);
         l_run *= alpha;
         m_run = m_new;
       }
       const float mu = (m_run == -INFINITY) ? 0.0f : m_run;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        s0[j] = fast_exp2(fmaf(s0[j], c, -mu));
-        s1[j] = fast_exp2(fmaf(s1[j], c, -mu));
-        constexpr int EPP = 16 / kPieces;
-        if (j % EPP == EPP - 1) {
-          asm volatile("" : "+v"(s0[j]), "+v"(s1[j]));   // keep the copies spread
-          piece(j / EPP);
-        }
-      }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        pf[0][s] = pack_bf16x8(s0, s);
-        pf[1][s] = pack_bf16x8(s1, s);
-      }
-      // Row sums in fp32 (the LSE needs them to better than bf16 rounding).
-      float la = 0.0f, lb = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        la += s0[j];
-        lb += s1[j];
-      }
-      l_run += la + lb;
+      l_run += fwd_weights<kPieces>(c, mu, s0, s1, pf, piece);
     };
 
     // G_j: PV of tile j-1 (V_{j-1} in vbp) and scores of tile j (K_j in kb),
@@ -424,7 +235,7 @@ void fwd_bf16_kernel(FwdParams p) {
     // read. (Conditionally skipping either half would make the register
     // allocator copy the accumulators around every such branch.)
     auto gphase = [&](int j, const char *kb, const char *vbp) __attribute__((always_inline)) {
-      if (j <= nt && wave_active) matrix(std::true_type{}, std::true_type{}, kb, vbp);
+      if (j <= nt && wave_active) fwd_matrix_phase<D>(kb, vbp, ro, to, qf, pf, s0, s1, oacc);
     };
     auto xphase_body = [&](int j, auto &&piece) __attribute__((always_inline)) {
       auto all_pieces = [&]() __attribute__((always_inline)) {

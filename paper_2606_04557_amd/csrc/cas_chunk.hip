@@ -5,18 +5,19 @@
 // Query i of a request's n new tokens sees keys 0 .. L - n + i of its L. The g
 // heads of a group share their KV head's keys, so a row is a (token, head) pair
 // and a workgroup of eight waves takes 256 of them, 32 per wave, over a range of
-// 64-key tiles: S^T = K Q^T, an online softmax (a lane owns one row; its partner
-// lane 32 away the other keys of the tile), O^T += V^T P^T with P^T straight from
-// the score registers. Tiles are gathered page by page: a copy instruction moves
-// 4 or 8 key rows, which lie in one page since pages are multiples of 16.
-#include "cas_device.h"
+// 64-key tiles, with the phases of the prefix forward: the two waves of a SIMD
+// take turns, one in a matrix phase (O += V^T P of the tile before, S = K Q^T of
+// this one) while the other is in its softmax phase (cas_bf16.hip has the
+// schedule). Here the tiles are gathered page by page, and the second pass for
+// rows that the fixed softmax reference does not fit is a plain loop.
+//
+// This file is compiled to honour NaN: that second pass also keeps values which
+// are not finite from the rows that do not see their keys.
+#include "cas_bf16_pipe.h"
 
 namespace cas {
 
 namespace {
-
-constexpr int kChunkWaves = 8;
-constexpr int kKT = 64;
 
 __device__ __forceinline__ bool odd16(unsigned bits) { return (bits & 0x7f80u) == 0x7f80u; }   // inf or NaN
 
@@ -24,7 +25,7 @@ __device__ __forceinline__ bool odd16(unsigned bits) { return (bits & 0x7f80u) =
 template <int D>
 __device__ __forceinline__ bool has_odd(const char *tile, int lane) {
   bool odd = false;
-#pragma unroll 4
+#pragma unroll 1
   for (int i = lane; i < kKT * D / 8; i += 64) {
     const u32x4 w = *reinterpret_cast<const u32x4 *>(tile + 16 * i);
 #pragma unroll
@@ -57,23 +58,32 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 v) {
 }
 
 template <int D>
-__global__ __launch_bounds__(kChunkWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+__global__ __launch_bounds__(kFastThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void chunk_bf16_kernel(ChunkParams p) {
-  constexpr int NSTEP = D / 16, DT = D / 32, TB = kKT * D * 2;
-  constexpr int CPR = D / 8, RPI = 64 / CPR, NI = kKT / RPI / kChunkWaves;   // copy instructions of a tile per wave
-  __shared__ __attribute__((aligned(1024))) char kb[2][TB];
-  __shared__ __attribute__((aligned(1024))) char vb[2][TB];
+  constexpr int NSTEP = D / 16, DT = D / 32;
+  constexpr int TB = kKT * D * 2;
+  constexpr int CPR = D / 8, RPI = 64 / CPR;   // 16-byte chunks of a key row, key rows of a copy instruction
+  constexpr int PER = kKT / RPI / 4;           // copy instructions of a tile for each of group B's four waves
+  __shared__ __attribute__((aligned(1024))) char kb0[TB];
+  __shared__ __attribute__((aligned(1024))) char kb1[TB];
+  __shared__ __attribute__((aligned(1024))) char kb2[TB];
+  __shared__ __attribute__((aligned(1024))) char vb0[TB];
+  __shared__ __attribute__((aligned(1024))) char vb1[TB];
+  __shared__ __attribute__((aligned(1024))) char vb2[TB];
+
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave >> 2, w4 = wave & 3;
   const int G = lane >> 5, n = lane & 31;
   const DevChunkItem it = load_const(p.items, (int)blockIdx.x);
-  const int g = p.g, Hkv = p.Hkv, Hq = Hkv * g, P = p.page_size;
-  const int nrows = min(it.len * g, it.row0 + kChunkWaves * 32);
-  const int row0 = it.row0 + wave * 32, my_row = row0 + n;
-  const int before = it.kv_len - it.len;                 // token t sees keys 0 .. before + t
-  const bool active = row0 < nrows;
-  const int lo = before + row0 / g, hi = before + (min(row0 + 32, nrows) - 1) / g;   // last keys of the wave's rows
-  const int my_t = my_row / g, my_last = before + my_t;
-  const int h = it.kvh * g + (my_row - my_t * g);
+  const int g = p.g, Hkv = p.Hkv, Hq = Hkv * g;
+  const int nrows = it.len * g;
+  const int row0 = it.row0 + wave * kFastRowsPerWave, my_row = row0 + n;
+  const bool wave_active = row0 < nrows;
+  const int before = it.kv_len - it.len;       // token t sees keys 0 .. before + t
+  const int last_lo = __builtin_amdgcn_readfirstlane(before + row0 / g);
+  const int last_hi = __builtin_amdgcn_readfirstlane(before + (min(row0 + kFastRowsPerWave, nrows) - 1) / g);
+  const int my_t = my_row / g;
+  const int nt = it.tile1 - it.tile0;
   const float c = p.scale_log2;
 
   RowOffsets<D> ro;
@@ -81,115 +91,235 @@ void chunk_bf16_kernel(ChunkParams p) {
   TrOffsets<D> to;
   to.init(lane);
   bf16x8 qf[NSTEP];
-#pragma unroll
-  for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
   if (my_row < nrows) {
-    const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + h) * D;
+    const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + it.kvh * g + (my_row - my_t * g)) * D;
 #pragma unroll
     for (int st = 0; st < NSTEP; ++st) qf[st] = *reinterpret_cast<const bf16x8 *>(rp + st * 16 + G * 8);
-  }
-
-  // Rows at or past kv_len go through a resource that ends before them: zeros.
-  const int row_bytes = Hkv * D * 2;
-  auto copy = [&](const void *pool, char *tile_buf, int tile) __attribute__((always_inline)) {
+  } else {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int inst = wave + i * kChunkWaves, r0 = inst * RPI, key = tile * kKT + r0;
-      const int valid = min(RPI, it.kv_len - key);
-      const int page = load_const(p.page_ids, it.page0 + min(key, it.kv_len - 1) / P);
-      const __bf16 *base = (const __bf16 *)pool + (((int64_t)page * P + (key & (P - 1))) * Hkv + it.kvh) * D;
-      const int r = lane / CPR;
-      dma16(make_rsrc(base, valid > 0 ? (valid - 1) * row_bytes + D * 2 : 0),
-            r * row_bytes + (((lane % CPR) ^ swz<D>(r0 + r)) << 4), tile_buf + inst * 1024);
-    }
+    for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
+  }
+  // Tile copies are waited for with partial vmcnt counts, which must not
+  // include these loads.
+  wait_vmcnt<0>();
+
+  // Copies. Instruction i of wave w4 moves key rows r0 .. r0 + RPI - 1 of a tile,
+  // r0 = RPI (w4 + 4 i), which lie in one page (pages are multiples of 16 rows).
+  // It has a resource of its own, which ends behind the request's last key: later
+  // rows read as zero, and are masked. Rows 16 apart share their swizzle, so one
+  // lane offset serves every instruction.
+  static_assert(4 * RPI % 16 == 0, "the swizzle of a wave's rows is the same for every instruction");
+  const int page_shift = __builtin_ctz(p.page_size), row_elems = Hkv * D;
+  const int lane_off = (lane / CPR) * row_elems * 2 + (((lane % CPR) ^ swz<D>(w4 * RPI + lane / CPR)) << 4);
+  struct Tile {
+    int key0;        // first key of the wave's first instruction
+    int page[PER];
+  };
+  auto tile_at = [&](int j) __attribute__((always_inline)) {
+    Tile t;
+    t.key0 = (it.tile0 + j) * kKT + w4 * RPI;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      t.page[i] = load_const(p.page_ids, it.page0 + (min(t.key0 + 4 * RPI * i, it.kv_len - 1) >> page_shift));
+    return t;
+  };
+  auto copy = [&](char *buf, const void *pool, const Tile &t, bool has, int i) __attribute__((always_inline)) {
+    const int key = t.key0 + 4 * RPI * i;
+    const int64_t row = ((int64_t)t.page[i] << page_shift) + (key & ((1 << page_shift) - 1));
+    const int valid = has ? min(RPI, it.kv_len - key) : 0;
+    dma16(make_rsrc((const __bf16 *)pool + row * row_elems + it.kvh * D, valid > 0 ? ((valid - 1) * row_elems + D) * 2 : 0),
+          lane_off, buf + (w4 + 4 * i) * 1024);
   };
 
   f32x16 oacc[DT];
+  float m_run = -INFINITY, l_run = 0.0f;   // exponent offset of this lane's row, row sum of its keys
+  auto live = [&](int j) __attribute__((always_inline)) { return wave_active && (it.tile0 + j) * kKT <= last_hi; };
+  constexpr int kPieces = 2 * PER;         // copy instructions of a softmax phase
+  static_assert(16 % kPieces == 0, "copies spread over the 16 exponential pairs");
+
+  {
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
-  float m = -INFINITY, l = 0.0f;
-  copy(p.k_pages, kb[0], it.tile0);
-  copy(p.v_pages, vb[0], it.tile0);
-  for (int tile = it.tile0; tile < it.tile1; ++tile) {
-    const int cur = (tile - it.tile0) & 1;
-    wait_vmcnt<0>();
-    __syncthreads();
-    if (tile + 1 < it.tile1) {
-      copy(p.k_pages, kb[cur ^ 1], tile + 1);
-      copy(p.v_pages, vb[cur ^ 1], tile + 1);
-    }
-    const int key0 = tile * kKT;
-    if (!active || key0 > hi) continue;
-    f32x16 s[2] = {zero16(), zero16()};
-#pragma unroll
-    for (int st = 0; st < NSTEP; ++st)
-#pragma unroll
-      for (int a = 0; a < 2; ++a) s[a] = Mma<__bf16>::run(row_frag_at<D>(kb[cur], ro, 32 * a, st), qf[st], s[a]);
-    if (key0 + kKT - 1 > lo) {
-      const int lim = my_last - key0 - 4 * G;
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+    f32x16 s0 = zero16(), s1 = zero16();
+    bf16x8 pf[2][2];
+    auto no_weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int a = 0; a < 2; ++a)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) s[a][j] = 32 * a + crow(j, 0) <= lim ? s[a][j] : -INFINITY;
+        for (int s = 0; s < 2; ++s) pf[a][s] = Mma<__bf16>::zero();
+    };
+    no_weights();
+    auto softmax = [&](auto MASK, int lim, auto &&piece) __attribute__((always_inline)) {
+      if constexpr (decltype(MASK)::value) fwd_mask(lim, G, s0, s1);
+      // Only until every row of the wave has seen a key.
+      if (wave_any(m_run == -INFINITY)) {
+        const float mt = fwd_tile_max(s0, s1, c);
+        m_run = (m_run == -INFINITY) ? mt : m_run;
+      }
+      const float mu = (m_run == -INFINITY) ? 0.0f : m_run;
+      l_run += fwd_weights<kPieces>(c, mu, s0, s1, pf, piece);
+    };
+    auto gphase = [&](int j, const char *kb, const char *vbp) __attribute__((always_inline)) {
+      if (j <= nt && wave_active) fwd_matrix_phase<D>(kb, vbp, ro, to, qf, pf, s0, s1, oacc);
+    };
+    auto xphase = [&](int j, auto &&piece) __attribute__((always_inline)) {
+      auto all_pieces = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < kPieces; ++n) piece(n);
+      };
+      if (j < 0 || j >= nt) {
+        all_pieces();
+        return;
+      }
+      if (!live(j)) {
+        no_weights();
+        all_pieces();
+        return;
+      }
+      const int key0 = (it.tile0 + j) * kKT;
+      if (key0 + kKT - 1 > last_lo) softmax(std::true_type{}, before + my_t - key0, piece);
+      else softmax(std::false_type{}, kKT - 1, piece);
+    };
+    Tile tk;   // of the K copied last, whose V is copied next
+    auto no_piece = [](int) {};
+    auto even_b = [&](int i, char *kbn, char *vbn) __attribute__((always_inline)) {
+      const Tile tv = tk;
+      const Tile tn = tile_at(min(i + 2, nt - 1));
+      const bool has_v = i + 1 < nt, has_k = i + 2 < nt;
+      xphase(i - 1, [&](int n) __attribute__((always_inline)) {
+        if (n < PER) copy(vbn, p.v_pages, tv, has_v, n);
+        else copy(kbn, p.k_pages, tn, has_k, n - PER);
+      });
+      tk = tn;
+      wait_vmcnt<2 * PER>();
+    };
+
+    // (At least one tile: the host lists no empty range.) G_0 multiplies V
+    // buffer 2 by P = 0: clear it so no stale bit pattern (a NaN) can reach O.
+    for (int i = tid; i < TB / 16; i += kFastThreads) reinterpret_cast<uint4 *>(vb2)[i] = uint4{0, 0, 0, 0};
+    if (grp == 1) {
+      tk = tile_at(0);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) copy(kb0, p.k_pages, tk, true, i);
+      wait_vmcnt<0>();
+      const Tile t1 = tile_at(min(1, nt - 1));
+#pragma unroll
+      for (int i = 0; i < PER; ++i) copy(vb0, p.v_pages, tk, true, i);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) copy(kb1, p.k_pages, t1, nt > 1, i);
+      tk = t1;
     }
-    float mx = -INFINITY;
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[a][j]);
-    const float m_new = fmaxf(m, fmaxf(mx, xor32(mx)) * c);
-    const float mu = m_new == -INFINITY ? 0.0f : m_new;
-    const float alpha = fast_exp2(m - mu);
-    float sum = 0.0f;
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        s[a][j] = fast_exp2(fmaf(s[a][j], c, -mu));
-        sum += s[a][j];
+    lds_barrier();
+    // Six phases per iteration (three tiles), so every buffer is a fixed LDS
+    // address: G_i reads K_i from kb[i%3] and V_{i-1} from vb[(i-1)%3]; the
+    // copies of phase 2i go to kb[(i+2)%3] and vb[(i+1)%3].
+    auto run = [&](auto GROUP_A) __attribute__((always_inline)) {
+      constexpr bool A = decltype(GROUP_A)::value;
+      auto even = [&](int i, const char *kbi, const char *vbp, char *kbn, char *vbn) __attribute__((always_inline)) {
+        if constexpr (A) gphase(i, kbi, vbp);
+        else even_b(i, kbn, vbn);
+        lds_barrier();
+      };
+      auto odd = [&](int i, const char *kbi, const char *vbp) __attribute__((always_inline)) {
+        if constexpr (A) xphase(i, no_piece);
+        else gphase(i, kbi, vbp);
+        lds_barrier();
+      };
+      for (int i = 0; i <= nt; i += 3) {
+        even(i, kb0, vb2, kb2, vb1);
+        odd(i, kb0, vb2);
+        if (i + 1 > nt) break;
+        even(i + 1, kb1, vb0, kb0, vb2);
+        odd(i + 1, kb1, vb0);
+        if (i + 2 > nt) break;
+        even(i + 2, kb2, vb1, kb1, vb0);
+        odd(i + 2, kb2, vb1);
       }
-    l = l * alpha + sum;
-    m = m_new;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
-    // A value that is not finite would reach, as 0 times it, the rows that do not
-    // see its key. In tiles that some rows see in part such values are left out
-    // of the product and added to the rows that do see them.
-    const bool odd_values = key0 + kKT - 1 > lo && has_odd<D>(vb[cur], lane);
-    if (odd_values) add_odd<D>(vb[cur], my_last - key0, G, oacc);
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        const bf16x8 pf = pack_bf16x8(s[a], st);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          bf16x8 vf = tr_frag_at<D>(vb[cur], to, 32 * a + 16 * st, dt);
-          if (odd_values) vf = finite_only(vf);
-          oacc[dt] = Mma<__bf16>::run(vf, pf, oacc[dt]);
-        }
-      }
+    };
+    if (grp == 0) run(std::true_type{});
+    else run(std::false_type{});
+    wait_vmcnt<0>();
   }
+
+  // Every wave reaches this point. A row sum that reached 2^kRefMargin or
+  // overflowed needs the exact online softmax, an O that is not finite may come
+  // from a key that its row does not see: the workgroup takes its tiles again,
+  // one after the other.
+  bool again = ((__float_as_uint(l_run) >> 23) & 0xffu) >= 127u + (unsigned)kRefMargin;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) again |= (__float_as_uint(oacc[dt][i]) & 0x7f800000u) == 0x7f800000u;
+  if (__syncthreads_or(again ? 1 : 0)) {
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+    m_run = -INFINITY;
+    l_run = 0.0f;
+#pragma unroll 1
+    for (int j = 0; j < nt; ++j) {
+      lds_barrier();   // every wave is done with the tile before
+      if (grp == 1) {
+        const Tile t = tile_at(j);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+          copy(kb0, p.k_pages, t, true, i);
+          copy(vb0, p.v_pages, t, true, i);
+        }
+        wait_vmcnt<0>();
+      }
+      lds_barrier();
+      if (!live(j)) continue;
+      const int key0 = (it.tile0 + j) * kKT, lim = before + my_t - key0;
+      const bool part = key0 + kKT - 1 > last_lo;   // some row sees the tile in part
+      f32x16 s0 = zero16(), s1 = zero16();
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) {
+        s0 = Mma<__bf16>::run(row_frag_at<D>(kb0, ro, 0, st), qf[st], s0);
+        s1 = Mma<__bf16>::run(row_frag_at<D>(kb0, ro, 32, st), qf[st], s1);
+      }
+      if (part) fwd_mask(lim, G, s0, s1);
+      const float m_new = fmaxf(m_run, fwd_tile_max(s0, s1, c));
+      const float mu = m_new == -INFINITY ? 0.0f : m_new;
+      const float alpha = fast_exp2(m_run - mu);
+      m_run = m_new;
+      bf16x8 pf[2][2];
+      l_run = l_run * alpha + fwd_weights<1>(c, mu, s0, s1, pf, [](int) {});
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
+      const bool odd = part && has_odd<D>(vb0, lane);
+      if (odd) add_odd<D>(vb0, lim, G, oacc);
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            bf16x8 vf = tr_frag_at<D>(vb0, to, 32 * a + 16 * h, dt);
+            if (odd) vf = finite_only(vf);
+            oacc[dt] = Mma<__bf16>::run(vf, pf[a][h], oacc[dt]);
+          }
+    }
+  }
+
+  const float lt = l_run + xor32(l_run);
   if (my_row >= nrows) return;
-  const float lt = l + xor32(l);
+  const int h = it.kvh * g + (my_row - my_t * g);
+  // (A piece of a split may hold no key that the row sees. A NaN sum stays NaN.)
   const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-  const float lse = lt == 0.0f ? -INFINITY : (m + log2f(lt)) * kLn2;
-  if (it.part < 0) {
-    __bf16 *op = (__bf16 *)p.o + (((int64_t)it.tok0 + my_t) * Hq + h) * D;
+  const float lse = lt == 0.0f ? -INFINITY : (m_run + log2f(lt)) * kLn2;
+  auto store = [&](auto *op) __attribute__((always_inline)) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int j = 0; j < 16; j += 4)
         store4(op + dt * 32 + crow(j, G), oacc[dt][j] * inv, oacc[dt][j + 1] * inv, oacc[dt][j + 2] * inv, oacc[dt][j + 3] * inv);
+  };
+  if (it.part < 0) {
+    store((__bf16 *)p.o + (((int64_t)it.tok0 + my_t) * Hq + h) * D);
     if (G == 0 && p.lse != nullptr) p.lse[(int64_t)h * p.Tq + it.tok0 + my_t] = lse;
   } else {
-    const int64_t R = (int64_t)it.part * (kChunkWaves * 32) + (my_row - it.row0);
-    float *op = p.part_o + R * D;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int j = 0; j < 16; j += 4)
-        store4(op + dt * 32 + crow(j, G), oacc[dt][j] * inv, oacc[dt][j + 1] * inv, oacc[dt][j + 2] * inv, oacc[dt][j + 3] * inv);
+    const int64_t R = (int64_t)it.part * kFastRowsPerWg + (my_row - it.row0);
+    store(p.part_o + R * D);
     if (G == 0) p.part_lse[R] = lse;
   }
 }
@@ -222,8 +352,8 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
 }  // namespace
 
 hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_items, hipStream_t s) {
-  if (D == 64) hipLaunchKernelGGL(chunk_bf16_kernel<64>, dim3((unsigned)n_items), dim3(kChunkWaves * 64), 0, s, p);
-  else hipLaunchKernelGGL(chunk_bf16_kernel<128>, dim3((unsigned)n_items), dim3(kChunkWaves * 64), 0, s, p);
+  if (D == 64) hipLaunchKernelGGL(chunk_bf16_kernel<64>, dim3((unsigned)n_items), dim3(kFastThreads), 0, s, p);
+  else hipLaunchKernelGGL(chunk_bf16_kernel<128>, dim3((unsigned)n_items), dim3(kFastThreads), 0, s, p);
   return hipGetLastError();
 }
 
