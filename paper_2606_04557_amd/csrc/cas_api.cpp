@@ -1427,10 +1427,6 @@ cas_status_t set_error(cas_status_t s, const std::string &msg) { return fail(s, 
 
 cas_status_t set_hip_error(const char *what, hipError_t e) { return hip_fail(what, e); }
 
-cas_status_t upload_launch_tables(size_t bytes, void *ws, hipStream_t stream, const std::function<void(char *)> &fill) {
-  return ring_upload(bytes, ws, stream, fill);
-}
-
 hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch) {
   return timed(name, s, launch);
 }

@@ -90,19 +90,6 @@ void chunk_bf16_kernel(ChunkParams p) {
   ro.init(n, G);
   TrOffsets<D> to;
   to.init(lane);
-  bf16x8 qf[NSTEP];
-  if (my_row < nrows) {
-    const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + it.kvh * g + (my_row - my_t * g)) * D;
-#pragma unroll
-    for (int st = 0; st < NSTEP; ++st) qf[st] = *reinterpret_cast<const bf16x8 *>(rp + st * 16 + G * 8);
-  } else {
-#pragma unroll
-    for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
-  }
-  // Tile copies are waited for with partial vmcnt counts, which must not
-  // include these loads.
-  wait_vmcnt<0>();
-
   // Copies. Instruction i of wave w4 moves key rows r0 .. r0 + RPI - 1 of a tile,
   // r0 = RPI (w4 + 4 i), which lie in one page (pages are multiples of 16 rows).
   // It has a resource of its own, which ends behind the request's last key: later
@@ -130,6 +117,25 @@ void chunk_bf16_kernel(ChunkParams p) {
     dma16(make_rsrc((const __bf16 *)pool + row * row_elems + it.kvh * D, valid > 0 ? ((valid - 1) * row_elems + D) * 2 : 0),
           lane_off, buf + (w4 + 4 * i) * 1024);
   };
+  // The first K tile is on its way while the queries are.
+  Tile tk;   // of the K copied last, whose V is copied next
+  if (grp == 1) {
+    tk = tile_at(0);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) copy(kb0, p.k_pages, tk, true, i);
+  }
+  bf16x8 qf[NSTEP];
+  if (my_row < nrows) {
+    const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + it.kvh * g + (my_row - my_t * g)) * D;
+#pragma unroll
+    for (int st = 0; st < NSTEP; ++st) qf[st] = *reinterpret_cast<const bf16x8 *>(rp + st * 16 + G * 8);
+  } else {
+#pragma unroll
+    for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
+  }
+  // Tile copies are waited for with partial vmcnt counts, which must not
+  // include these loads (and phase 0 reads the first K).
+  wait_vmcnt<0>();
 
   f32x16 oacc[DT];
   float m_run = -INFINITY, l_run = 0.0f;   // exponent offset of this lane's row, row sum of its keys
@@ -180,7 +186,6 @@ void chunk_bf16_kernel(ChunkParams p) {
       if (key0 + kKT - 1 > last_lo) softmax(std::true_type{}, before + my_t - key0, piece);
       else softmax(std::false_type{}, kKT - 1, piece);
     };
-    Tile tk;   // of the K copied last, whose V is copied next
     auto no_piece = [](int) {};
     auto even_b = [&](int i, char *kbn, char *vbn) __attribute__((always_inline)) {
       const Tile tv = tk;
@@ -198,10 +203,6 @@ void chunk_bf16_kernel(ChunkParams p) {
     // buffer 2 by P = 0: clear it so no stale bit pattern (a NaN) can reach O.
     for (int i = tid; i < TB / 16; i += kFastThreads) reinterpret_cast<uint4 *>(vb2)[i] = uint4{0, 0, 0, 0};
     if (grp == 1) {
-      tk = tile_at(0);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) copy(kb0, p.k_pages, tk, true, i);
-      wait_vmcnt<0>();
       const Tile t1 = tile_at(min(1, nt - 1));
 #pragma unroll
       for (int i = 0; i < PER; ++i) copy(vb0, p.v_pages, tk, true, i);
@@ -324,29 +325,74 @@ void chunk_bf16_kernel(ChunkParams p) {
   }
 }
 
-// The partials of a block of rows, weighted by their LSE: D / 4 lanes per row,
-// 4 channels each.
-template <int D>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p) {
-  constexpr int CPR = D / 4, RPW = 256 / CPR;
-  const DevChunkMerge mg = load_const(p.merges, (int)blockIdx.y);
-  const int c4 = threadIdx.x % CPR, r = blockIdx.x * RPW + threadIdx.x / CPR, row = mg.row0 + r;
-  if (row >= mg.len * p.g) return;
-  const int64_t R = (int64_t)mg.part0 * 256 + r;
+// The partials of a block of rows, weighted by their LSE. A row is D/4 lanes of 4
+// channels each, GR of these groups taking every GR-th partial; their sums meet
+// in LDS. Blocks of at most kChunkFewRows rows come first in the list and have
+// units for those only, so that single tokens do not cost a chunk's workgroups.
+template <int D, int GR>
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p, int few) {
+  constexpr int CPR = D / 4;
+  constexpr int RPW = 256 / (CPR * GR);   // rows per workgroup
+  constexpr int UF = kChunkFewRows / RPW, UA = kFastRowsPerWg / RPW;   // units of a block
+  __shared__ f32x4 acc_l[256];
+  __shared__ float w_l[256];
+  const int tid = threadIdx.x, c4 = tid % CPR, gr = (tid / CPR) % GR;
+  const int bid = blockIdx.x;
+  const int which = bid < few * UF ? bid / UF : few + (bid - few * UF) / UA;
+  const int unit = bid < few * UF ? bid % UF : (bid - few * UF) % UA;
+  const DevChunkMerge mg = load_const(p.merges, which);
+  const int nrows = min(mg.len * p.g - mg.row0, kFastRowsPerWg);
+  if (unit * RPW >= nrows) return;
+  const int r = unit * RPW + tid / (CPR * GR);
+  const int64_t R = (int64_t)mg.part0 * kFastRowsPerWg + min(r, nrows - 1);
+  const float *lses = p.part_lse + R;
   float mx = -INFINITY;
-  for (int i = 0; i < mg.nparts; ++i) mx = fmaxf(mx, p.part_lse[R + 256 * i]);
+  for (int i = c4; i < mg.nparts; i += CPR) mx = fmaxf(mx, lses[i * kFastRowsPerWg]);
+#pragma unroll
+  for (int m = CPR / 2; m >= 1; m >>= 1) mx = fmaxf(mx, __shfl_xor(mx, m, CPR));
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   float w_sum = 0.0f;
-  for (int i = 0; i < mg.nparts; ++i) {
-    const float ls = p.part_lse[R + 256 * i];
+#pragma unroll 4
+  for (int i = gr; i < mg.nparts; i += GR) {
+    const float ls = lses[i * kFastRowsPerWg];
     const float w = ls == -INFINITY ? 0.0f : expf(ls - mx);
     w_sum += w;
-    acc += w * *reinterpret_cast<const f32x4 *>(p.part_o + (R + 256 * i) * D + 4 * c4);
+    acc += w * *reinterpret_cast<const f32x4 *>(p.part_o + (R + (int64_t)i * kFastRowsPerWg) * D + 4 * c4);
   }
+  if constexpr (GR > 1) {
+    acc_l[tid] = acc;
+    w_l[tid] = w_sum;
+    __syncthreads();
+    if (gr == 0) {
+#pragma unroll
+      for (int k = 1; k < GR; ++k) {
+        acc += acc_l[tid + k * CPR];
+        w_sum += w_l[tid + k * CPR];
+      }
+    }
+  }
+  if (gr != 0 || r >= nrows) return;
   const float inv = w_sum == 0.0f ? 0.0f : 1.0f / w_sum;
-  const int t = row / p.g, h = mg.kvh * p.g + (row - t * p.g), Hq = p.Hkv * p.g;
+  const int row = mg.row0 + r, t = row / p.g, h = mg.kvh * p.g + (row - t * p.g), Hq = p.Hkv * p.g;
   store4((__bf16 *)p.o + (((int64_t)mg.tok0 + t) * Hq + h) * D + 4 * c4, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
   if (c4 == 0 && p.lse != nullptr) p.lse[(int64_t)h * p.Tq + mg.tok0 + t] = w_sum == 0.0f ? -INFINITY : mx + logf(w_sum);
+}
+
+// Copies the launch tables to the workspace and then says so to the host, which
+// may fill their slot anew: a flag in host memory instead of an event, whose
+// barrier kept the next kernel waiting for 6 us.
+__global__ __launch_bounds__(1024) void table_flag_kernel(uint4 *dst, const uint4 *src, int64_t n16, uint32_t *flag, uint32_t value) {
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < n16; i += 1024) dst[i] = src[i];
+  __syncthreads();   // (every load has returned)
+  if (threadIdx.x == 0) __hip_atomic_store(flag, value, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_SYSTEM);
+}
+
+template <int D, int GR>
+void launch_chunk_merge_t(const ChunkParams &p, int few, int n_merges, hipStream_t s) {
+  constexpr int RPW = 256 / (D / 4 * GR);
+  const int64_t grid = (int64_t)few * (kChunkFewRows / RPW) + (int64_t)(n_merges - few) * (kFastRowsPerWg / RPW);
+  hipLaunchKernelGGL((chunk_merge_kernel<D, GR>), dim3((unsigned)grid), dim3(256), 0, s, p, few);
 }
 
 }  // namespace
@@ -357,9 +403,15 @@ hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_items, hipStream
   return hipGetLastError();
 }
 
-hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int n_merges, hipStream_t s) {
-  if (D == 64) hipLaunchKernelGGL(chunk_merge_kernel<64>, dim3(256 * 64 / 4 / 256, (unsigned)n_merges), dim3(256), 0, s, p);
-  else hipLaunchKernelGGL(chunk_merge_kernel<128>, dim3(256 * 128 / 4 / 256, (unsigned)n_merges), dim3(256), 0, s, p);
+// Eight groups a row where each takes two partials or more (few rows, then), else two.
+hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_merges, int max_parts, hipStream_t s) {
+  if (D == 64) max_parts >= 16 ? launch_chunk_merge_t<64, 8>(p, few, n_merges, s) : launch_chunk_merge_t<64, 2>(p, few, n_merges, s);
+  else max_parts >= 16 ? launch_chunk_merge_t<128, 8>(p, few, n_merges, s) : launch_chunk_merge_t<128, 2>(p, few, n_merges, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_table_flag(void *dst, const void *src, size_t bytes, uint32_t *flag, uint32_t value, hipStream_t s) {
+  hipLaunchKernelGGL(table_flag_kernel, dim3(1), dim3(1024), 0, s, (uint4 *)dst, (const uint4 *)src, (int64_t)(bytes / 16), flag, value);
   return hipGetLastError();
 }
 

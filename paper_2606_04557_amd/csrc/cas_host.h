@@ -31,10 +31,6 @@ bool overlap_free(std::vector<Interval> &iv, std::string &msg);
 // CAS_ERR_WORKSPACE (and the size that the call needs) unless ws holds `need` bytes.
 cas_status_t check_workspace(void *ws, size_t have, size_t need);
 
-// Copies `bytes` of launch tables, written by fill() into pinned memory, to ws
-// on the stream.
-cas_status_t upload_launch_tables(size_t bytes, void *ws, hipStream_t stream, const std::function<void(char *)> &fill);
-
 // launch(), bracketed by timing events while cas_timing_enable is on.
 hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch);
 

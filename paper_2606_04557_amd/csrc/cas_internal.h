@@ -323,6 +323,7 @@ struct DevChunkItem {
 struct DevChunkMerge {
   int32_t tok0, len, row0, kvh, part0, nparts;
 };
+constexpr int kChunkFewRows = 32;
 struct ChunkParams {
   const void *q;
   const void *k_pages;
@@ -378,7 +379,11 @@ hipError_t launch_decode_bf16(const DecodeParams &p, int D, int n_work, int row_
 hipError_t launch_decode_merge_bf16(const DecodeParams &p, int D, int max_split, hipStream_t s);
 hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_groups, hipStream_t s);
 hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_items, hipStream_t s);
-hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int n_merges, hipStream_t s);
+// n_merges blocks, of which the first `few` have at most kChunkFewRows rows.
+hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_merges, int max_parts, hipStream_t s);
+// Copies `bytes` (a multiple of 16) of pinned host memory to device memory and
+// then sets *flag (pinned host memory) to value.
+hipError_t launch_table_flag(void *dst, const void *src, size_t bytes, uint32_t *flag, uint32_t value, hipStream_t s);
 hipError_t launch_append(const AppendParams &p, int D, int n_items, int head_groups, hipStream_t s);
 
 }  // namespace cas

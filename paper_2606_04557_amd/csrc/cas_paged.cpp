@@ -8,8 +8,11 @@
 #include <cstring>
 #include <exception>
 #include <functional>
+#include <map>
 #include <memory>
+#include <mutex>
 #include <string>
+#include <thread>
 #include <vector>
 
 #include "../../include/cas.h"
@@ -371,8 +374,8 @@ constexpr int kMaxChunkParts = 64;  // pieces of one block of rows
 
 struct ChunkPlan {
   std::vector<DevChunkItem> items;   // in dispatch order
-  std::vector<DevChunkMerge> merges;
-  int32_t parts = 0, max_parts = 1;
+  std::vector<DevChunkMerge> merges;   // the blocks of few rows first
+  int32_t parts = 0, max_parts = 1, few = 0;
   int64_t tiles = 0;
   size_t off_merges = 0, off_pages = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
 };
@@ -451,7 +454,7 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
     for (int k = 2; k <= 32; k += k < 8 ? 1 : 8) tries.push_back(ceil_div(longest, k));
     for (int64_t per : tries) {
       per = std::max<int64_t>(per, std::max<int64_t>(2, ceil_div(longest, kMaxChunkParts)));
-      if (per >= best) continue;
+      if (per >= longest) continue;
       const double c = step_cost(per);
       if (c < best_cost) {
         best_cost = c;
@@ -471,6 +474,9 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
       pl.max_parts = std::max(pl.max_parts, k);
       pl.tiles += x.tiles;
     }
+  pl.few = (int32_t)(std::stable_partition(pl.merges.begin(), pl.merges.end(), [&](const DevChunkMerge &m) {
+    return (int64_t)m.len * g - m.row0 <= kChunkFewRows;
+  }) - pl.merges.begin());
   // Dispatch order. Workgroup i goes to XCD i mod X, each with its own L2, so a KV
   // head's workgroups stay on one XCD (or on X / Hkv of them), longest first.
   auto longer = [](const DevChunkItem &a, const DevChunkItem &b) { return a.tile1 - a.tile0 > b.tile1 - b.tile0; };
@@ -509,6 +515,56 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   return CAS_OK;
 }
 
+// Pinned slots for launch tables on their way to a workspace, one ring per
+// device. A slot is free once the kernel that read it has set its flag.
+struct TableRing {
+  static constexpr int kSlots = 16;
+  char *host = nullptr;              // kSlots slots, then their flags
+  size_t slot_bytes = 0;
+  uint32_t want[kSlots] = {};        // value of the slot's flag when it is free
+  int next = 0;
+  uint32_t *flag(int i) const { return (uint32_t *)(host + kSlots * slot_bytes) + i; }
+  void wait(int i) const {
+    while (__atomic_load_n(flag(i), __ATOMIC_ACQUIRE) != want[i]) std::this_thread::yield();
+  }
+};
+std::mutex g_tables_mu;
+std::map<int, TableRing> g_tables;
+
+template <typename Fill>
+cas_status_t upload_tables(size_t bytes, void *ws, hipStream_t stream, Fill &&fill) {
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return set_hip_error("hipGetDevice", e);
+  std::lock_guard<std::mutex> lk(g_tables_mu);
+  TableRing &r = g_tables[dev];
+  if (bytes > r.slot_bytes) {
+    size_t sb = 64 << 10;
+    while (sb < bytes) sb *= 2;
+    char *host = nullptr;
+    // Coherent: the kernel reads slots that the host has just rewritten, and the
+    // host the flags that it writes.
+    e = hipHostMalloc((void **)&host, sb * TableRing::kSlots + 256, hipHostMallocCoherent);
+    if (e != hipSuccess) return set_hip_error("hipHostMalloc", e);
+    for (int i = 0; r.host && i < TableRing::kSlots; ++i) r.wait(i);
+    char *old = r.host;
+    r = TableRing{};
+    r.host = host;
+    r.slot_bytes = sb;
+    std::memset(host + sb * TableRing::kSlots, 0, 256);
+    if (old && (e = hipHostFree(old)) != hipSuccess) return set_hip_error("hipHostFree", e);
+  }
+  const int slot = r.next;
+  r.wait(slot);
+  char *h = r.host + (size_t)slot * r.slot_bytes;
+  fill(h);
+  e = launch_table_flag(ws, h, bytes, r.flag(slot), r.want[slot] + 1, stream);
+  if (e != hipSuccess) return set_hip_error("table upload launch", e);
+  ++r.want[slot];
+  r.next = (slot + 1) % TableRing::kSlots;
+  return CAS_OK;
+}
+
 cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const void *q, const void *k_pages, const void *v_pages,
                        void *o, float *lse, void *workspace, size_t ws_bytes, hipStream_t stream) {
   if (pl.items.empty()) return CAS_OK;
@@ -542,7 +598,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
     fill(h.data());
     const hipError_t e = launch_table_args_upload(h.data(), pl.table_bytes, workspace, stream);
     if (e != hipSuccess) return set_hip_error("table upload launch", e);
-  } else if ((s = upload_launch_tables(pl.table_bytes, workspace, stream, fill)) != CAS_OK) {
+  } else if ((s = upload_tables(pl.table_bytes, workspace, stream, fill)) != CAS_OK) {
     return s;
   }
   ChunkParams c{};
@@ -563,11 +619,10 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   c.scale_log2 = p->softmax_scale * 1.4426950408889634f;
   hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, (int)pl.items.size(), stream); });
   if (e != hipSuccess) return set_hip_error("chunk launch", e);
-  // (A grid has at most 65,535 rows.)
-  for (size_t m = 0; m < pl.merges.size(); m += 65535) {
-    c.merges = (const DevChunkMerge *)(ws + pl.off_merges) + m;
-    const int n = (int)std::min<size_t>(65535, pl.merges.size() - m);
-    e = timed_launch("chunk_merge", stream, [&] { return launch_chunk_merge_bf16(c, p->head_dim, n, stream); });
+  if (!pl.merges.empty()) {
+    e = timed_launch("chunk_merge", stream, [&] {
+      return launch_chunk_merge_bf16(c, p->head_dim, pl.few, (int)pl.merges.size(), pl.max_parts, stream);
+    });
     if (e != hipSuccess) return set_hip_error("chunk_merge launch", e);
   }
   return CAS_OK;
