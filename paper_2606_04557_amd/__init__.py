@@ -489,26 +489,46 @@ class Rope:
 
     def device_turns(self, device):
         """The frequencies on a GPU (float64 [rotary_dim/2])."""
-        return self._on(device)[1]
-
-    def _on(self, device):
         import torch
-        got = self._device.get(device)
+        device = torch.device(device)
+        return self._on(device.index if device.index is not None else torch.cuda.current_device())[1]
+
+    def _on(self, index: int):
+        got = self._device.get(index)
         if got is None:
-            t = torch.tensor(self.turns, dtype=torch.float64, device=device)
-            got = self._device[device] = (_lib.Rope(self._LAYOUTS[self.layout], self.rotary_dim, t.data_ptr(), self.scale), t)
+            import torch
+            t = torch.tensor(self.turns, dtype=torch.float64, device=torch.device("cuda", index))
+            got = self._device[index] = (_lib.Rope(self._LAYOUTS[self.layout], self.rotary_dim, t.data_ptr(), self.scale), t)
         return got
 
 
-def _on_device(device, call):
-    """call() with ``device`` the current one, as launches need it."""
+# These calls take a few microseconds on the GPU at their smallest, so their
+# marshalling is kept short: device numbers instead of device objects, and the
+# C structures packed in one go.
+_ROPE_TENSOR = struct.Struct("@PPqqqqi4x")
+_APPEND = struct.Struct("@PPqqqqPqqPP")
+assert _ROPE_TENSOR.size == ctypes.sizeof(_lib.RopeTensor) and _APPEND.size == ctypes.sizeof(_lib.Append)
+
+
+def _gpu(what: str, t) -> int:
+    """The number of the GPU that holds t."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{what} must be on a GPU, not on {t.device}")
+    return index
+
+
+def _on_device(index: int, stream, call) -> None:
+    """call(stream handle), checked, with GPU ``index`` the current one, as launches need it."""
     import torch
-    if device.type != "cuda":
-        raise ValueError(f"tensors must be on a GPU, not on {device}")
-    if device.index is None or device.index == torch.cuda.current_device():
-        return call()
-    with torch.cuda.device(device):
-        return call()
+    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if index == torch._C._cuda_getDevice():
+        status = call(handle)
+    else:
+        with torch.cuda.device(index):
+            status = call(handle)
+    if status != _lib.CAS_OK:
+        _check(status)
 
 
 def _empty(stream, shape, dtype, device):
@@ -520,68 +540,79 @@ def _empty(stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _same_kind(what: str, t, shape, dtype, device) -> None:
-    if tuple(t.shape) != tuple(shape):
+def _same_kind(what: str, t, shape, dtype, index: int) -> None:
+    if t.shape != shape:
         raise ValueError(f"{what} must be {list(shape)}, is {list(t.shape)}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, is {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{what} is on {t.device}, not on {device}")
+    if t.get_device() != index:
+        raise ValueError(f"{what} is on {t.device}, not on GPU {index}")
 
 
-def _token_strides(what: str, t) -> Tuple[int, int, int, int]:
-    """(tokens, heads, token stride, head stride) of a [.., tokens, heads, d] tensor; 0 for a stride that nothing uses."""
+def _token_strides(what: str, t) -> Tuple[int, int, int, int, int]:
+    """(tokens, heads, d, token stride, head stride) of a [.., tokens, heads, d]
+    tensor; 0 for a stride that nothing uses."""
     shape, st = t.shape, t.stride()
-    if len(shape) < 3:
+    dims = len(shape)
+    if dims == 3:
+        n, heads, d = shape
+        step, head_step, ch = st
+        if n <= 1:
+            step = 0
+    elif dims < 3:
         raise ValueError(f"{what} must be [.., tokens, heads, d]")
-    n = 1
-    step = st[-3]
-    for size, stride in zip(reversed(shape[:-2]), reversed(st[:-2])):
-        if size != 1:
-            if n == 1:
-                step = stride
-            elif stride != n * step:
-                raise ValueError(f"{what}: the leading dimensions have no common token stride")
-        n *= size
-    if shape[-1] > 1 and st[-1] != 1:
+    else:
+        n, step = 1, 0
+        for size, stride in zip(reversed(shape[:-2]), reversed(st[:-2])):
+            if size != 1:
+                if n == 1:
+                    step = stride
+                elif stride != n * step:
+                    raise ValueError(f"{what}: the leading dimensions have no common token stride")
+            n *= size
+        heads, d = shape[-2:]
+        head_step, ch = st[-2:]
+    if ch != 1 and d > 1:
         raise ValueError(f"{what}: channel stride must be 1")
-    return n, shape[-2], step if n > 1 else 0, st[-2] if shape[-2] > 1 else 0
+    return n, heads, d, step, head_step if heads > 1 else 0
 
 
 def _rope(xs, positions, rope: Rope, outs, stream, inverse: int) -> List[object]:
     import torch
-    xs = list(xs)
-    if not 1 <= len(xs) <= 4:
+    n = len(xs)
+    if not 1 <= n <= 4:
         raise ValueError("1 to 4 tensors")
-    x0 = xs[0]
-    dev, D = x0.device, x0.shape[-1]
-    outs = [None] * len(xs) if outs is None else list(outs)
-    if len(outs) != len(xs):
+    outs = [None] * n if outs is None else list(outs)
+    if len(outs) != n:
         raise ValueError("outs must have an entry per tensor")
-    tens = (_lib.RopeTensor * len(xs))()
-    T = None
-    for i, x in enumerate(xs):
-        n, heads, st, sh = _token_strides(f"tensor {i}", x)
-        if T is None:
-            T = n
-        if n != T or x.shape[-1] != D:
-            raise ValueError("the tensors must have the same tokens and head_dim")
-        if x.dtype != x0.dtype or x.device != dev:
-            raise ValueError("the tensors must have one dtype and device")
-        if outs[i] is None:
-            outs[i] = _empty(stream, x.shape, x.dtype, dev)
-        y = outs[i]
-        if y is not x:
-            _same_kind(f"output {i}", y, x.shape, x.dtype, dev)
-        _, _, yt, yh = _token_strides(f"output {i}", y)
-        tens[i] = _lib.RopeTensor(x.data_ptr(), y.data_ptr(), st, sh, yt, yh, heads)
-    if positions.dtype != torch.int32:
-        raise TypeError("positions must be int32")
-    if positions.numel() != T or not positions.is_contiguous() or positions.device != dev:
-        raise ValueError("positions must be contiguous, one per token, on the tensors' device")
+    x0 = xs[0]
+    dtype, index = x0.dtype, x0.get_device()
     code = _dtype_code(x0)
-    _on_device(dev, lambda: _check(load().cas_rope(ctypes.byref(rope._on(dev)[0]), code, D, T, positions.data_ptr(), tens,
-                                                   len(xs), inverse, _stream_handle(dev, stream))))
+    packed, T, D = b"", None, None
+    for i, x in enumerate(xs):
+        t, heads, d, st, sh = _token_strides("x", x)
+        if T is None:
+            T, D = t, d
+        elif t != T or d != D:
+            raise ValueError("the tensors must have the same tokens and head_dim")
+        elif x.dtype is not dtype or x.get_device() != index:
+            raise ValueError("the tensors must have one dtype and device")
+        y = outs[i]
+        if y is None:
+            y = outs[i] = _empty(stream, x.shape, dtype, x.device)
+        if y is x:
+            yt, yh = st, sh
+        else:
+            _same_kind("output", y, x.shape, dtype, index)
+            _, _, _, yt, yh = _token_strides("output", y)
+        packed += _ROPE_TENSOR.pack(x.data_ptr(), y.data_ptr(), st, sh, yt, yh, heads)
+    if positions.dtype is not torch.int32:
+        raise TypeError("positions must be int32")
+    if positions.numel() != T or not positions.is_contiguous() or positions.get_device() != index:
+        raise ValueError("positions must be contiguous, one per token, on the tensors' device")
+    _gpu("x", x0)
+    _on_device(index, stream, lambda handle: load().cas_rope(rope._on(index)[0], code, D, T, positions.data_ptr(), packed, n,
+                                                             inverse, handle))
     return outs
 
 
@@ -598,6 +629,14 @@ def rope_bwd(grads: Sequence[object], positions, rope: Rope, outs: Optional[Sequ
     return _rope(grads, positions, rope, outs, stream, 1)
 
 
+def _check_pools(k_pages, v_pages, c, dtype, index: int) -> None:
+    shape = (c.num_pages, c.page_size, c.num_kv_heads, c.head_dim)
+    _same_kind("k_pages", k_pages, shape, dtype, index)
+    _same_kind("v_pages", v_pages, shape, dtype, index)
+    if not (k_pages.is_contiguous() and v_pages.is_contiguous()):
+        raise ValueError("k_pages and v_pages must be contiguous")
+
+
 def paged_append(k, v, k_pages, v_pages, problem: DecodeProblem, rope: Optional[Rope] = None, q=None, q_out=None,
                  starts: Optional[Sequence[int]] = None, stream=None):
     """Writes the problem's new tokens, k and v ([Tq, Hkv, d] bf16, packed by
@@ -608,40 +647,42 @@ def paged_append(k, v, k_pages, v_pages, problem: DecodeProblem, rope: Optional[
     place among the keys. Rows of k, v and q behind the last request's are not
     read, and no other row of the pools is written."""
     import torch
-    c = problem.c
-    Tq, Hkv, D, Hq, dev, dt = problem.Tq, c.num_kv_heads, c.head_dim, c.num_kv_heads * c.group_size, k.device, torch.bfloat16
-    for what, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-        _same_kind(what, t, (c.num_pages, c.page_size, Hkv, D), dt, dev)
-        if not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous")
-    a = _lib.Append()
-    for what, t, heads in (("k", k, Hkv), ("v", v, Hkv), ("q", q, Hq)):
-        if t is None:
-            continue
-        n, h, st, sh = _token_strides(what, t)
-        if n < Tq:
-            raise ValueError(f"{what} has {n} tokens, the problem {Tq}")
-        _same_kind(what, t, (*t.shape[:-2], heads, D), dt, dev)
-        setattr(a, what, t.data_ptr())
-        setattr(a, what + "_stride_tok", st)
-        setattr(a, what + "_stride_head", sh)
+    c, Tq, dtype, index = problem.c, problem.Tq, torch.bfloat16, k.get_device()
+    Hkv, D = c.num_kv_heads, c.head_dim
+    Hq = Hkv * c.group_size
+    _check_pools(k_pages, v_pages, c, dtype, index)
+
+    def rows(what, t, heads):
+        n, h, d, st, sh = _token_strides(what, t)
+        if n < Tq or h != heads or d != D:
+            raise ValueError(f"{what} must be [Tq, {heads}, {D}] with Tq >= {Tq}, is {list(t.shape)}")
+        if t.dtype is not dtype:
+            raise TypeError(f"{what} must be {dtype}, is {t.dtype}")
+        if t.get_device() != index:
+            raise ValueError(f"{what} is on {t.device}, not on GPU {index}")
+        return t.data_ptr(), st, sh
+
+    kp, kt, kh = rows("k", k, Hkv)
+    vp, vt, vh = rows("v", v, Hkv)
+    qp = qt = qh = op = sp = 0
     if q is not None:
+        qp, qt, qh = rows("q", q, Hq)
         if q_out is None:
-            q_out = _empty(stream, (Tq, Hq, D), dt, dev)
-        if q_out.numel() < Tq * Hq * D or not q_out.is_contiguous() or q_out.shape[-2:] != (Hq, D) or q_out.dtype != dt \
-                or q_out.device != dev:
+            q_out = _empty(stream, (Tq, Hq, D), dtype, k.device)
+        n, h, d, _, _ = _token_strides("q_out", q_out)
+        if n < Tq or h != Hq or d != D or q_out.dtype is not dtype or q_out.get_device() != index or not q_out.is_contiguous():
             raise ValueError("q_out must be a contiguous bf16 [Tq, Hq, d] on the tensors' device")
-        a.q_out = q_out.data_ptr()
+        op = q_out.data_ptr()
     if starts is not None:
         if len(starts) != c.batch:
             raise ValueError("starts must have an entry per request")
-        a.starts = (ctypes.c_int32 * c.batch).from_buffer(array.array("i", starts))
-
-    def call():
-        plan = problem.append_plan()
-        _check(load().cas_paged_append_run(plan.handle, None if rope is None else ctypes.byref(rope._on(dev)[0]), ctypes.byref(a),
-                                           k_pages.data_ptr(), v_pages.data_ptr(), _stream_handle(dev, stream)))
-    _on_device(dev, call)
+        starts = array.array("i", starts)
+        sp = starts.buffer_info()[0]
+    _gpu("k", k)
+    packed = _APPEND.pack(kp, vp, kt, kh, vt, vh, qp, qt, qh, op, sp)
+    _on_device(index, stream, lambda handle: load().cas_paged_append_run(
+        problem.append_plan().handle, None if rope is None else rope._on(index)[0], packed, k_pages.data_ptr(),
+        v_pages.data_ptr(), handle))
     return q_out
 
 
@@ -658,34 +699,34 @@ def paged_chunk_fwd(q, k_pages, v_pages, problem: DecodeProblem, o=None, lse=Non
     Requests may have no new token. Returns O (as q; rows behind the last
     request's are neither read nor written) and LSE [Hq, Tq] (fp32)."""
     import torch
-    c = problem.c
-    Tq, Hkv, D, Hq, dev, dt = problem.Tq, c.num_kv_heads, c.head_dim, c.num_kv_heads * c.group_size, q.device, torch.bfloat16
+    c, Tq, dtype, index = problem.c, problem.Tq, torch.bfloat16, q.get_device()
+    Hq, D = c.num_kv_heads * c.group_size, c.head_dim
     if q.dim() != 3 or q.shape[0] < Tq:
         raise ValueError(f"q must be [Tq, Hq, d] with Tq >= {Tq}")
-    _same_kind("q", q, (q.shape[0], Hq, D), dt, dev)
-    for what, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-        _same_kind(what, t, (c.num_pages, c.page_size, Hkv, D), dt, dev)
+    shape = (q.shape[0], Hq, D)
+    _same_kind("q", q, shape, dtype, index)
+    _check_pools(k_pages, v_pages, c, dtype, index)
     if o is None:
-        o = _empty(stream, q.shape, dt, dev)
-    if lse is None and need_lse:
-        lse = _empty(stream, (Hq, Tq), torch.float32, dev)
-    _same_kind("o", o, q.shape, dt, dev)
+        o = _empty(stream, shape, dtype, q.device)
+    else:
+        _same_kind("o", o, shape, dtype, index)
     if lse is not None:
-        _same_kind("lse", lse, (Hq, Tq), torch.float32, dev)
-    for what, t in (("q", q), ("k_pages", k_pages), ("v_pages", v_pages), ("o", o), ("lse", lse)):
-        if t is not None and not t.is_contiguous():
-            raise ValueError(f"{what} must be contiguous")
+        _same_kind("lse", lse, (Hq, Tq), torch.float32, index)
+    elif need_lse:
+        lse = _empty(stream, (Hq, Tq), torch.float32, q.device)
+    if not (q.is_contiguous() and o.is_contiguous() and (lse is None or lse.is_contiguous())):
+        raise ValueError("q, o and lse must be contiguous")
+    _gpu("q", q)
 
-    def call():
-        plan = problem.chunk_plan()
-        ws = workspace
-        if ws is None or ws.numel() * ws.element_size() < plan.ws_bytes:
-            ws = _empty(stream, (max(plan.ws_bytes, 1),), torch.uint8, dev)
-        elif ws.device != dev or not ws.is_contiguous():
+    def call(handle):
+        plan, ws = problem.chunk_plan(), workspace
+        if ws is not None and (ws.get_device() != index or not ws.is_contiguous()):
             raise ValueError("workspace must be contiguous and on the tensors' device")
-        _check(load().cas_paged_chunk_run(plan.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), o.data_ptr(),
-                                          _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _stream_handle(dev, stream)))
-    _on_device(dev, call)
+        if ws is None or ws.nbytes < plan.ws_bytes:
+            ws = _empty(stream, (max(plan.ws_bytes, 1),), torch.uint8, q.device)
+        return load().cas_paged_chunk_run(plan.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), o.data_ptr(),
+                                          0 if lse is None else lse.data_ptr(), ws.data_ptr(), ws.nbytes, handle)
+    _on_device(index, stream, call)
     return o, lse
 
 

@@ -183,10 +183,11 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cas_paged_decode_plan_matches.restype = i32
     f64 = ctypes.c_double
     lib.cas_rope_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, P(f64)]
-    lib.cas_rope.argtypes = [P(Rope), ctypes.c_int, i32, ctypes.c_int64, vp, P(RopeTensor), i32, i32, vp]
-    lib.cas_paged_append.argtypes = [P(DecodeProblem), P(Rope), P(Append), vp, vp, vp]
+    # (The binding packs cas_rope_tensor_t and cas_append_t into bytes, whose address vp passes.)
+    lib.cas_rope.argtypes = [P(Rope), ctypes.c_int, i32, ctypes.c_int64, vp, vp, i32, i32, vp]
+    lib.cas_paged_append.argtypes = [P(DecodeProblem), P(Rope), vp, vp, vp, vp]
     lib.cas_paged_append_plan_create.argtypes = [P(DecodeProblem), P(vp)]
-    lib.cas_paged_append_run.argtypes = [vp, P(Rope), P(Append), vp, vp, vp]
+    lib.cas_paged_append_run.argtypes = [vp, P(Rope), vp, vp, vp, vp]
     lib.cas_paged_append_plan_matches.argtypes = [vp, P(DecodeProblem)]
     lib.cas_paged_append_plan_matches.restype = i32
     lib.cas_paged_append_plan_destroy.argtypes = [vp]

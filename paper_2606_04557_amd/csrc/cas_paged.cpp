@@ -95,8 +95,7 @@ constexpr int64_t kMaxRopeTokens = (int64_t)1 << 26;
 cas_status_t check_strides(const char *what, int64_t st, int64_t sh, int es) {
   if (st < 0 || sh < 0 || st > kMaxStride || sh > kMaxStride)
     return set_error(CAS_ERR_INVALID_ARGUMENT, std::string(what) + ": strides must be in [0, 2^31]");
-  if ((st * es) % 16 || (sh * es) % 16)
-    return set_error(CAS_ERR_ALIGNMENT, std::string(what) + ": strides must be multiples of 16 bytes");
+  if (((st | sh) * es) % 16) return set_error(CAS_ERR_ALIGNMENT, std::string(what) + ": strides must be multiples of 16 bytes");
   return CAS_OK;
 }
 
@@ -124,19 +123,19 @@ cas_status_t rope_call(const cas_rope_t *rope, cas_dtype_t dtype, int32_t D, int
   if ((uintptr_t)positions & 3u) return set_error(CAS_ERR_ALIGNMENT, "positions must be 4-byte aligned");
   const int es = dtype == CAS_DTYPE_BF16 ? 2 : 4;
   RopeParams p{};
-  std::vector<Footprint> in, out;
+  Footprint in[4], out[4];
   int heads = 1;
   for (int i = 0; i < n; ++i) {
     const cas_rope_tensor_t &t = ts[i];
-    const std::string name = "tensor " + str(i);
-    if (!t.x || !t.y) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": x and y must be non-NULL");
-    if (t.heads < 1 || t.heads > (1 << 16)) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": heads must be in [1, 2^16]");
-    if (!aligned16(t.x) || !aligned16(t.y)) return set_error(CAS_ERR_ALIGNMENT, name + ": x and y must be 16-byte aligned");
-    if ((s = check_strides((name + " x").c_str(), t.x_stride_tok, t.x_stride_head, es)) != CAS_OK) return s;
-    if ((s = check_strides((name + " y").c_str(), t.y_stride_tok, t.y_stride_head, es)) != CAS_OK) return s;
-    in.push_back(footprint(t.x, tokens, t.heads, t.x_stride_tok, t.x_stride_head, D, es));
-    out.push_back(footprint(t.y, tokens, t.heads, t.y_stride_tok, t.y_stride_head, D, es));
-    if (!out.back().distinct) return set_error(CAS_ERR_INVALID_ARGUMENT, name + ": y overlaps itself");
+    auto refuse = [&](cas_status_t code, const char *why) { return set_error(code, "tensor " + str(i) + ": " + why); };
+    if (!t.x || !t.y) return refuse(CAS_ERR_INVALID_ARGUMENT, "x and y must be non-NULL");
+    if (t.heads < 1 || t.heads > (1 << 16)) return refuse(CAS_ERR_INVALID_ARGUMENT, "heads must be in [1, 2^16]");
+    if (!aligned16(t.x) || !aligned16(t.y)) return refuse(CAS_ERR_ALIGNMENT, "x and y must be 16-byte aligned");
+    if ((s = check_strides("x", t.x_stride_tok, t.x_stride_head, es)) != CAS_OK) return s;
+    if ((s = check_strides("y", t.y_stride_tok, t.y_stride_head, es)) != CAS_OK) return s;
+    in[i] = footprint(t.x, tokens, t.heads, t.x_stride_tok, t.x_stride_head, D, es);
+    out[i] = footprint(t.y, tokens, t.heads, t.y_stride_tok, t.y_stride_head, D, es);
+    if (!out[i].distinct) return refuse(CAS_ERR_INVALID_ARGUMENT, "y overlaps itself");
     p.t[i] = DevRopeTensor{t.x, t.y, t.x_stride_tok, t.x_stride_head, t.y_stride_tok, t.y_stride_head, t.heads, 0};
     heads = std::max(heads, t.heads);
   }
@@ -144,13 +143,15 @@ cas_status_t rope_call(const cas_rope_t *rope, cas_dtype_t dtype, int32_t D, int
   const Footprint turns{(uintptr_t)rope->turns, (uintptr_t)rope->turns + (uintptr_t)rope->rotary_dim * 4, 0,
                         (uint64_t)rope->rotary_dim * 4, true};
   for (int i = 0; i < n; ++i) {
-    const std::string name = "tensor " + str(i) + ": y overlaps ";
-    if (!apart(out[i], pos) || !apart(out[i], turns)) return set_error(CAS_ERR_INVALID_ARGUMENT, name + "positions or turns");
+    auto refuse = [&](const std::string &what) {
+      return set_error(CAS_ERR_INVALID_ARGUMENT, "tensor " + str(i) + ": y overlaps " + what);
+    };
+    if (!apart(out[i], pos) || !apart(out[i], turns)) return refuse("positions or turns");
     for (int j = 0; j < n; ++j) {
       const bool in_place = i == j && ts[i].x == ts[i].y && (tokens == 1 || ts[i].x_stride_tok == ts[i].y_stride_tok) &&
                             (ts[i].heads == 1 || ts[i].x_stride_head == ts[i].y_stride_head);
-      if (!in_place && !apart(out[i], in[j])) return set_error(CAS_ERR_INVALID_ARGUMENT, name + "the x of tensor " + str(j));
-      if (i != j && !apart(out[i], out[j])) return set_error(CAS_ERR_INVALID_ARGUMENT, name + "the y of tensor " + str(j));
+      if (!in_place && !apart(out[i], in[j])) return refuse("the x of tensor " + str(j));
+      if (i != j && !apart(out[i], out[j])) return refuse("the y of tensor " + str(j));
     }
   }
   p.rope = dev_rope(rope, inverse != 0);
