@@ -294,22 +294,30 @@ struct RopeParams {
   int32_t slots;            // threads' heads of one token at a time, a power of two
 };
 
-// Appending to the paged cache: n consecutive tokens, tok0 of the new ones, go
-// to rows row0 .. row0 + n - 1 of the pool's rows from page `page` on; the first
-// has position pos0. One item per workgroup (of each tensor and head group).
-struct DevAppendItem {
-  int32_t tok0, page, pos0;
-  int16_t row0, n;
+// Appending to the paged cache. A workgroup (of each tensor and head group)
+// takes per_wg consecutive new tokens of one request. What it needs to know
+// travels as kernel arguments (4 KiB in all), in `words`: the requests of the
+// launch, the request of every workgroup (16 bits each, from word map0 on), and the
+// ids of the pages that the tokens go to (from word page0 on).
+struct DevAppendRequest {
+  int32_t unit0;    // its first workgroup
+  int32_t tok0, n;  // its new tokens
+  int32_t row0;     // row of the first one in its first page
+  int32_t entry0;   // that page's index among the launch's page ids
+  int32_t pos0;     // position of the first one
 };
-constexpr int kAppendItems = 224;   // items in one launch's kernel arguments (4 KiB in all)
+constexpr int kAppendWords = 976;
+constexpr int kAppendMaxPerWg = 16;   // tokens of a workgroup: two pages hold them
 struct AppendParams {
   DevRope rope;             // turns null: nothing is rotated
   const void *k, *v, *q;
   void *k_pages, *v_pages, *q_out;
   int64_t k_tok, k_head, v_tok, v_head, q_tok, q_head;
-  int32_t Hkv, g, page_size, slots;
-  DevAppendItem items[kAppendItems];
+  int32_t Hkv, g, page_shift, slots;
+  int32_t map0, page0;
+  uint32_t words[kAppendWords];
 };
+static_assert(sizeof(AppendParams) <= 4096, "kernel arguments");
 
 // Chunk attention over pages. One workgroup: up to 256 packed rows from row0 on
 // (row r of a request is its token r / g, head r % g of the KV head's group) of
@@ -384,6 +392,6 @@ hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_m
 // Copies `bytes` (a multiple of 16) of pinned host memory to device memory and
 // then sets *flag (pinned host memory) to value.
 hipError_t launch_table_flag(void *dst, const void *src, size_t bytes, uint32_t *flag, uint32_t value, hipStream_t s);
-hipError_t launch_append(const AppendParams &p, int D, int n_items, int head_groups, hipStream_t s);
+hipError_t launch_append(const AppendParams &p, int D, int units, int head_groups, hipStream_t s);
 
 }  // namespace cas

@@ -103,15 +103,26 @@ struct RopeUnit {
       }
     }
   }
-  // Heads h0, h0 + step, ... of one token; x and y point at its first head.
+  // Heads h0, h0 + step, ... of one token; x and y point at its first head. Up to
+  // four heads are loaded before the first is stored.
   __device__ __forceinline__ void heads(const T *x, int64_t x_head, T *y, int64_t y_head, int h0, int step, int n) const {
-    for (int h = h0; h < n; h += step) {
-      Eight<T> a, b;
-      a.load(x + h * x_head + oa);
-      b.load(x + h * x_head + ob);
-      turn(a, b);
-      a.store(y + h * y_head + oa);
-      b.store(y + h * y_head + ob);
+    int h = h0;
+    for (; h + 3 * step < n; h += 4 * step) some<4>(x, x_head, y, y_head, h, step);
+    for (; h < n; h += step) some<1>(x, x_head, y, y_head, h, step);
+  }
+  template <int N>
+  __device__ __forceinline__ void some(const T *x, int64_t x_head, T *y, int64_t y_head, int h, int step) const {
+    Eight<T> a[N], b[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      a[i].load(x + (h + i * step) * x_head + oa);
+      b[i].load(x + (h + i * step) * x_head + ob);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      turn(a[i], b[i]);
+      a[i].store(y + (h + i * step) * y_head + oa);
+      b[i].store(y + (h + i * step) * y_head + ob);
     }
   }
 };
@@ -134,25 +145,34 @@ template <int D, bool IL>
 __global__ __launch_bounds__(kRopeThreads) void append_kernel(AppendParams p) {
   constexpr int U = D / 16;
   const int u = threadIdx.x % U, w = threadIdx.x / U;
-  const DevAppendItem it = p.items[blockIdx.x];
-  const int i = w / p.slots;
+  const uint32_t *words = p.words;
+  const int unit = blockIdx.x, per_wg = kRopeThreads / U / p.slots;
+  const int which = words[p.map0 + unit / 2] >> (16 * (unit & 1)) & 0xffff;
+  const uint32_t *rq = words + which * (int)(sizeof(DevAppendRequest) / 4);
+  const DevAppendRequest r{(int)rq[0], (int)rq[1], (int)rq[2], (int)rq[3], (int)rq[4], (int)rq[5]};
+  const int i0 = (unit - r.unit0) * per_wg, i = i0 + w / p.slots;
   const int h0 = blockIdx.y * p.slots + w % p.slots, step = gridDim.y * p.slots;
   const int heads = blockIdx.z == 2 ? p.Hkv * p.g : p.Hkv;
-  if (i >= it.n || h0 >= heads) return;
-  const int64_t tok = (int64_t)it.tok0 + i;
+  if (i >= r.n || h0 >= heads) return;
+  const int64_t tok = (int64_t)r.tok0 + i;
   DevRope rope = p.rope;
   if (blockIdx.z == 1) rope.turns = nullptr;
-  RopeUnit<__bf16, IL> r;
-  r.init(rope, u, it.pos0 + i);
+  RopeUnit<__bf16, IL> turner;
+  turner.init(rope, u, r.pos0 + i);
   if (blockIdx.z == 2) {
-    r.heads((const __bf16 *)p.q + tok * p.q_tok, p.q_head, (__bf16 *)p.q_out + tok * heads * D, D, h0, step, heads);
+    turner.heads((const __bf16 *)p.q + tok * p.q_tok, p.q_head, (__bf16 *)p.q_out + tok * heads * D, D, h0, step, heads);
     return;
   }
-  const int64_t row = ((int64_t)it.page * p.page_size + it.row0 + i) * p.Hkv * D;
+  // The workgroup's first token's page and the one after it, if its last token is in that.
+  const int last = min(i0 + per_wg, r.n) - 1;
+  const int e0 = (r.row0 + i0) >> p.page_shift, e1 = (r.row0 + last) >> p.page_shift, e = (r.row0 + i) >> p.page_shift;
+  const int page_a = words[p.page0 + r.entry0 + e0], page_b = words[p.page0 + r.entry0 + e1];
+  const int64_t row = ((int64_t)(e == e0 ? page_a : page_b) << p.page_shift) + ((r.row0 + i) & ((1 << p.page_shift) - 1));
+  const int64_t at = row * p.Hkv * D;
   if (blockIdx.z == 0)
-    r.heads((const __bf16 *)p.k + tok * p.k_tok, p.k_head, (__bf16 *)p.k_pages + row, D, h0, step, heads);
+    turner.heads((const __bf16 *)p.k + tok * p.k_tok, p.k_head, (__bf16 *)p.k_pages + at, D, h0, step, heads);
   else
-    r.heads((const __bf16 *)p.v + tok * p.v_tok, p.v_head, (__bf16 *)p.v_pages + row, D, h0, step, heads);
+    turner.heads((const __bf16 *)p.v + tok * p.v_tok, p.v_head, (__bf16 *)p.v_pages + at, D, h0, step, heads);
 }
 
 template <typename T, int D>
@@ -182,8 +202,8 @@ hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_gro
   return hipGetLastError();
 }
 
-hipError_t launch_append(const AppendParams &p, int D, int n_items, int head_groups, hipStream_t s) {
-  const dim3 grid((unsigned)n_items, (unsigned)head_groups, p.q ? 3u : 2u);
+hipError_t launch_append(const AppendParams &p, int D, int units, int head_groups, hipStream_t s) {
+  const dim3 grid((unsigned)units, (unsigned)head_groups, p.q ? 3u : 2u);
   if (D == 64) launch_append_t<64>(p, grid, s);
   else launch_append_t<128>(p, grid, s);
   return hipGetLastError();
