@@ -524,22 +524,24 @@ int32_t cas_paged_chunk_plan_matches(const cas_chunk_plan_t *plan, const cas_dec
 cas_status_t cas_paged_chunk_plan_destroy(cas_chunk_plan_t *plan);
 
 /*
- * A plan's launch tables (host only; for tests and profiling tools). items may
- * be NULL; otherwise it receives 9 values per workgroup in dispatch order: first
- * token and token count of the request, its key count, its first entry of
- * page_ids, the block's first row (tokens x group heads), KV head, first and one
- * past the last 64-key tile, and the partial that it writes (-1: the result).
+ * A plan's launch tables (host only; for tests and profiling tools). items and
+ * wg_items may be NULL; otherwise items receives 9 values per item: first token
+ * and token count of the request, its key count, its first entry of page_ids, the
+ * block's first row (tokens x group heads), KV head, first and one past the last
+ * 64-key tile, and the partial that it writes (-1: the result); and wg_items the
+ * first item of every workgroup, in dispatch order, and the end (workgroups + 1).
  */
 typedef struct {
   int32_t workgroups;
+  int32_t items;
   int32_t partials;
   int32_t max_partials;   /* most of one block of rows (1: no merge) */
-  int32_t reserved;
   int64_t key_tiles;      /* 64-key tiles walked by all workgroups */
   size_t ws_bytes;
 } cas_chunk_plan_info_t;
 
-cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items);
+cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items,
+                                       int32_t *wg_items);
 
 /*
  * Budget manager (paper: paragraphs "Budget Manager" and "Pool rotation";

@@ -9,7 +9,9 @@
 // take turns, one in a matrix phase (O += V^T P of the tile before, S = K Q^T of
 // this one) while the other is in its softmax phase (cas_bf16.hip has the
 // schedule). Here the tiles are gathered page by page, and the second pass for
-// rows that the fixed softmax reference does not fit is a plain loop.
+// rows that the fixed softmax reference does not fit is a plain loop. A workgroup
+// works through a list of items (blocks of rows, or pieces of their keys), which
+// the host makes equally long for all compute units.
 //
 // This file is compiled to honour NaN: that second pass also keeps values which
 // are not finite from the rows that do not see their keys.
@@ -59,7 +61,7 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 v) {
 
 template <int D>
 __global__ __launch_bounds__(kFastThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void chunk_bf16_kernel(ChunkParams p) {
+void chunk_bf16_kernel(ChunkParams p0) {
   constexpr int NSTEP = D / 16, DT = D / 32;
   constexpr int TB = kKT * D * 2;
   constexpr int CPR = D / 8, RPI = 64 / CPR;   // 16-byte chunks of a key row, key rows of a copy instruction
@@ -71,257 +73,274 @@ void chunk_bf16_kernel(ChunkParams p) {
   __shared__ __attribute__((aligned(1024))) char vb1[TB];
   __shared__ __attribute__((aligned(1024))) char vb2[TB];
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int grp = wave >> 2, w4 = wave & 3;
-  const int G = lane >> 5, n = lane & 31;
-  const DevChunkItem it = load_const(p.items, (int)blockIdx.x);
-  const int g = p.g, Hkv = p.Hkv, Hq = Hkv * g;
-  const int nrows = it.len * g;
-  const int row0 = it.row0 + wave * kFastRowsPerWave, my_row = row0 + n;
-  const bool wave_active = row0 < nrows;
-  const int before = it.kv_len - it.len;       // token t sees keys 0 .. before + t
-  const int last_lo = __builtin_amdgcn_readfirstlane(before + row0 / g);
-  const int last_hi = __builtin_amdgcn_readfirstlane(before + (min(row0 + kFastRowsPerWave, nrows) - 1) / g);
-  const int my_t = my_row / g;
-  const int nt = it.tile1 - it.tile0;
-  const float c = p.scale_log2;
-
-  RowOffsets<D> ro;
-  ro.init(n, G);
-  TrOffsets<D> to;
-  to.init(lane);
-  // Copies. Instruction i of wave w4 moves key rows r0 .. r0 + RPI - 1 of a tile,
-  // r0 = RPI (w4 + 4 i), which lie in one page (pages are multiples of 16 rows).
-  // It has a resource of its own, which ends behind the request's last key: later
-  // rows read as zero, and are masked. Rows 16 apart share their swizzle, so one
-  // lane offset serves every instruction.
-  static_assert(4 * RPI % 16 == 0, "the swizzle of a wave's rows is the same for every instruction");
-  const int page_shift = __builtin_ctz(p.page_size), row_elems = Hkv * D;
-  const int lane_off = (lane / CPR) * row_elems * 2 + (((lane % CPR) ^ swz<D>(w4 * RPI + lane / CPR)) << 4);
-  struct Tile {
-    int key0;        // first key of the wave's first instruction
-    int page[PER];
-  };
-  auto tile_at = [&](int j) __attribute__((always_inline)) {
-    Tile t;
-    t.key0 = (it.tile0 + j) * kKT + w4 * RPI;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      t.page[i] = load_const(p.page_ids, it.page0 + (min(t.key0 + 4 * RPI * i, it.kv_len - 1) >> page_shift));
-    return t;
-  };
-  auto copy = [&](char *buf, const void *pool, const Tile &t, bool has, int i) __attribute__((always_inline)) {
-    const int key = t.key0 + 4 * RPI * i;
-    const int64_t row = ((int64_t)t.page[i] << page_shift) + (key & ((1 << page_shift) - 1));
-    const int valid = has ? min(RPI, it.kv_len - key) : 0;
-    dma16(make_rsrc((const __bf16 *)pool + row * row_elems + it.kvh * D, valid > 0 ? ((valid - 1) * row_elems + D) * 2 : 0),
-          lane_off, buf + (w4 + 4 * i) * 1024);
-  };
-  // The first K tile is on its way while the queries are.
-  Tile tk;   // of the K copied last, whose V is copied next
-  if (grp == 1) {
-    tk = tile_at(0);
-#pragma unroll
-    for (int i = 0; i < PER; ++i) copy(kb0, p.k_pages, tk, true, i);
-  }
-  bf16x8 qf[NSTEP];
-  if (my_row < nrows) {
-    const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + it.kvh * g + (my_row - my_t * g)) * D;
-#pragma unroll
-    for (int st = 0; st < NSTEP; ++st) qf[st] = *reinterpret_cast<const bf16x8 *>(rp + st * 16 + G * 8);
-  } else {
-#pragma unroll
-    for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
-  }
-  // Tile copies are waited for with partial vmcnt counts, which must not
-  // include these loads (and phase 0 reads the first K).
-  wait_vmcnt<0>();
-
-  f32x16 oacc[DT];
-  float m_run = -INFINITY, l_run = 0.0f;   // exponent offset of this lane's row, row sum of its keys
-  auto live = [&](int j) __attribute__((always_inline)) { return wave_active && (it.tile0 + j) * kKT <= last_hi; };
-  constexpr int kPieces = 2 * PER;         // copy instructions of a softmax phase
-  static_assert(16 % kPieces == 0, "copies spread over the 16 exponential pairs");
-
-  {
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
-    f32x16 s0 = zero16(), s1 = zero16();
-    bf16x8 pf[2][2];
-    auto no_weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) pf[a][s] = Mma<__bf16>::zero();
-    };
-    no_weights();
-    auto softmax = [&](auto MASK, int lim, auto &&piece) __attribute__((always_inline)) {
-      if constexpr (decltype(MASK)::value) fwd_mask(lim, G, s0, s1);
-      // Only until every row of the wave has seen a key.
-      if (wave_any(m_run == -INFINITY)) {
-        const float mt = fwd_tile_max(s0, s1, c);
-        m_run = (m_run == -INFINITY) ? mt : m_run;
-      }
-      const float mu = (m_run == -INFINITY) ? 0.0f : m_run;
-      l_run += fwd_weights<kPieces>(c, mu, s0, s1, pf, piece);
-    };
-    auto gphase = [&](int j, const char *kb, const char *vbp) __attribute__((always_inline)) {
-      if (j <= nt && wave_active) fwd_matrix_phase<D>(kb, vbp, ro, to, qf, pf, s0, s1, oacc);
-    };
-    auto xphase = [&](int j, auto &&piece) __attribute__((always_inline)) {
-      auto all_pieces = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int n = 0; n < kPieces; ++n) piece(n);
-      };
-      if (j < 0 || j >= nt) {
-        all_pieces();
-        return;
-      }
-      if (!live(j)) {
-        no_weights();
-        all_pieces();
-        return;
-      }
-      const int key0 = (it.tile0 + j) * kKT;
-      if (key0 + kKT - 1 > last_lo) softmax(std::true_type{}, before + my_t - key0, piece);
-      else softmax(std::false_type{}, kKT - 1, piece);
-    };
-    auto no_piece = [](int) {};
-    auto even_b = [&](int i, char *kbn, char *vbn) __attribute__((always_inline)) {
-      const Tile tv = tk;
-      const Tile tn = tile_at(min(i + 2, nt - 1));
-      const bool has_v = i + 1 < nt, has_k = i + 2 < nt;
-      xphase(i - 1, [&](int n) __attribute__((always_inline)) {
-        if (n < PER) copy(vbn, p.v_pages, tv, has_v, n);
-        else copy(kbn, p.k_pages, tn, has_k, n - PER);
-      });
-      tk = tn;
-      wait_vmcnt<2 * PER>();
-    };
-
-    // (At least one tile: the host lists no empty range.) G_0 multiplies V
-    // buffer 2 by P = 0: clear it so no stale bit pattern (a NaN) can reach O.
-    for (int i = tid; i < TB / 16; i += kFastThreads) reinterpret_cast<uint4 *>(vb2)[i] = uint4{0, 0, 0, 0};
-    if (grp == 1) {
-      const Tile t1 = tile_at(min(1, nt - 1));
-#pragma unroll
-      for (int i = 0; i < PER; ++i) copy(vb0, p.v_pages, tk, true, i);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) copy(kb1, p.k_pages, t1, nt > 1, i);
-      tk = t1;
-    }
-    lds_barrier();
-    // Six phases per iteration (three tiles), so every buffer is a fixed LDS
-    // address: G_i reads K_i from kb[i%3] and V_{i-1} from vb[(i-1)%3]; the
-    // copies of phase 2i go to kb[(i+2)%3] and vb[(i+1)%3].
-    auto run = [&](auto GROUP_A) __attribute__((always_inline)) {
-      constexpr bool A = decltype(GROUP_A)::value;
-      auto even = [&](int i, const char *kbi, const char *vbp, char *kbn, char *vbn) __attribute__((always_inline)) {
-        if constexpr (A) gphase(i, kbi, vbp);
-        else even_b(i, kbn, vbn);
-        lds_barrier();
-      };
-      auto odd = [&](int i, const char *kbi, const char *vbp) __attribute__((always_inline)) {
-        if constexpr (A) xphase(i, no_piece);
-        else gphase(i, kbi, vbp);
-        lds_barrier();
-      };
-      for (int i = 0; i <= nt; i += 3) {
-        even(i, kb0, vb2, kb2, vb1);
-        odd(i, kb0, vb2);
-        if (i + 1 > nt) break;
-        even(i + 1, kb1, vb0, kb0, vb2);
-        odd(i + 1, kb1, vb0);
-        if (i + 2 > nt) break;
-        even(i + 2, kb2, vb1, kb1, vb0);
-        odd(i + 2, kb2, vb1);
-      }
-    };
-    if (grp == 0) run(std::true_type{});
-    else run(std::false_type{});
-    wait_vmcnt<0>();
-  }
-
-  // Every wave reaches this point. A row sum that reached 2^kRefMargin or
-  // overflowed needs the exact online softmax, an O that is not finite may come
-  // from a key that its row does not see: the workgroup takes its tiles again,
-  // one after the other.
-  bool again = ((__float_as_uint(l_run) >> 23) & 0xffu) >= 127u + (unsigned)kRefMargin;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) again |= (__float_as_uint(oacc[dt][i]) & 0x7f800000u) == 0x7f800000u;
-  if (__syncthreads_or(again ? 1 : 0)) {
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
-    m_run = -INFINITY;
-    l_run = 0.0f;
+  const int end = load_const(p0.wg_items, (int)blockIdx.x + 1);
 #pragma unroll 1
-    for (int j = 0; j < nt; ++j) {
-      lds_barrier();   // every wave is done with the tile before
-      if (grp == 1) {
-        const Tile t = tile_at(j);
+  for (int at = load_const(p0.wg_items, (int)blockIdx.x); at < end; ++at) {
+    // Per item, the lane index and the parameters are read anew: values kept
+    // across items would be held in registers through the tile loop.
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const ChunkParams p = load_kernarg<ChunkParams>();
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int grp = wave >> 2, w4 = wave & 3;
+    const int G = lane >> 5, n = lane & 31;
+    const int g = p.g, Hkv = p.Hkv, Hq = Hkv * g;
+    const float c = p.scale_log2;
+    RowOffsets<D> ro;
+    ro.init(n, G);
+    TrOffsets<D> to;
+    to.init(lane);
+    const int page_shift = __builtin_ctz(p.page_size), row_elems = Hkv * D;
+    const int lane_off = (lane / CPR) * row_elems * 2 + (((lane % CPR) ^ swz<D>(w4 * RPI + lane / CPR)) << 4);
+    const DevChunkItem it = load_const(p.items, __builtin_amdgcn_readfirstlane(at));
+    const int nrows = it.len * g;
+    const int row0 = it.row0 + wave * kFastRowsPerWave, my_row = row0 + n;
+    const bool wave_active = row0 < nrows;
+    const int before = it.kv_len - it.len;       // token t sees keys 0 .. before + t
+    const int last_lo = __builtin_amdgcn_readfirstlane(before + row0 / g);
+    const int last_hi = __builtin_amdgcn_readfirstlane(before + (min(row0 + kFastRowsPerWave, nrows) - 1) / g);
+    const int my_t = my_row / g;
+    const int nt = it.tile1 - it.tile0;
+
+    // Copies. Instruction i of wave w4 moves key rows r0 .. r0 + RPI - 1 of a tile,
+    // r0 = RPI (w4 + 4 i), which lie in one page (pages are multiples of 16 rows).
+    // It has a resource of its own, which ends behind the request's last key: later
+    // rows read as zero, and are masked. Rows 16 apart share their swizzle, so one
+    // lane offset serves every instruction.
+    static_assert(4 * RPI % 16 == 0, "the swizzle of a wave's rows is the same for every instruction");
+    struct Tile {
+      int key0;        // first key of the wave's first instruction
+      int page[PER];
+    };
+    auto tile_at = [&](int j) __attribute__((always_inline)) {
+      Tile t;
+      t.key0 = (it.tile0 + j) * kKT + w4 * RPI;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          copy(kb0, p.k_pages, t, true, i);
-          copy(vb0, p.v_pages, t, true, i);
+      for (int i = 0; i < PER; ++i)
+        t.page[i] = load_const(p.page_ids, it.page0 + (min(t.key0 + 4 * RPI * i, it.kv_len - 1) >> page_shift));
+      return t;
+    };
+    auto copy = [&](char *buf, const void *pool, const Tile &t, bool has, int i) __attribute__((always_inline)) {
+      const int key = t.key0 + 4 * RPI * i;
+      const int64_t row = ((int64_t)t.page[i] << page_shift) + (key & ((1 << page_shift) - 1));
+      const int valid = has ? min(RPI, it.kv_len - key) : 0;
+      dma16(make_rsrc((const __bf16 *)pool + row * row_elems + it.kvh * D, valid > 0 ? ((valid - 1) * row_elems + D) * 2 : 0),
+            lane_off, buf + (w4 + 4 * i) * 1024);
+    };
+    // The first K tile is on its way while the queries are.
+    Tile tk;   // of the K copied last, whose V is copied next
+    if (grp == 1) {
+      tk = tile_at(0);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) copy(kb0, p.k_pages, tk, true, i);
+    }
+    bf16x8 qf[NSTEP];
+    if (my_row < nrows) {
+      const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + it.kvh * g + (my_row - my_t * g)) * D;
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) qf[st] = *reinterpret_cast<const bf16x8 *>(rp + st * 16 + G * 8);
+    } else {
+#pragma unroll
+      for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
+    }
+    // Tile copies are waited for with partial vmcnt counts, which must not
+    // include these loads (and phase 0 reads the first K).
+    wait_vmcnt<0>();
+
+    f32x16 oacc[DT];
+    float m_run = -INFINITY, l_run = 0.0f;   // exponent offset of this lane's row, row sum of its keys
+    auto live = [&](int j) __attribute__((always_inline)) { return wave_active && (it.tile0 + j) * kKT <= last_hi; };
+    constexpr int kPieces = 2 * PER;         // copy instructions of a softmax phase
+    static_assert(16 % kPieces == 0, "copies spread over the 16 exponential pairs");
+
+    {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+      f32x16 s0 = zero16(), s1 = zero16();
+      bf16x8 pf[2][2];
+      auto no_weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) pf[a][s] = Mma<__bf16>::zero();
+      };
+      no_weights();
+      auto softmax = [&](auto MASK, int lim, auto &&piece) __attribute__((always_inline)) {
+        if constexpr (decltype(MASK)::value) fwd_mask(lim, G, s0, s1);
+        // Only until every row of the wave has seen a key.
+        if (wave_any(m_run == -INFINITY)) {
+          const float mt = fwd_tile_max(s0, s1, c);
+          m_run = (m_run == -INFINITY) ? mt : m_run;
         }
-        wait_vmcnt<0>();
+        const float mu = (m_run == -INFINITY) ? 0.0f : m_run;
+        l_run += fwd_weights<kPieces>(c, mu, s0, s1, pf, piece);
+      };
+      auto gphase = [&](int j, const char *kb, const char *vbp) __attribute__((always_inline)) {
+        if (j <= nt && wave_active) fwd_matrix_phase<D>(kb, vbp, ro, to, qf, pf, s0, s1, oacc);
+      };
+      auto xphase = [&](int j, auto &&piece) __attribute__((always_inline)) {
+        auto all_pieces = [&]() __attribute__((always_inline)) {
+#pragma unroll
+          for (int n = 0; n < kPieces; ++n) piece(n);
+        };
+        if (j < 0 || j >= nt) {
+          all_pieces();
+          return;
+        }
+        if (!live(j)) {
+          no_weights();
+          all_pieces();
+          return;
+        }
+        const int key0 = (it.tile0 + j) * kKT;
+        if (key0 + kKT - 1 > last_lo) softmax(std::true_type{}, before + my_t - key0, piece);
+        else softmax(std::false_type{}, kKT - 1, piece);
+      };
+      auto no_piece = [](int) {};
+      auto even_b = [&](int i, char *kbn, char *vbn) __attribute__((always_inline)) {
+        const Tile tv = tk;
+        const Tile tn = tile_at(min(i + 2, nt - 1));
+        const bool has_v = i + 1 < nt, has_k = i + 2 < nt;
+        xphase(i - 1, [&](int n) __attribute__((always_inline)) {
+          if (n < PER) copy(vbn, p.v_pages, tv, has_v, n);
+          else copy(kbn, p.k_pages, tn, has_k, n - PER);
+        });
+        tk = tn;
+        wait_vmcnt<2 * PER>();
+      };
+
+      // (At least one tile: the host lists no empty range.) G_0 multiplies V
+      // buffer 2 by P = 0: clear it so no stale bit pattern (a NaN) can reach O.
+      for (int i = tid; i < TB / 16; i += kFastThreads) reinterpret_cast<uint4 *>(vb2)[i] = uint4{0, 0, 0, 0};
+      if (grp == 1) {
+        const Tile t1 = tile_at(min(1, nt - 1));
+#pragma unroll
+        for (int i = 0; i < PER; ++i) copy(vb0, p.v_pages, tk, true, i);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) copy(kb1, p.k_pages, t1, nt > 1, i);
+        tk = t1;
       }
       lds_barrier();
-      if (!live(j)) continue;
-      const int key0 = (it.tile0 + j) * kKT, lim = before + my_t - key0;
-      const bool part = key0 + kKT - 1 > last_lo;   // some row sees the tile in part
-      f32x16 s0 = zero16(), s1 = zero16();
-#pragma unroll
-      for (int st = 0; st < NSTEP; ++st) {
-        s0 = Mma<__bf16>::run(row_frag_at<D>(kb0, ro, 0, st), qf[st], s0);
-        s1 = Mma<__bf16>::run(row_frag_at<D>(kb0, ro, 32, st), qf[st], s1);
-      }
-      if (part) fwd_mask(lim, G, s0, s1);
-      const float m_new = fmaxf(m_run, fwd_tile_max(s0, s1, c));
-      const float mu = m_new == -INFINITY ? 0.0f : m_new;
-      const float alpha = fast_exp2(m_run - mu);
-      m_run = m_new;
-      bf16x8 pf[2][2];
-      l_run = l_run * alpha + fwd_weights<1>(c, mu, s0, s1, pf, [](int) {});
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
-      const bool odd = part && has_odd<D>(vb0, lane);
-      if (odd) add_odd<D>(vb0, lim, G, oacc);
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            bf16x8 vf = tr_frag_at<D>(vb0, to, 32 * a + 16 * h, dt);
-            if (odd) vf = finite_only(vf);
-            oacc[dt] = Mma<__bf16>::run(vf, pf[a][h], oacc[dt]);
-          }
+      // Six phases per iteration (three tiles), so every buffer is a fixed LDS
+      // address: G_i reads K_i from kb[i%3] and V_{i-1} from vb[(i-1)%3]; the
+      // copies of phase 2i go to kb[(i+2)%3] and vb[(i+1)%3].
+      auto run = [&](auto GROUP_A) __attribute__((always_inline)) {
+        constexpr bool A = decltype(GROUP_A)::value;
+        auto even = [&](int i, const char *kbi, const char *vbp, char *kbn, char *vbn) __attribute__((always_inline)) {
+          if constexpr (A) gphase(i, kbi, vbp);
+          else even_b(i, kbn, vbn);
+          lds_barrier();
+        };
+        auto odd = [&](int i, const char *kbi, const char *vbp) __attribute__((always_inline)) {
+          if constexpr (A) xphase(i, no_piece);
+          else gphase(i, kbi, vbp);
+          lds_barrier();
+        };
+        for (int i = 0; i <= nt; i += 3) {
+          even(i, kb0, vb2, kb2, vb1);
+          odd(i, kb0, vb2);
+          if (i + 1 > nt) break;
+          even(i + 1, kb1, vb0, kb0, vb2);
+          odd(i + 1, kb1, vb0);
+          if (i + 2 > nt) break;
+          even(i + 2, kb2, vb1, kb1, vb0);
+          odd(i + 2, kb2, vb1);
+        }
+      };
+      if (grp == 0) run(std::true_type{});
+      else run(std::false_type{});
+      wait_vmcnt<0>();
     }
-  }
 
-  const float lt = l_run + xor32(l_run);
-  if (my_row >= nrows) return;
-  const int h = it.kvh * g + (my_row - my_t * g);
-  // (A piece of a split may hold no key that the row sees. A NaN sum stays NaN.)
-  const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-  const float lse = lt == 0.0f ? -INFINITY : (m_run + log2f(lt)) * kLn2;
-  auto store = [&](auto *op) __attribute__((always_inline)) {
+    // Every wave reaches this point. A row sum that reached 2^kRefMargin or
+    // overflowed needs the exact online softmax, an O that is not finite may come
+    // from a key that its row does not see: the workgroup takes its tiles again,
+    // one after the other.
+    bool again = ((__float_as_uint(l_run) >> 23) & 0xffu) >= 127u + (unsigned)kRefMargin;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int j = 0; j < 16; j += 4)
-        store4(op + dt * 32 + crow(j, G), oacc[dt][j] * inv, oacc[dt][j + 1] * inv, oacc[dt][j + 2] * inv, oacc[dt][j + 3] * inv);
-  };
-  if (it.part < 0) {
-    store((__bf16 *)p.o + (((int64_t)it.tok0 + my_t) * Hq + h) * D);
-    if (G == 0 && p.lse != nullptr) p.lse[(int64_t)h * p.Tq + it.tok0 + my_t] = lse;
-  } else {
-    const int64_t R = (int64_t)it.part * kFastRowsPerWg + (my_row - it.row0);
-    store(p.part_o + R * D);
-    if (G == 0) p.part_lse[R] = lse;
+      for (int i = 0; i < 16; ++i) again |= (__float_as_uint(oacc[dt][i]) & 0x7f800000u) == 0x7f800000u;
+    if (__syncthreads_or(again ? 1 : 0)) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+      m_run = -INFINITY;
+      l_run = 0.0f;
+#pragma unroll 1
+      for (int j = 0; j < nt; ++j) {
+        lds_barrier();   // every wave is done with the tile before
+        if (grp == 1) {
+          const Tile t = tile_at(j);
+#pragma unroll
+          for (int i = 0; i < PER; ++i) {
+            copy(kb0, p.k_pages, t, true, i);
+            copy(vb0, p.v_pages, t, true, i);
+          }
+          wait_vmcnt<0>();
+        }
+        lds_barrier();
+        if (!live(j)) continue;
+        const int key0 = (it.tile0 + j) * kKT, lim = before + my_t - key0;
+        const bool part = key0 + kKT - 1 > last_lo;   // some row sees the tile in part
+        f32x16 s0 = zero16(), s1 = zero16();
+#pragma unroll
+        for (int st = 0; st < NSTEP; ++st) {
+          s0 = Mma<__bf16>::run(row_frag_at<D>(kb0, ro, 0, st), qf[st], s0);
+          s1 = Mma<__bf16>::run(row_frag_at<D>(kb0, ro, 32, st), qf[st], s1);
+        }
+        if (part) fwd_mask(lim, G, s0, s1);
+        const float m_new = fmaxf(m_run, fwd_tile_max(s0, s1, c));
+        const float mu = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = fast_exp2(m_run - mu);
+        m_run = m_new;
+        bf16x8 pf[2][2];
+        l_run = l_run * alpha + fwd_weights<1>(c, mu, s0, s1, pf, [](int) {});
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
+        const bool odd = part && has_odd<D>(vb0, lane);
+        if (odd) add_odd<D>(vb0, lim, G, oacc);
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+              bf16x8 vf = tr_frag_at<D>(vb0, to, 32 * a + 16 * h, dt);
+              if (odd) vf = finite_only(vf);
+              oacc[dt] = Mma<__bf16>::run(vf, pf[a][h], oacc[dt]);
+            }
+      }
+      lds_barrier();   // (the next item's copies go to the same tiles)
+    }
+
+    const float lt = l_run + xor32(l_run);
+    const float m_out = m_run;
+    // (Read anew, again: nothing of this is held through the tile loop.)
+    const ChunkParams pe = load_kernarg<ChunkParams>();
+    const DevChunkItem ie = load_const(pe.items, __builtin_amdgcn_readfirstlane(at));
+    int te = threadIdx.x;
+    asm volatile("" : "+v"(te));
+    const int ge = pe.g, r = ie.row0 + (te >> 6) * kFastRowsPerWave + (te & 31), Ge = te >> 5 & 1;
+    if (r >= ie.len * ge) continue;
+    const int t = r / ge, h = ie.kvh * ge + (r - t * ge);
+    // (A piece of a split may hold no key that the row sees. A NaN sum stays NaN.)
+    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+    const float lse = lt == 0.0f ? -INFINITY : (m_out + log2f(lt)) * kLn2;
+    auto store = [&](auto *op) __attribute__((always_inline)) {
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4)
+          store4(op + dt * 32 + crow(j, Ge), oacc[dt][j] * inv, oacc[dt][j + 1] * inv, oacc[dt][j + 2] * inv, oacc[dt][j + 3] * inv);
+    };
+    if (ie.part < 0) {
+      store((__bf16 *)pe.o + (((int64_t)ie.tok0 + t) * (pe.Hkv * ge) + h) * D);
+      if (Ge == 0 && pe.lse != nullptr) pe.lse[(int64_t)h * pe.Tq + ie.tok0 + t] = lse;
+    } else {
+      const int64_t R = (int64_t)ie.part * kFastRowsPerWg + (r - ie.row0);
+      store(pe.part_o + R * D);
+      if (Ge == 0) pe.part_lse[R] = lse;
+    }
   }
 }
 
@@ -397,9 +416,9 @@ void launch_chunk_merge_t(const ChunkParams &p, int few, int n_merges, hipStream
 
 }  // namespace
 
-hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_items, hipStream_t s) {
-  if (D == 64) hipLaunchKernelGGL(chunk_bf16_kernel<64>, dim3((unsigned)n_items), dim3(kFastThreads), 0, s, p);
-  else hipLaunchKernelGGL(chunk_bf16_kernel<128>, dim3((unsigned)n_items), dim3(kFastThreads), 0, s, p);
+hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_wgs, hipStream_t s) {
+  if (D == 64) hipLaunchKernelGGL(chunk_bf16_kernel<64>, dim3((unsigned)n_wgs), dim3(kFastThreads), 0, s, p);
+  else hipLaunchKernelGGL(chunk_bf16_kernel<128>, dim3((unsigned)n_wgs), dim3(kFastThreads), 0, s, p);
   return hipGetLastError();
 }
 

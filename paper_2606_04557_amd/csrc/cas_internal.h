@@ -319,11 +319,11 @@ struct AppendParams {
 };
 static_assert(sizeof(AppendParams) <= 4096, "kernel arguments");
 
-// Chunk attention over pages. One workgroup: up to 256 packed rows from row0 on
+// Chunk attention over pages. One item: up to 256 packed rows from row0 on
 // (row r of a request is its token r / g, head r % g of the KV head's group) of
 // a request with `len` new tokens from tok0 on, its last of kv_len keys, in the
 // pages page_ids[page0 ..], over 64-key tiles [tile0, tile1). part: which
-// partial it writes, or -1: no other workgroup has these rows.
+// partial it writes, or -1: no other item has these rows.
 struct DevChunkItem {
   int32_t tok0, len, kv_len, page0, row0, kvh, tile0, tile1, part;
 };
@@ -339,6 +339,7 @@ struct ChunkParams {
   void *o;
   float *lse;                  // [Hq][Tq] or null
   const DevChunkItem *items;
+  const int32_t *wg_items;     // workgroup i: items[wg_items[i] .. wg_items[i + 1])
   const DevChunkMerge *merges;
   const int32_t *page_ids;
   float *part_o;               // [partial][256][D], normalised
@@ -386,7 +387,7 @@ hipError_t launch_adam_bf16(const AdamParams &p, int D, int n_chunks, hipStream_
 hipError_t launch_decode_bf16(const DecodeParams &p, int D, int n_work, int row_blocks, hipStream_t s);
 hipError_t launch_decode_merge_bf16(const DecodeParams &p, int D, int max_split, hipStream_t s);
 hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_groups, hipStream_t s);
-hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_items, hipStream_t s);
+hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_wgs, hipStream_t s);
 // n_merges blocks, of which the first `few` have at most kChunkFewRows rows.
 hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_merges, int max_parts, hipStream_t s);
 // Copies `bytes` (a multiple of 16) of pinned host memory to device memory and

@@ -389,143 +389,196 @@ cas_status_t run_append(const cas_decode_problem_t *p, const cas_rope_t *rope, c
 // ---------------------------------------------------------------------------
 constexpr int kChunkRows = 256;     // packed rows of a workgroup
 constexpr int kChunkTile = 64;
-constexpr int kMaxChunkParts = 64;  // pieces of one block of rows
 
 struct ChunkPlan {
-  std::vector<DevChunkItem> items;   // in dispatch order
+  std::vector<DevChunkItem> items;   // workgroup after workgroup, in dispatch order
+  std::vector<int32_t> wg_items;     // its first item, of every workgroup, and the end
   std::vector<DevChunkMerge> merges;   // the blocks of few rows first
   int32_t parts = 0, max_parts = 1, few = 0;
   int64_t tiles = 0;
-  size_t off_merges = 0, off_pages = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
+  size_t off_wgs = 0, off_merges = 0, off_pages = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Blocks of rows of every request and KV head, cut along the key axis where the
-// blocks alone would leave compute units without work. Costs are in key tiles;
-// one workgroup runs per compute unit at a time and costs about kWgTiles beside
-// its tiles (dispatch, first loads, epilogue), a merge kMergeTiles for its
-// launch, and the partials' bytes at kBytesPerTile.
-constexpr double kWgTiles = 8.0, kMergeTiles = 3.0, kBytesPerTile = 5e6;
+// Costs, in 64-key tiles of 256 rows with d = 128 (1.94 us). A tile of few rows
+// costs more than its share (a phase waits for its copies and barriers): 1.14 us
+// for 32 rows, 1.38 for 128; with d = 64 0.88 to 1.30 us. kWgCost: what a
+// workgroup costs beside its tiles (dispatch, first loads, pipeline fill and
+// drain, epilogue), kItemCost: a further item of a workgroup; kMergeCost: a
+// merge's launch; the partials' bytes, written and read, at kBytesPerTile.
+double tile_cost(int D, int rows) { return D == 128 ? 0.57 + 0.43 * rows / 256 : 0.45 + 0.22 * rows / 256; }
+constexpr double kWgCost = 5.0, kItemCost = 3.0, kMergeCost = 3.0, kBytesPerTile = 5e6;
+constexpr double kWorthIt = 0.97;   // of the cost without cuts: below it, blocks are cut
+constexpr int kMinPiece = 2;        // tiles
+constexpr int kManyRounds = 8;
 
+struct ChunkBlock {
+  int32_t b, row0, rows, tiles, kvh;
+  double cost;   // of a tile
+};
+struct ChunkPiece {
+  int32_t block, t0, t1;
+};
+
+// Cuts the blocks for n_bins workgroups that all cost about the same: whole
+// blocks, longest first, to the workgroup with the least so far while they fit,
+// then the other blocks in pieces into what is left. Returns the largest cost.
+double fill_bins(const std::vector<ChunkBlock> &blocks, int n_bins, std::vector<std::vector<ChunkPiece>> &bins) {
+  bins.assign(n_bins, {});
+  std::vector<double> load(n_bins, kWgCost - kItemCost);
+  std::vector<int32_t> order(blocks.size());
+  double sum = 0.0;
+  for (size_t i = 0; i < blocks.size(); ++i) {
+    order[i] = (int32_t)i;
+    sum += blocks[i].tiles * blocks[i].cost;
+  }
+  auto whole = [&](int32_t i) { return blocks[i].tiles * blocks[i].cost + kItemCost; };
+  std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return whole(x) > whole(y); });
+  // An equal share of all blocks, and a piece beside whole ones; at least a piece.
+  double target = kWgCost + (sum + kItemCost * (double)blocks.size()) / n_bins;
+  for (const ChunkBlock &x : blocks) target = std::max(target, kWgCost + std::min<int>(kMinPiece, x.tiles) * x.cost);
+  std::vector<int32_t> left;
+  auto later = [&](int x, int y) { return load[x] != load[y] ? load[x] > load[y] : x > y; };
+  std::vector<int> heap(n_bins);
+  for (int i = 0; i < n_bins; ++i) heap[i] = i;
+  std::make_heap(heap.begin(), heap.end(), later);
+  for (int32_t i : order) {
+    const int x = heap.front();
+    if (load[x] + whole(i) > target) {
+      left.push_back(i);
+      continue;
+    }
+    std::pop_heap(heap.begin(), heap.end(), later);
+    bins[x].push_back({i, 0, blocks[i].tiles});
+    load[x] += whole(i);
+    std::push_heap(heap.begin(), heap.end(), later);
+  }
+  std::vector<int> by_room(n_bins);
+  for (int i = 0; i < n_bins; ++i) by_room[i] = i;
+  std::stable_sort(by_room.begin(), by_room.end(), [&](int x, int y) { return load[x] < load[y]; });
+  size_t k = 0;
+  for (int32_t i : left) {
+    for (int32_t t = 0; t < blocks[i].tiles;) {
+      const int32_t rest = blocks[i].tiles - t;
+      int32_t take = rest;
+      if (k < by_room.size()) {
+        take = (int32_t)std::max(0.0, std::min((double)rest, (target - load[by_room[k]] - kItemCost) / blocks[i].cost + 0.5));
+        if (take < std::min(kMinPiece, rest)) {
+          ++k;
+          continue;
+        }
+        if (rest - take < kMinPiece) take = rest;
+      }
+      const int x = k < by_room.size() ? by_room[k] : (int)(std::min_element(load.begin(), load.end()) - load.begin());
+      bins[x].push_back({i, t, t + take});
+      load[x] += kItemCost + take * blocks[i].cost;
+      t += take;
+      if (t < blocks[i].tiles) ++k;   // (the workgroup is full)
+    }
+  }
+  return *std::max_element(load.begin(), load.end());
+}
+
+// The launch plan. Either a workgroup per block, longest first, which the
+// hardware hands out as compute units become free; or, where that leaves some
+// idle, one workgroup per compute unit with an equal share, blocks cut along the
+// key axis as that needs and merged afterwards.
+//
+// Workgroup i goes to XCD i mod X, each with its own L2, so a KV head's workgroups
+// stay on one XCD (or on X / Hkv of them) where the heads divide evenly.
 cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   cas_status_t s = check_paged(p);
   if (s != CAS_OK) return s;
   if (!std::isfinite(p->softmax_scale) || !(p->softmax_scale > 0.0f))
     return set_error(CAS_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
-  const int B = p->batch, g = p->group_size, Hkv = p->num_kv_heads;
+  const int B = p->batch, g = p->group_size, Hkv = p->num_kv_heads, D = p->head_dim;
   const Topology topo = device_topology();
-  struct Block {
-    int32_t b, row0, rows, tiles;
-  };
-  std::vector<Block> blocks;   // of one KV head
-  int32_t longest = 0;
-  int64_t total = 0;
-  for (int b = 0; b < B; ++b) {
-    const int64_t n = p->q_offsets[b + 1] - p->q_offsets[b], nrows = n * g, before = p->kv_lens[b] - n;
-    for (int64_t r = 0; r < nrows; r += kChunkRows) {
-      const int64_t r1 = std::min<int64_t>(nrows, r + kChunkRows);
-      const int32_t nt = (int32_t)((before + (r1 - 1) / g) / kChunkTile + 1);   // up to its last query's own key
-      blocks.push_back({b, (int32_t)r, (int32_t)(r1 - r), nt});
-      longest = std::max(longest, nt);
-      total += nt;
-    }
-  }
-  if ((int64_t)blocks.size() * Hkv > INT32_MAX / kMaxChunkParts) return set_error(CAS_ERR_UNSUPPORTED, "too many workgroups");
-  auto pieces = [&](const Block &x, int64_t per) { return std::min<int64_t>(kMaxChunkParts, ceil_div(x.tiles, per)); };
-  // An estimate of the step with pieces of at most `per` tiles: the work spread
-  // evenly, the longest workgroup, and what the k + 1 shortest of the k * cus + 1
-  // longest ones take, of which one unit gets k + 1.
-  const int64_t cus = topo.cus;
-  std::vector<double> cost;
-  auto step_cost = [&](int64_t per) {
-    double sum = 0.0, bytes = 0.0;
-    cost.clear();
-    int64_t n = 0;
-    for (const Block &x : blocks) n += pieces(x, per) * Hkv;
-    const bool few = n <= 4 * cus;
-    double most = 0.0;
-    for (const Block &x : blocks) {
-      const int64_t k = pieces(x, per);
-      const double c = kWgTiles + (double)ceil_div(x.tiles, k);
-      sum += (kWgTiles * k + x.tiles) * Hkv;
-      most = std::max(most, c);
-      if (k > 1) bytes += (double)k * x.rows * p->head_dim * 4 * Hkv;
-      for (int64_t i = 0; few && i < k * Hkv; ++i) cost.push_back(c);
-    }
-    double t = std::max(sum / (double)cus, most);
-    if (few) {
-      std::sort(cost.begin(), cost.end(), std::greater<double>());
-      for (int64_t k = 1; k * cus < (int64_t)cost.size(); ++k) {
-        double c = 0.0;
-        for (int64_t i = k * cus - k; i <= k * cus; ++i) c += cost[i];
-        t = std::max(t, c);
+  const int X = std::max(1, topo.xcds), cus = std::max(X, topo.cus);
+  // KV heads kvh with kvh mod groups == i share the XCDs x with x mod groups == i.
+  const int groups = Hkv % X == 0 ? X : X % Hkv == 0 ? Hkv : 1;
+  const int bins = cus / groups, heads = Hkv / groups;   // of a group
+  std::vector<ChunkBlock> blocks;                        // of the first group's heads
+  double sum = 0.0;
+  for (int h = 0; h < heads; ++h)
+    for (int b = 0; b < B; ++b) {
+      const int64_t n = p->q_offsets[b + 1] - p->q_offsets[b], nrows = n * g, before = p->kv_lens[b] - n;
+      for (int64_t r = 0; r < nrows; r += kChunkRows) {
+        const int64_t r1 = std::min<int64_t>(nrows, r + kChunkRows);
+        const int32_t nt = (int32_t)((before + (r1 - 1) / g) / kChunkTile + 1);   // up to its last query's own key
+        blocks.push_back({b, (int32_t)r, (int32_t)(r1 - r), nt, h * groups, tile_cost(D, (int)(r1 - r))});
+        sum += blocks.back().tiles * blocks.back().cost + kWgCost;
       }
     }
-    return bytes > 0.0 ? t + kMergeTiles + bytes / kBytesPerTile : t;
-  };
-  int64_t best = std::max<int32_t>(1, longest);
-  if (!blocks.empty()) {
-    double best_cost = step_cost(best);
-    // Lengths that give the units 1, 2, ... pieces each, and shorter and shorter ones.
-    std::vector<int64_t> tries;
-    for (int r = 1; r <= 4; ++r) tries.push_back(ceil_div(total * Hkv, cus * r));
-    for (int k = 2; k <= 32; k += k < 8 ? 1 : 8) tries.push_back(ceil_div(longest, k));
-    for (int64_t per : tries) {
-      per = std::max<int64_t>(per, std::max<int64_t>(2, ceil_div(longest, kMaxChunkParts)));
-      if (per >= longest) continue;
-      const double c = step_cost(per);
-      if (c < best_cost) {
-        best_cost = c;
-        best = per;
+  if ((int64_t)blocks.size() * groups > INT32_MAX / 256) return set_error(CAS_ERR_UNSUPPORTED, "too many workgroups");
+  // A group's workgroups, in order, and what they cost; first a block each.
+  std::vector<std::vector<ChunkPiece>> wgs;
+  std::stable_sort(blocks.begin(), blocks.end(), [](const ChunkBlock &x, const ChunkBlock &y) { return x.tiles * x.cost > y.tiles * y.cost; });
+  auto whole = [&](size_t i) { return blocks[i].tiles * blocks[i].cost + kWgCost; };
+  double alone = sum / bins;
+  // (Of the k * bins + 1 longest blocks, one unit gets k + 1.)
+  for (size_t k = 0; k < 4 && k * bins < blocks.size(); ++k) {
+    double c = 0.0;
+    for (size_t i = k * bins - k; i <= k * bins; ++i) c += whole(i);
+    alone = std::max(alone, c);
+  }
+  for (size_t i = 0; i < blocks.size(); ++i) wgs.push_back({{(int32_t)i, 0, blocks[i].tiles}});
+  // Units differ in speed by a few per cent, which evens out where each gets
+  // several blocks from the hardware: with kManyRounds of them nothing is cut.
+  if (!blocks.empty() && blocks.size() < (size_t)(kManyRounds * bins)) {
+    std::vector<std::vector<ChunkPiece>> equal;
+    double even = fill_bins(blocks, bins, equal) + kMergeCost;
+    std::vector<int32_t> n_pieces(blocks.size(), 0);
+    for (const auto &w : equal)
+      for (const ChunkPiece &x : w) ++n_pieces[x.block];
+    double bytes = 0.0;
+    for (size_t i = 0; i < blocks.size(); ++i)
+      if (n_pieces[i] > 1) bytes += (double)n_pieces[i] * blocks[i].rows * D * 4;
+    even += bytes * groups / kBytesPerTile;
+    if (even < kWorthIt * alone) wgs.swap(equal);
+  }
+  wgs.erase(std::remove_if(wgs.begin(), wgs.end(), [](const std::vector<ChunkPiece> &w) { return w.empty(); }), wgs.end());
+  // Partials: a block's lie together, in the order of its keys.
+  std::vector<std::vector<int32_t>> cut(blocks.size());
+  for (const auto &w : wgs)
+    for (const ChunkPiece &x : w) cut[x.block].push_back(x.t0);
+  std::vector<int32_t> part0(blocks.size(), -1);
+  int32_t parts = 0;   // of a group
+  for (size_t i = 0; i < blocks.size(); ++i) {
+    std::sort(cut[i].begin(), cut[i].end());
+    pl.max_parts = std::max(pl.max_parts, (int32_t)cut[i].size());
+    if (cut[i].size() < 2) continue;
+    part0[i] = parts;
+    parts += (int32_t)cut[i].size();
+  }
+  if ((int64_t)parts * groups > INT32_MAX / kChunkRows) return set_error(CAS_ERR_UNSUPPORTED, "too many partials");
+  pl.parts = parts * groups;
+  for (int few = 1; few >= 0; --few) {
+    for (int gr = 0; gr < groups; ++gr)
+      for (size_t i = 0; i < blocks.size(); ++i) {
+        const ChunkBlock &x = blocks[i];
+        if (part0[i] < 0 || (x.rows <= kChunkFewRows) != (few == 1)) continue;
+        pl.merges.push_back({p->q_offsets[x.b], p->q_offsets[x.b + 1] - p->q_offsets[x.b], x.row0, x.kvh + gr, gr * parts + part0[i],
+                             (int32_t)cut[i].size()});
+      }
+    if (few) pl.few = (int32_t)pl.merges.size();
+  }
+  // Groups in turn, so that workgroup i belongs to group i mod groups.
+  for (const auto &w : wgs)
+    for (int gr = 0; gr < groups; ++gr) {
+      pl.wg_items.push_back((int32_t)pl.items.size());
+      for (const ChunkPiece &y : w) {
+        const ChunkBlock &x = blocks[y.block];
+        const int32_t tok0 = p->q_offsets[x.b];
+        const int32_t part = part0[y.block] < 0 ? -1 : gr * parts + part0[y.block] +
+            (int32_t)(std::lower_bound(cut[y.block].begin(), cut[y.block].end(), y.t0) - cut[y.block].begin());
+        pl.items.push_back({tok0, p->q_offsets[x.b + 1] - tok0, p->kv_lens[x.b], p->page_offsets[x.b], x.row0, x.kvh + gr, y.t0, y.t1, part});
+        pl.tiles += y.t1 - y.t0;
       }
     }
-  }
-  // The items of one KV head; its blocks' partials lie together.
-  std::vector<std::vector<DevChunkItem>> by_head(Hkv);
-  for (int kvh = 0; kvh < Hkv; ++kvh)
-    for (const Block &x : blocks) {
-      const int32_t k = (int32_t)pieces(x, best), tok0 = p->q_offsets[x.b], len = p->q_offsets[x.b + 1] - tok0;
-      if (k > 1) pl.merges.push_back({tok0, len, x.row0, kvh, pl.parts, k});
-      for (int32_t i = 0; i < k; ++i)
-        by_head[kvh].push_back({tok0, len, p->kv_lens[x.b], p->page_offsets[x.b], x.row0, kvh,
-                                (int32_t)((int64_t)x.tiles * i / k), (int32_t)((int64_t)x.tiles * (i + 1) / k), k > 1 ? pl.parts++ : -1});
-      pl.max_parts = std::max(pl.max_parts, k);
-      pl.tiles += x.tiles;
-    }
-  pl.few = (int32_t)(std::stable_partition(pl.merges.begin(), pl.merges.end(), [&](const DevChunkMerge &m) {
-    return (int64_t)m.len * g - m.row0 <= kChunkFewRows;
-  }) - pl.merges.begin());
-  // Dispatch order. Workgroup i goes to XCD i mod X, each with its own L2, so a KV
-  // head's workgroups stay on one XCD (or on X / Hkv of them), longest first.
-  auto longer = [](const DevChunkItem &a, const DevChunkItem &b) { return a.tile1 - a.tile0 > b.tile1 - b.tile0; };
-  const int X = std::max(1, topo.xcds);
-  std::vector<std::vector<DevChunkItem>> share;
-  if (Hkv % X == 0) {
-    share.resize(X);
-    for (int kvh = 0; kvh < Hkv; ++kvh) {
-      auto &v = share[kvh % X];
-      v.insert(v.end(), by_head[kvh].begin(), by_head[kvh].end());
-    }
-  } else if (X % Hkv == 0) {
-    share.resize(X);
-    for (int kvh = 0; kvh < Hkv; ++kvh) {
-      std::stable_sort(by_head[kvh].begin(), by_head[kvh].end(), longer);
-      for (size_t i = 0; i < by_head[kvh].size(); ++i) share[kvh + Hkv * (i % (X / Hkv))].push_back(by_head[kvh][i]);
-    }
-  } else {
-    share.resize(1);
-    for (auto &v : by_head) share[0].insert(share[0].end(), v.begin(), v.end());
-  }
-  size_t rounds = 0;
-  for (auto &v : share) {
-    std::stable_sort(v.begin(), v.end(), longer);
-    rounds = std::max(rounds, v.size());
-  }
-  for (size_t i = 0; i < rounds; ++i)
-    for (auto &v : share)
-      if (i < v.size()) pl.items.push_back(v[i]);
-  pl.off_merges = align256(pl.items.size() * sizeof(DevChunkItem));
+  pl.wg_items.push_back((int32_t)pl.items.size());
+  pl.off_wgs = align256(pl.items.size() * sizeof(DevChunkItem));
+  pl.off_merges = align256(pl.off_wgs + pl.wg_items.size() * sizeof(int32_t));
   pl.off_pages = align256(pl.off_merges + pl.merges.size() * sizeof(DevChunkMerge));
   pl.table_bytes = align256(pl.off_pages + (size_t)p->page_offsets[B] * sizeof(int32_t));
   pl.off_plse = pl.table_bytes;
@@ -606,6 +659,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   char *ws = (char *)workspace;
   auto fill = [&](char *h) {
     std::memcpy(h, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
+    std::memcpy(h + pl.off_wgs, pl.wg_items.data(), pl.wg_items.size() * sizeof(int32_t));
     if (!pl.merges.empty()) std::memcpy(h + pl.off_merges, pl.merges.data(), pl.merges.size() * sizeof(DevChunkMerge));
     std::memcpy(h + pl.off_pages, p->page_ids, (size_t)p->page_offsets[p->batch] * sizeof(int32_t));
   };
@@ -627,6 +681,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   c.o = o;
   c.lse = lse;
   c.items = (const DevChunkItem *)ws;
+  c.wg_items = (const int32_t *)(ws + pl.off_wgs);
   c.merges = (const DevChunkMerge *)(ws + pl.off_merges);
   c.page_ids = (const int32_t *)(ws + pl.off_pages);
   c.part_lse = (float *)(ws + pl.off_plse);
@@ -636,7 +691,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   c.page_size = p->page_size;
   c.Tq = p->q_offsets[p->batch];
   c.scale_log2 = p->softmax_scale * 1.4426950408889634f;
-  hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, (int)pl.items.size(), stream); });
+  hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, (int)pl.wg_items.size() - 1, stream); });
   if (e != hipSuccess) return set_hip_error("chunk launch", e);
   if (!pl.merges.empty()) {
     e = timed_launch("chunk_merge", stream, [&] {
@@ -777,17 +832,20 @@ cas_status_t cas_paged_chunk_plan_destroy(cas_chunk_plan_t *plan) {
   return CAS_OK;
 }
 
-cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items) {
+cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items,
+                                       int32_t *wg_items) {
   if (!plan || !info) return set_error(CAS_ERR_INVALID_ARGUMENT, "plan or info is NULL");
   const ChunkPlan &pl = plan->plan;
   *info = cas_chunk_plan_info_t{};
-  info->workgroups = (int32_t)pl.items.size();
+  info->workgroups = (int32_t)pl.wg_items.size() - 1;
+  info->items = (int32_t)pl.items.size();
   info->partials = pl.parts;
   info->max_partials = pl.max_parts;
   info->key_tiles = pl.tiles;
   info->ws_bytes = pl.bytes;
   static_assert(sizeof(DevChunkItem) == 36, "a table of 32-bit values");
   if (items && !pl.items.empty()) std::memcpy(items, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
+  if (wg_items) std::memcpy(wg_items, pl.wg_items.data(), pl.wg_items.size() * sizeof(int32_t));
   return CAS_OK;
 }
 

@@ -27,8 +27,9 @@ def problem(cas, q, kv, P=16, Hkv=2, g=2, D=64, pages=None):
 def check(cas, q, kv, **kw):
     prob = problem(cas, q, kv, **kw)
     P, Hkv, g = prob.c.page_size, prob.c.num_kv_heads, prob.c.group_size
-    info, items = cas.chunk_plan(prob)
-    assert len(items) == info.workgroups and sum(i[7] - i[6] for i in items) == info.key_tiles
+    info, items, wgs = cas.chunk_plan(prob)
+    assert len(items) == info.items and sum(i[7] - i[6] for i in items) == info.key_tiles
+    assert len(wgs) == info.workgroups + 1 and (wgs[0], wgs[-1]) == (0, info.items) and all(a < b for a, b in zip(wgs, wgs[1:]))
     seen, parts = {}, {}
     page0 = [0]
     for L in kv:
@@ -50,7 +51,7 @@ def check(cas, q, kv, **kw):
         p = sorted(parts[k])
         assert p == [-1] if len(p) == 1 else p == list(range(p[0], p[0] + len(p))) and p[0] >= 0
         all_parts += [x for x in p if x >= 0]
-    assert sorted(all_parts) == list(range(info.partials)) and info.max_partials <= 64
+    assert sorted(all_parts) == list(range(info.partials))
     assert cas.paged_chunk_workspace_size(prob) == info.ws_bytes >= info.partials * ROWS * (prob.c.head_dim + 1) * 4
     return info
 
@@ -65,14 +66,33 @@ def test_plans(cas):
               D=r.choice([64, 128]))
 
 
-def test_splits_fill_the_compute_units(cas):
-    """A prompt's chunk over a long context is cut into about as many workgroups
-    as there are compute units, a batch that fills them is not cut."""
-    one = check(cas, [512], [16384 + 512], Hkv=8, g=4, D=128)
-    assert one.workgroups == 256 and one.max_partials == 4
-    full = check(cas, [2048] * 4, [4096] * 4, Hkv=8, g=4, D=128)
+def loads(cas, prob):
+    info, items, wgs = cas.chunk_plan(prob)
+    return info, [sum(i[7] - i[6] for i in items[a:b]) for a, b in zip(wgs, wgs[1:])]
+
+
+def test_workgroups_have_equal_shares(cas):
+    """A prompt's chunk over a long context is cut into one workgroup per compute
+    unit, blocks that fill them without a rest are not cut, and neither are many."""
+    kw = dict(Hkv=8, g=4, D=128)
+    one, n = loads(cas, problem(cas, [512], [16384 + 512], **kw))
+    assert one.workgroups == 256 and max(n) <= 1.1 * one.key_tiles / 256
+    full, n = loads(cas, problem(cas, [2048] * 4, [4096] * 4, **kw))
     assert full.partials == 0
-    assert check(cas, [1], [64], Hkv=8, g=4, D=128).partials == 0
+    odd, n = loads(cas, problem(cas, [300] * 16, [4500] * 16, **kw))       # 640 blocks: two and a half per unit
+    assert odd.workgroups == 256 and odd.partials > 0 and max(n) <= 1.1 * odd.key_tiles / 256
+    many, n = loads(cas, problem(cas, [2000] * 16, [4500] * 16, **kw))
+    assert many.partials == 0 and many.workgroups == many.items
+    assert loads(cas, problem(cas, [1], [64], **kw))[0].partials == 0
+
+
+def test_heads_keep_to_their_xcds(cas):
+    """Workgroup i runs on XCD i mod 8."""
+    for Hkv in (1, 2, 4, 8, 16):
+        _, items, wgs = cas.chunk_plan(problem(cas, [700, 1, 90], [5000, 3000, 90], Hkv=Hkv, g=4, D=128))
+        groups = min(Hkv, 8)
+        for i, (a, b) in enumerate(zip(wgs, wgs[1:])):
+            assert all(x[5] % groups == i % groups for x in items[a:b])
 
 
 @pytest.mark.parametrize("q,kv,pages,code", [
