@@ -524,12 +524,12 @@ int32_t cas_paged_chunk_plan_matches(const cas_chunk_plan_t *plan, const cas_dec
 cas_status_t cas_paged_chunk_plan_destroy(cas_chunk_plan_t *plan);
 
 /*
- * A plan's launch tables (host only; for tests and profiling tools). items and
- * wg_items may be NULL; otherwise items receives 9 values per item: first token
- * and token count of the request, its key count, its first entry of page_ids, the
- * block's first row (tokens x group heads), KV head, first and one past the last
- * 64-key tile, and the partial that it writes (-1: the result); and wg_items the
- * first item of every workgroup, in dispatch order, and the end (workgroups + 1).
+ * A plan's launch table (host only; for tests and profiling tools). items may be
+ * NULL; otherwise it receives 10 values per item: first token and token count of
+ * the request, its key count, its first entry of page_ids, the block's first row
+ * (tokens x group heads), KV head, first and one past the last 64-key tile, the
+ * partial that it writes (-1: the result), and its workgroup's next item (-1:
+ * none). Workgroup i, in dispatch order, begins with item i.
  */
 typedef struct {
   int32_t workgroups;
@@ -540,8 +540,7 @@ typedef struct {
   size_t ws_bytes;
 } cas_chunk_plan_info_t;
 
-cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items,
-                                       int32_t *wg_items);
+cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items);
 
 /*
  * Budget manager (paper: paragraphs "Budget Manager" and "Pool rotation";

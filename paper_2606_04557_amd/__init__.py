@@ -731,13 +731,19 @@ def paged_chunk_fwd(q, k_pages, v_pages, problem: DecodeProblem, o=None, lse=Non
 
 
 def chunk_plan(problem: DecodeProblem):
-    """The launch plan of paged_chunk_fwd (cas_paged_chunk_plan_info): its counts,
-    its items (a tuple each) and the first item of every workgroup."""
+    """The launch plan of paged_chunk_fwd (cas_paged_chunk_plan_info): its counts
+    and the items of every workgroup (a tuple each)."""
     plan, info = problem.chunk_plan(), _lib.ChunkPlanInfo()
-    _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), None, None))
-    items, wgs = (ctypes.c_int32 * (9 * max(info.items, 1)))(), (ctypes.c_int32 * (info.workgroups + 1))()
-    _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), items, wgs))
-    return info, list(zip(*[iter(items)] * 9))[:info.items], list(wgs)
+    _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), None))
+    flat = (ctypes.c_int32 * (10 * max(info.items, 1)))()
+    _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), flat))
+    items, wgs = list(zip(*[iter(flat)] * 10)), []
+    for i in range(info.workgroups):
+        wgs.append([])
+        while i >= 0:
+            wgs[-1].append(items[i])
+            i = items[i][9]
+    return info, wgs
 
 
 def plan_rotation(steps: Sequence[int], active: Sequence[bool], budget: int, swap_fraction: float):

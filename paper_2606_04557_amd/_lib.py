@@ -198,7 +198,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cas_paged_chunk_plan_matches.argtypes = [vp, P(DecodeProblem)]
     lib.cas_paged_chunk_plan_matches.restype = i32
     lib.cas_paged_chunk_plan_destroy.argtypes = [vp]
-    lib.cas_paged_chunk_plan_info.argtypes = [vp, P(ChunkPlanInfo), P(i32), P(i32)]
+    lib.cas_paged_chunk_plan_info.argtypes = [vp, P(ChunkPlanInfo), P(i32)]
     u8p = P(ctypes.c_uint8)
     lib.cas_pool_plan_rotation.argtypes = [P(i32), u8p, i32, i32, ctypes.c_float, P(i32), P(i32), P(i32)]
     lib.cas_pool_create.argtypes = [P(PoolConfig), P(vp)]

@@ -61,7 +61,7 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 v) {
 
 template <int D>
 __global__ __launch_bounds__(kFastThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void chunk_bf16_kernel(ChunkParams p0) {
+void chunk_bf16_kernel(ChunkParams) {
   constexpr int NSTEP = D / 16, DT = D / 32;
   constexpr int TB = kKT * D * 2;
   constexpr int CPR = D / 8, RPI = 64 / CPR;   // 16-byte chunks of a key row, key rows of a copy instruction
@@ -73,9 +73,8 @@ void chunk_bf16_kernel(ChunkParams p0) {
   __shared__ __attribute__((aligned(1024))) char vb1[TB];
   __shared__ __attribute__((aligned(1024))) char vb2[TB];
 
-  const int end = load_const(p0.wg_items, (int)blockIdx.x + 1);
 #pragma unroll 1
-  for (int at = load_const(p0.wg_items, (int)blockIdx.x); at < end; ++at) {
+  for (int at = blockIdx.x; at >= 0;) {
     // Per item, the lane index and the parameters are read anew: values kept
     // across items would be held in registers through the tile loop.
     int tid = threadIdx.x;
@@ -92,7 +91,7 @@ void chunk_bf16_kernel(ChunkParams p0) {
     to.init(lane);
     const int page_shift = __builtin_ctz(p.page_size), row_elems = Hkv * D;
     const int lane_off = (lane / CPR) * row_elems * 2 + (((lane % CPR) ^ swz<D>(w4 * RPI + lane / CPR)) << 4);
-    const DevChunkItem it = load_const(p.items, __builtin_amdgcn_readfirstlane(at));
+    const DevChunkItem it = load_const(p.items, at);
     const int nrows = it.len * g;
     const int row0 = it.row0 + wave * kFastRowsPerWave, my_row = row0 + n;
     const bool wave_active = row0 < nrows;
@@ -127,10 +126,13 @@ void chunk_bf16_kernel(ChunkParams p0) {
       dma16(make_rsrc((const __bf16 *)pool + row * row_elems + it.kvh * D, valid > 0 ? ((valid - 1) * row_elems + D) * 2 : 0),
             lane_off, buf + (w4 + 4 * i) * 1024);
     };
-    // The first K tile is on its way while the queries are.
-    Tile tk;   // of the K copied last, whose V is copied next
+    // On their way together: the first K tile, the queries, then the first V and
+    // the second K.
+    Tile tk, tn;   // of the K copied last, whose V is copied next, and of the next K
     if (grp == 1) {
+      wait_vmcnt<0>();   // (the item before's stores: the partial counts below are of copies alone)
       tk = tile_at(0);
+      tn = tile_at(min(1, nt - 1));
 #pragma unroll
       for (int i = 0; i < PER; ++i) copy(kb0, p.k_pages, tk, true, i);
     }
@@ -143,9 +145,17 @@ void chunk_bf16_kernel(ChunkParams p0) {
 #pragma unroll
       for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
     }
-    // Tile copies are waited for with partial vmcnt counts, which must not
-    // include these loads (and phase 0 reads the first K).
-    wait_vmcnt<0>();
+    if (grp == 1) {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) copy(vb0, p.v_pages, tk, true, i);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) copy(kb1, p.k_pages, tn, nt > 1, i);
+      tk = tn;
+      tn = tile_at(min(2, nt - 1));
+      wait_vmcnt<2 * PER>();   // the first K and the queries
+    } else {
+      wait_vmcnt<0>();
+    }
 
     f32x16 oacc[DT];
     float m_run = -INFINITY, l_run = 0.0f;   // exponent offset of this lane's row, row sum of its keys
@@ -198,28 +208,20 @@ void chunk_bf16_kernel(ChunkParams p0) {
       };
       auto no_piece = [](int) {};
       auto even_b = [&](int i, char *kbn, char *vbn) __attribute__((always_inline)) {
-        const Tile tv = tk;
-        const Tile tn = tile_at(min(i + 2, nt - 1));
+        const Tile tv = tk, tc = tn;
+        tn = tile_at(min(i + 3, nt - 1));   // (page ids, a tile ahead of their use)
         const bool has_v = i + 1 < nt, has_k = i + 2 < nt;
         xphase(i - 1, [&](int n) __attribute__((always_inline)) {
           if (n < PER) copy(vbn, p.v_pages, tv, has_v, n);
-          else copy(kbn, p.k_pages, tn, has_k, n - PER);
+          else copy(kbn, p.k_pages, tc, has_k, n - PER);
         });
-        tk = tn;
+        tk = tc;
         wait_vmcnt<2 * PER>();
       };
 
       // (At least one tile: the host lists no empty range.) G_0 multiplies V
       // buffer 2 by P = 0: clear it so no stale bit pattern (a NaN) can reach O.
       for (int i = tid; i < TB / 16; i += kFastThreads) reinterpret_cast<uint4 *>(vb2)[i] = uint4{0, 0, 0, 0};
-      if (grp == 1) {
-        const Tile t1 = tile_at(min(1, nt - 1));
-#pragma unroll
-        for (int i = 0; i < PER; ++i) copy(vb0, p.v_pages, tk, true, i);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) copy(kb1, p.k_pages, t1, nt > 1, i);
-        tk = t1;
-      }
       lds_barrier();
       // Six phases per iteration (three tiles), so every buffer is a fixed LDS
       // address: G_i reads K_i from kb[i%3] and V_{i-1} from vb[(i-1)%3]; the
@@ -317,7 +319,8 @@ void chunk_bf16_kernel(ChunkParams p0) {
     const float m_out = m_run;
     // (Read anew, again: nothing of this is held through the tile loop.)
     const ChunkParams pe = load_kernarg<ChunkParams>();
-    const DevChunkItem ie = load_const(pe.items, __builtin_amdgcn_readfirstlane(at));
+    const DevChunkItem ie = load_const(pe.items, at);
+    at = __builtin_amdgcn_readfirstlane(ie.next);
     int te = threadIdx.x;
     asm volatile("" : "+v"(te));
     const int ge = pe.g, r = ie.row0 + (te >> 6) * kFastRowsPerWave + (te & 31), Ge = te >> 5 & 1;

@@ -326,6 +326,7 @@ static_assert(sizeof(AppendParams) <= 4096, "kernel arguments");
 // partial it writes, or -1: no other item has these rows.
 struct DevChunkItem {
   int32_t tok0, len, kv_len, page0, row0, kvh, tile0, tile1, part;
+  int32_t next;   // the workgroup's next item, or -1; its first is its own index
 };
 // A block of rows whose keys were split: partials part0 .. part0 + nparts - 1.
 struct DevChunkMerge {
@@ -339,7 +340,6 @@ struct ChunkParams {
   void *o;
   float *lse;                  // [Hq][Tq] or null
   const DevChunkItem *items;
-  const int32_t *wg_items;     // workgroup i: items[wg_items[i] .. wg_items[i + 1])
   const DevChunkMerge *merges;
   const int32_t *page_ids;
   float *part_o;               // [partial][256][D], normalised

@@ -391,12 +391,12 @@ constexpr int kChunkRows = 256;     // packed rows of a workgroup
 constexpr int kChunkTile = 64;
 
 struct ChunkPlan {
-  std::vector<DevChunkItem> items;   // workgroup after workgroup, in dispatch order
-  std::vector<int32_t> wg_items;     // its first item, of every workgroup, and the end
+  std::vector<DevChunkItem> items;   // the first ones of the workgroups, in dispatch order, then the others
+  int32_t wgs = 0;
   std::vector<DevChunkMerge> merges;   // the blocks of few rows first
   int32_t parts = 0, max_parts = 1, few = 0;
   int64_t tiles = 0;
-  size_t off_wgs = 0, off_merges = 0, off_pages = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
+  size_t off_merges = 0, off_pages = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -564,21 +564,27 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
     if (few) pl.few = (int32_t)pl.merges.size();
   }
   // Groups in turn, so that workgroup i belongs to group i mod groups.
+  auto item = [&](const ChunkPiece &y, int gr) {
+    const ChunkBlock &x = blocks[y.block];
+    const int32_t tok0 = p->q_offsets[x.b], len = p->q_offsets[x.b + 1] - tok0;
+    const auto &c = cut[y.block];
+    const int32_t part = part0[y.block] < 0 ? -1 : gr * parts + part0[y.block] + (int32_t)(std::lower_bound(c.begin(), c.end(), y.t0) - c.begin());
+    pl.tiles += y.t1 - y.t0;
+    return DevChunkItem{tok0, len, p->kv_lens[x.b], p->page_offsets[x.b], x.row0, x.kvh + gr, y.t0, y.t1, part, -1};
+  };
+  pl.wgs = (int32_t)wgs.size() * groups;
   for (const auto &w : wgs)
+    for (int gr = 0; gr < groups; ++gr) pl.items.push_back(item(w[0], gr));
+  for (size_t i = 0; i < wgs.size(); ++i)
     for (int gr = 0; gr < groups; ++gr) {
-      pl.wg_items.push_back((int32_t)pl.items.size());
-      for (const ChunkPiece &y : w) {
-        const ChunkBlock &x = blocks[y.block];
-        const int32_t tok0 = p->q_offsets[x.b];
-        const int32_t part = part0[y.block] < 0 ? -1 : gr * parts + part0[y.block] +
-            (int32_t)(std::lower_bound(cut[y.block].begin(), cut[y.block].end(), y.t0) - cut[y.block].begin());
-        pl.items.push_back({tok0, p->q_offsets[x.b + 1] - tok0, p->kv_lens[x.b], p->page_offsets[x.b], x.row0, x.kvh + gr, y.t0, y.t1, part});
-        pl.tiles += y.t1 - y.t0;
+      size_t last = i * groups + gr;
+      for (size_t k = 1; k < wgs[i].size(); ++k) {
+        pl.items[last].next = (int32_t)pl.items.size();
+        last = pl.items.size();
+        pl.items.push_back(item(wgs[i][k], gr));
       }
     }
-  pl.wg_items.push_back((int32_t)pl.items.size());
-  pl.off_wgs = align256(pl.items.size() * sizeof(DevChunkItem));
-  pl.off_merges = align256(pl.off_wgs + pl.wg_items.size() * sizeof(int32_t));
+  pl.off_merges = align256(pl.items.size() * sizeof(DevChunkItem));
   pl.off_pages = align256(pl.off_merges + pl.merges.size() * sizeof(DevChunkMerge));
   pl.table_bytes = align256(pl.off_pages + (size_t)p->page_offsets[B] * sizeof(int32_t));
   pl.off_plse = pl.table_bytes;
@@ -659,7 +665,6 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   char *ws = (char *)workspace;
   auto fill = [&](char *h) {
     std::memcpy(h, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
-    std::memcpy(h + pl.off_wgs, pl.wg_items.data(), pl.wg_items.size() * sizeof(int32_t));
     if (!pl.merges.empty()) std::memcpy(h + pl.off_merges, pl.merges.data(), pl.merges.size() * sizeof(DevChunkMerge));
     std::memcpy(h + pl.off_pages, p->page_ids, (size_t)p->page_offsets[p->batch] * sizeof(int32_t));
   };
@@ -681,7 +686,6 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   c.o = o;
   c.lse = lse;
   c.items = (const DevChunkItem *)ws;
-  c.wg_items = (const int32_t *)(ws + pl.off_wgs);
   c.merges = (const DevChunkMerge *)(ws + pl.off_merges);
   c.page_ids = (const int32_t *)(ws + pl.off_pages);
   c.part_lse = (float *)(ws + pl.off_plse);
@@ -691,7 +695,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   c.page_size = p->page_size;
   c.Tq = p->q_offsets[p->batch];
   c.scale_log2 = p->softmax_scale * 1.4426950408889634f;
-  hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, (int)pl.wg_items.size() - 1, stream); });
+  hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, pl.wgs, stream); });
   if (e != hipSuccess) return set_hip_error("chunk launch", e);
   if (!pl.merges.empty()) {
     e = timed_launch("chunk_merge", stream, [&] {
@@ -832,20 +836,18 @@ cas_status_t cas_paged_chunk_plan_destroy(cas_chunk_plan_t *plan) {
   return CAS_OK;
 }
 
-cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items,
-                                       int32_t *wg_items) {
+cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items) {
   if (!plan || !info) return set_error(CAS_ERR_INVALID_ARGUMENT, "plan or info is NULL");
   const ChunkPlan &pl = plan->plan;
   *info = cas_chunk_plan_info_t{};
-  info->workgroups = (int32_t)pl.wg_items.size() - 1;
+  info->workgroups = pl.wgs;
   info->items = (int32_t)pl.items.size();
   info->partials = pl.parts;
   info->max_partials = pl.max_parts;
   info->key_tiles = pl.tiles;
   info->ws_bytes = pl.bytes;
-  static_assert(sizeof(DevChunkItem) == 36, "a table of 32-bit values");
+  static_assert(sizeof(DevChunkItem) == 40, "a table of 32-bit values");
   if (items && !pl.items.empty()) std::memcpy(items, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
-  if (wg_items) std::memcpy(wg_items, pl.wg_items.data(), pl.wg_items.size() * sizeof(int32_t));
   return CAS_OK;
 }
 

@@ -27,15 +27,15 @@ def problem(cas, q, kv, P=16, Hkv=2, g=2, D=64, pages=None):
 def check(cas, q, kv, **kw):
     prob = problem(cas, q, kv, **kw)
     P, Hkv, g = prob.c.page_size, prob.c.num_kv_heads, prob.c.group_size
-    info, items, wgs = cas.chunk_plan(prob)
-    assert len(items) == info.items and sum(i[7] - i[6] for i in items) == info.key_tiles
-    assert len(wgs) == info.workgroups + 1 and (wgs[0], wgs[-1]) == (0, info.items) and all(a < b for a, b in zip(wgs, wgs[1:]))
+    info, wgs = cas.chunk_plan(prob)
+    items = [i for w in wgs for i in w]
+    assert len(wgs) == info.workgroups and len(items) == info.items and sum(i[7] - i[6] for i in items) == info.key_tiles
     seen, parts = {}, {}
     page0 = [0]
     for L in kv:
         page0.append(page0[-1] + -(-L // P))
     first = {sum(q[:b]): b for b in reversed(range(len(q))) if q[b]}
-    for tok0, n, L, pg, row0, kvh, t0, t1, part in items:
+    for tok0, n, L, pg, row0, kvh, t0, t1, part, _ in items:
         b = first[tok0]
         assert (n, L, pg) == (q[b], kv[b], page0[b]) and row0 % ROWS == 0 and row0 < n * g and 0 <= kvh < Hkv
         last = L - n + (min(n * g, row0 + ROWS) - 1) // g      # of the block's rows
@@ -67,8 +67,8 @@ def test_plans(cas):
 
 
 def loads(cas, prob):
-    info, items, wgs = cas.chunk_plan(prob)
-    return info, [sum(i[7] - i[6] for i in items[a:b]) for a, b in zip(wgs, wgs[1:])]
+    info, wgs = cas.chunk_plan(prob)
+    return info, [sum(i[7] - i[6] for i in w) for w in wgs]
 
 
 def test_workgroups_have_equal_shares(cas):
@@ -89,10 +89,10 @@ def test_workgroups_have_equal_shares(cas):
 def test_heads_keep_to_their_xcds(cas):
     """Workgroup i runs on XCD i mod 8."""
     for Hkv in (1, 2, 4, 8, 16):
-        _, items, wgs = cas.chunk_plan(problem(cas, [700, 1, 90], [5000, 3000, 90], Hkv=Hkv, g=4, D=128))
+        _, wgs = cas.chunk_plan(problem(cas, [700, 1, 90], [5000, 3000, 90], Hkv=Hkv, g=4, D=128))
         groups = min(Hkv, 8)
-        for i, (a, b) in enumerate(zip(wgs, wgs[1:])):
-            assert all(x[5] % groups == i % groups for x in items[a:b])
+        for i, w in enumerate(wgs):
+            assert all(x[5] % groups == i % groups for x in w)
 
 
 @pytest.mark.parametrize("q,kv,pages,code", [
