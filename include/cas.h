@@ -502,7 +502,8 @@ cas_status_t cas_paged_append_plan_destroy(cas_append_plan_t *plan);
  * cas_paged_append); requests without new tokens are allowed. That call streams
  * the keys once for every 32 rows (tokens x heads of a group) and is for steps
  * of a few tokens per request; this one takes 256 rows at a time on the matrix
- * cores. Rows of q and o behind the last request's are neither read nor
+ * cores. Requests of one new token next to each other whose pages are shared go
+ * through that call's kernels. Rows of q and o behind the last request's are neither read nor
  * written; lse is [Hq, Tq]. Keys past a query's own position do not reach it,
  * whatever they and their values hold (NaN and infinities included).
  *
@@ -537,6 +538,8 @@ typedef struct {
   int32_t partials;
   int32_t max_partials;   /* most of one block of rows (1: no merge) */
   int64_t key_tiles;      /* 64-key tiles walked by all workgroups */
+  int32_t decode_parts;   /* runs of requests that the decode kernels take, and their new tokens */
+  int32_t decode_tokens;
   size_t ws_bytes;
 } cas_chunk_plan_info_t;
 

@@ -106,7 +106,8 @@ class Append(ctypes.Structure):
 
 class ChunkPlanInfo(ctypes.Structure):
     _fields_ = [("workgroups", ctypes.c_int32), ("items", ctypes.c_int32), ("partials", ctypes.c_int32),
-                ("max_partials", ctypes.c_int32), ("key_tiles", ctypes.c_int64), ("ws_bytes", ctypes.c_size_t)]
+                ("max_partials", ctypes.c_int32), ("key_tiles", ctypes.c_int64), ("decode_parts", ctypes.c_int32),
+                ("decode_tokens", ctypes.c_int32), ("ws_bytes", ctypes.c_size_t)]
 
 
 class PoolConfig(ctypes.Structure):

@@ -1625,9 +1625,11 @@ cas_status_t cas_paged_decode_plan_info(const cas_decode_problem_t *p, cas_decod
   return CAS_OK;
 }
 
+// lse_stride: between heads in lse (0: the query tokens). upload: how the tables
+// reach the workspace (null: through the pinned ring).
 static cas_status_t run_decode(const cas_decode_problem_t *p, const DecodePlan &plan, const void *q, const void *k_pages,
                                const void *v_pages, void *o, float *lse, void *workspace, size_t ws_bytes,
-                               void *hip_stream) {
+                               void *hip_stream, int lse_stride = 0, const TableUpload *upload = nullptr) {
   if (!q || !k_pages || !v_pages || !o) return fail(CAS_ERR_INVALID_ARGUMENT, "q, k_pages, v_pages and o must be non-NULL");
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || ((uintptr_t)lse & 3u))
     return fail(CAS_ERR_ALIGNMENT, "tensors must be 16-byte aligned (lse 4-byte)");
@@ -1638,7 +1640,9 @@ static cas_status_t run_decode(const cas_decode_problem_t *p, const DecodePlan &
   iv.push_back({(uintptr_t)k_pages, (uintptr_t)k_pages + pool, false, 0, "k_pages"});
   iv.push_back({(uintptr_t)v_pages, (uintptr_t)v_pages + pool, false, 0, "v_pages"});
   iv.push_back({(uintptr_t)o, (uintptr_t)o + qbytes, true, 1, "o"});
-  if (lse) iv.push_back({(uintptr_t)lse, (uintptr_t)lse + (uintptr_t)plan.Tq * plan.Hq * 4, true, 2, "lse"});
+  if (lse_stride == 0) lse_stride = plan.Tq;
+  if (lse)
+    iv.push_back({(uintptr_t)lse, (uintptr_t)lse + ((uintptr_t)(plan.Hq - 1) * lse_stride + plan.Tq) * 4, true, 2, "lse"});
   std::string msg;
   if (!overlap_free(iv, msg)) return fail(CAS_ERR_INVALID_ARGUMENT, msg);
   // A workspace for the same lengths that share nothing: neither do these.
@@ -1652,12 +1656,14 @@ static cas_status_t run_decode(const cas_decode_problem_t *p, const DecodePlan &
   hipStream_t stream = (hipStream_t)hip_stream;
   char *ws = (char *)workspace;
   const int npage_ids = p->page_offsets[p->batch];
-  s = ring_upload(dp.off_plse ? dp.off_plse : dp.bytes, workspace, stream, [&](char *h) {
+  const size_t table_bytes = dp.off_plse ? dp.off_plse : dp.bytes;
+  auto fill = [&](char *h) {
     std::memcpy(h, dp.rows.data(), dp.rows.size() * sizeof(DevDecodeRow));
     std::memcpy(h + dp.off_work, dp.work.data(), dp.work.size() * sizeof(DevDecodeWork));
     if (npage_ids) std::memcpy(h + dp.off_pages, p->page_ids, (size_t)npage_ids * sizeof(int32_t));
     std::memcpy(h + dp.off_tokparts, dp.tok_parts.data(), dp.tok_parts.size() * sizeof(int32_t));
-  });
+  };
+  s = upload ? (*upload)(table_bytes, workspace, stream, fill) : ring_upload(table_bytes, workspace, stream, fill);
   if (s != CAS_OK) return s;
   DecodeParams kp{};
   kp.q = q;
@@ -1675,7 +1681,7 @@ static cas_status_t run_decode(const cas_decode_problem_t *p, const DecodePlan &
   kp.Hkv = p->num_kv_heads;
   kp.g = p->group_size;
   kp.page_size = p->page_size;
-  kp.Tq = dp.Tq;
+  kp.Tq = lse_stride;
   kp.scale_log2 = p->softmax_scale * 1.4426950408889634f;
   hipError_t e = timed("decode", stream, [&] { return launch_decode_bf16(kp, p->head_dim, (int)dp.work.size(), dp.row_blocks, stream); });
   if (e != hipSuccess) return hip_fail("decode launch", e);
@@ -1730,6 +1736,26 @@ cas_status_t cas_paged_decode_run(const cas_decode_plan_t *plan, const void *q, 
   if (!plan) return fail(CAS_ERR_INVALID_ARGUMENT, "plan is NULL");
   return run_decode(&plan->p, plan->dp, q, k_pages, v_pages, o, lse, workspace, ws_bytes, hip_stream);
 }
+
+}  // extern "C"
+
+namespace cas {
+
+cas_status_t decode_run_part(const cas_decode_plan_t *plan, const void *q, const void *k_pages, const void *v_pages, void *o,
+                             float *lse, int lse_stride, void *workspace, size_t ws_bytes, const TableUpload &upload,
+                             hipStream_t stream) {
+  return run_decode(&plan->p, plan->dp, q, k_pages, v_pages, o, lse, workspace, ws_bytes, stream, lse_stride, &upload);
+}
+
+void decode_plan_counts(const cas_decode_plan_t *plan, int64_t *key_tiles, int32_t *shared_runs) {
+  *key_tiles = 0;
+  for (const DevDecodeWork &w : plan->dp.work) *key_tiles += w.tile1 - w.tile0;
+  *shared_runs = plan->dp.shared;
+}
+
+}  // namespace cas
+
+extern "C" {
 
 int32_t cas_paged_decode_plan_matches(const cas_decode_plan_t *plan, const cas_decode_problem_t *p) {
   if (!plan || !p || !p->q_offsets || !p->kv_lens || !p->page_offsets || !p->page_ids) return 0;

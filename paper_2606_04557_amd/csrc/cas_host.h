@@ -31,6 +31,17 @@ bool overlap_free(std::vector<Interval> &iv, std::string &msg);
 // CAS_ERR_WORKSPACE (and the size that the call needs) unless ws holds `need` bytes.
 cas_status_t check_workspace(void *ws, size_t have, size_t need);
 
+// Writes launch tables of `bytes` bytes to ws on the stream with fill().
+using TableUpload = std::function<cas_status_t(size_t bytes, void *ws, hipStream_t stream, const std::function<void(char *)> &fill)>;
+
+// cas_paged_decode_run for some of a call's tokens: rows of lse are lse_stride
+// apart (q, o and lse are at the first token's place), and the tables go up by `upload`.
+cas_status_t decode_run_part(const cas_decode_plan_t *plan, const void *q, const void *k_pages, const void *v_pages, void *o,
+                             float *lse, int lse_stride, void *workspace, size_t ws_bytes, const TableUpload &upload,
+                             hipStream_t stream);
+// Key tiles and shared page runs of a plan.
+void decode_plan_counts(const cas_decode_plan_t *plan, int64_t *key_tiles, int32_t *shared_runs);
+
 // launch(), bracketed by timing events while cas_timing_enable is on.
 hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch);
 

@@ -264,8 +264,8 @@ struct DecodeParams {
   const int32_t *tok_parts; // [Tq] partials of each query token's request (merge)
   float *part_o;          // [part][Tq * Hq][D] when a request has several partials
   float *part_lse;        // [part][Tq * Hq]
-  int64_t plane;          // Tq * Hq
-  int32_t Hkv, g, page_size, Tq;
+  int64_t plane;          // query tokens * Hq
+  int32_t Hkv, g, page_size, Tq;   // (Tq: between heads in lse)
   float scale_log2;
 };
 
@@ -390,9 +390,9 @@ hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_gro
 hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_wgs, hipStream_t s);
 // n_merges blocks, of which the first `few` have at most kChunkFewRows rows.
 hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_merges, int max_parts, hipStream_t s);
-// Copies `bytes` (a multiple of 16) of pinned host memory to device memory and
-// then sets *flag (pinned host memory) to value.
-hipError_t launch_table_flag(void *dst, const void *src, size_t bytes, uint32_t *flag, uint32_t value, hipStream_t s);
+// Copies `bytes` (a multiple of 16) of pinned host memory to device memory; when
+// all n_flags flags (pinned host memory) have the value, the source has been read.
+hipError_t launch_table_flags(void *dst, const void *src, size_t bytes, uint32_t *flags, int n_flags, uint32_t value, hipStream_t s);
 hipError_t launch_append(const AppendParams &p, int D, int units, int head_groups, hipStream_t s);
 
 }  // namespace cas

@@ -390,7 +390,16 @@ cas_status_t run_append(const cas_decode_problem_t *p, const cas_rope_t *rope, c
 constexpr int kChunkRows = 256;     // packed rows of a workgroup
 constexpr int kChunkTile = 64;
 
+// Consecutive requests of one new token each whose shared pages the decode kernels
+// stream once for all of them.
+struct DecodePart {
+  std::unique_ptr<cas_decode_plan_t, cas_status_t (*)(cas_decode_plan_t *)> plan{nullptr, cas_paged_decode_plan_destroy};
+  int32_t tok0 = 0, tokens = 0;
+  size_t off = 0, bytes = 0;   // in the workspace
+};
+
 struct ChunkPlan {
+  std::vector<DecodePart> decode;
   std::vector<DevChunkItem> items;   // the first ones of the workgroups, in dispatch order, then the others
   int32_t wgs = 0;
   std::vector<DevChunkMerge> merges;   // the blocks of few rows first
@@ -480,6 +489,53 @@ double fill_bins(const std::vector<ChunkBlock> &blocks, int n_bins, std::vector<
   return *std::max_element(load.begin(), load.end());
 }
 
+// Whether the requests b0 .. b1 - 1 (of one or no new token each) are better off
+// with the decode kernels, which stream a run of pages once for all requests that
+// read it: 32 requests over 8 of 16 cartridges of 1,024 tokens take 52 us there
+// and 163 us here, over 4 of 256 (nothing shared) 122 and 101 us. In us, with
+// launches and merge: 17 + 3.0 ns a 32-key tile there, 15 + 4.5 ns a 64-key tile
+// here, or beside chunks, with which they fill the compute units, 3.8 ns (30
+// requests over 4 of 64 beside two chunks: 177 and 170 us). Half the bytes with
+// d = 64: 1.5, 3.4 and 2.9 ns.
+cas_status_t plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, bool beside_chunks, std::vector<DecodePart> &out,
+                              bool &taken) {
+  taken = false;
+  std::vector<int32_t> qo{0}, kv, po{0}, ids;
+  int64_t tiles = 0;
+  for (int b = b0; b < b1; ++b) {
+    if (p->q_offsets[b + 1] == p->q_offsets[b]) continue;
+    qo.push_back(qo.back() + 1);
+    kv.push_back(p->kv_lens[b]);
+    ids.insert(ids.end(), p->page_ids + p->page_offsets[b], p->page_ids + p->page_offsets[b + 1]);
+    po.push_back((int32_t)ids.size());
+    tiles += ceil_div(p->kv_lens[b], kChunkTile) * p->num_kv_heads;
+  }
+  if (kv.size() < 2) return CAS_OK;
+  cas_decode_problem_t sub = *p;
+  sub.batch = (int32_t)kv.size();
+  sub.q_offsets = qo.data();
+  sub.kv_lens = kv.data();
+  sub.page_offsets = po.data();
+  sub.page_ids = ids.data();
+  cas_decode_plan_t *plan = nullptr;
+  DecodePart part;
+  const cas_status_t s = cas_paged_decode_plan_create(&sub, &plan, &part.bytes);
+  if (s != CAS_OK) return s;
+  part.plan.reset(plan);
+  int64_t decode_tiles = 0;
+  int32_t shared = 0;
+  decode_plan_counts(plan, &decode_tiles, &shared);
+  const bool d64 = p->head_dim == 64;
+  const double there = 17.0 + (d64 ? 1.5e-3 : 3.0e-3) * (double)decode_tiles;
+  const double here = beside_chunks ? (d64 ? 2.9e-3 : 3.8e-3) * (double)tiles : 15.0 + (d64 ? 3.4e-3 : 4.5e-3) * (double)tiles;
+  if (shared == 0 || there > here) return CAS_OK;
+  part.tok0 = p->q_offsets[b0];
+  part.tokens = sub.batch;
+  out.push_back(std::move(part));
+  taken = true;
+  return CAS_OK;
+}
+
 // The launch plan. Either a workgroup per block, longest first, which the
 // hardware hands out as compute units become free; or, where that leaves some
 // idle, one workgroup per compute unit with an equal share, blocks cut along the
@@ -493,6 +549,19 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   if (!std::isfinite(p->softmax_scale) || !(p->softmax_scale > 0.0f))
     return set_error(CAS_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
   const int B = p->batch, g = p->group_size, Hkv = p->num_kv_heads, D = p->head_dim;
+  std::vector<uint8_t> elsewhere(B, 0);   // requests that the decode kernels take
+  bool chunks = false;
+  for (int b = 0; b < B; ++b) chunks |= p->q_offsets[b + 1] - p->q_offsets[b] > 1;
+  for (int b = 0; b < B && g <= 2 * kDecRows;) {
+    int e = b;
+    while (e < B && p->q_offsets[e + 1] - p->q_offsets[e] <= 1) ++e;
+    if (e > b) {
+      bool taken = false;
+      if ((s = plan_decode_part(p, b, e, chunks, pl.decode, taken)) != CAS_OK) return s;
+      std::fill(elsewhere.begin() + b, elsewhere.begin() + e, taken);
+    }
+    b = std::max(e, b + 1);
+  }
   const Topology topo = device_topology();
   const int X = std::max(1, topo.xcds), cus = std::max(X, topo.cus);
   // KV heads kvh with kvh mod groups == i share the XCDs x with x mod groups == i.
@@ -503,7 +572,7 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   for (int h = 0; h < heads; ++h)
     for (int b = 0; b < B; ++b) {
       const int64_t n = p->q_offsets[b + 1] - p->q_offsets[b], nrows = n * g, before = p->kv_lens[b] - n;
-      for (int64_t r = 0; r < nrows; r += kChunkRows) {
+      for (int64_t r = 0; r < nrows && !elsewhere[b]; r += kChunkRows) {
         const int64_t r1 = std::min<int64_t>(nrows, r + kChunkRows);
         const int32_t nt = (int32_t)((before + (r1 - 1) / g) / kChunkTile + 1);   // up to its last query's own key
         blocks.push_back({b, (int32_t)r, (int32_t)(r1 - r), nt, h * groups, tile_cost(D, (int)(r1 - r))});
@@ -590,20 +659,27 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   pl.off_plse = pl.table_bytes;
   pl.off_po = align256(pl.off_plse + (size_t)pl.parts * kChunkRows * 4);
   pl.bytes = align256(pl.off_po + (size_t)pl.parts * kChunkRows * p->head_dim * 4);
+  for (DecodePart &d : pl.decode) {
+    d.off = pl.bytes;
+    pl.bytes = align256(pl.bytes + d.bytes);
+  }
   return CAS_OK;
 }
 
 // Pinned slots for launch tables on their way to a workspace, one ring per
-// device. A slot is free once the kernel that read it has set its flag.
+// device. A slot is free once the kernel that read it has set its flags.
 struct TableRing {
-  static constexpr int kSlots = 16;
+  static constexpr int kSlots = 16, kFlags = 16;
+  static constexpr size_t kFlagBytes = kSlots * kFlags * sizeof(uint32_t);
   char *host = nullptr;              // kSlots slots, then their flags
   size_t slot_bytes = 0;
-  uint32_t want[kSlots] = {};        // value of the slot's flag when it is free
+  uint32_t want[kSlots] = {};        // value of the slot's flags when it is free
+  int used[kSlots] = {};             // flags of the slot's last upload
   int next = 0;
-  uint32_t *flag(int i) const { return (uint32_t *)(host + kSlots * slot_bytes) + i; }
+  uint32_t *flags(int i) const { return (uint32_t *)(host + kSlots * slot_bytes) + i * kFlags; }
   void wait(int i) const {
-    while (__atomic_load_n(flag(i), __ATOMIC_ACQUIRE) != want[i]) std::this_thread::yield();
+    for (int f = 0; f < used[i]; ++f)
+      while (__atomic_load_n(flags(i) + f, __ATOMIC_ACQUIRE) != want[i]) std::this_thread::yield();
   }
 };
 std::mutex g_tables_mu;
@@ -622,30 +698,32 @@ cas_status_t upload_tables(size_t bytes, void *ws, hipStream_t stream, Fill &&fi
     char *host = nullptr;
     // Coherent: the kernel reads slots that the host has just rewritten, and the
     // host the flags that it writes.
-    e = hipHostMalloc((void **)&host, sb * TableRing::kSlots + 256, hipHostMallocCoherent);
+    e = hipHostMalloc((void **)&host, sb * TableRing::kSlots + TableRing::kFlagBytes, hipHostMallocCoherent);
     if (e != hipSuccess) return set_hip_error("hipHostMalloc", e);
     for (int i = 0; r.host && i < TableRing::kSlots; ++i) r.wait(i);
     char *old = r.host;
     r = TableRing{};
     r.host = host;
     r.slot_bytes = sb;
-    std::memset(host + sb * TableRing::kSlots, 0, 256);
+    std::memset(host + sb * TableRing::kSlots, 0, TableRing::kFlagBytes);
     if (old && (e = hipHostFree(old)) != hipSuccess) return set_hip_error("hipHostFree", e);
   }
   const int slot = r.next;
   r.wait(slot);
   char *h = r.host + (size_t)slot * r.slot_bytes;
   fill(h);
-  e = launch_table_flag(ws, h, bytes, r.flag(slot), r.want[slot] + 1, stream);
+  const int n = (int)std::min<size_t>(TableRing::kFlags, (bytes + 4095) / 4096);
+  e = launch_table_flags(ws, h, bytes, r.flags(slot), n, r.want[slot] + 1, stream);
   if (e != hipSuccess) return set_hip_error("table upload launch", e);
   ++r.want[slot];
+  r.used[slot] = n;
   r.next = (slot + 1) % TableRing::kSlots;
   return CAS_OK;
 }
 
 cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const void *q, const void *k_pages, const void *v_pages,
                        void *o, float *lse, void *workspace, size_t ws_bytes, hipStream_t stream) {
-  if (pl.items.empty()) return CAS_OK;
+  if (pl.items.empty() && pl.decode.empty()) return CAS_OK;
   if (!q || !k_pages || !v_pages || !o) return set_error(CAS_ERR_INVALID_ARGUMENT, "q, k_pages, v_pages and o must be non-NULL");
   if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(o) || ((uintptr_t)lse & 3u))
     return set_error(CAS_ERR_ALIGNMENT, "tensors must be 16-byte aligned (lse 4-byte)");
@@ -670,15 +748,23 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   };
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (stream && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
-  if (capture == hipStreamCaptureStatusActive) {
-    // A graph keeps kernel arguments, but not what the pinned ring holds now.
-    std::vector<char> h(pl.table_bytes, 0);
-    fill(h.data());
-    const hipError_t e = launch_table_args_upload(h.data(), pl.table_bytes, workspace, stream);
-    if (e != hipSuccess) return set_hip_error("table upload launch", e);
-  } else if ((s = upload_tables(pl.table_bytes, workspace, stream, fill)) != CAS_OK) {
-    return s;
+  const bool capturing = capture == hipStreamCaptureStatusActive;
+  const TableUpload upload = [&](size_t bytes, void *dst, hipStream_t st, const std::function<void(char *)> &write) {
+    if (!capturing) return upload_tables(bytes, dst, st, write);
+    // A graph keeps kernel arguments, but not what the pinned slots hold now.
+    std::vector<char> h((bytes + 15) & ~(size_t)15, 0);
+    write(h.data());
+    const hipError_t e = launch_table_args_upload(h.data(), h.size(), dst, st);
+    return e == hipSuccess ? CAS_OK : set_hip_error("table upload launch", e);
+  };
+  const int64_t row = (int64_t)p->num_kv_heads * p->group_size * p->head_dim * 2, Tq = p->q_offsets[p->batch];
+  for (const DecodePart &d : pl.decode) {
+    s = decode_run_part(d.plan.get(), (const char *)q + d.tok0 * row, k_pages, v_pages, (char *)o + d.tok0 * row,
+                        lse ? lse + d.tok0 : nullptr, (int)Tq, ws + d.off, d.bytes, upload, stream);
+    if (s != CAS_OK) return s;
   }
+  if (pl.items.empty()) return CAS_OK;
+  if ((s = upload(pl.table_bytes, workspace, stream, fill)) != CAS_OK) return s;
   ChunkParams c{};
   c.q = q;
   c.k_pages = k_pages;
@@ -845,6 +931,8 @@ cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_p
   info->partials = pl.parts;
   info->max_partials = pl.max_parts;
   info->key_tiles = pl.tiles;
+  info->decode_parts = (int32_t)pl.decode.size();
+  for (const DecodePart &d : pl.decode) info->decode_tokens += d.tokens;
   info->ws_bytes = pl.bytes;
   static_assert(sizeof(DevChunkItem) == 40, "a table of 32-bit values");
   if (items && !pl.items.empty()) std::memcpy(items, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));

@@ -32,7 +32,7 @@ def check(cas, q, kv, **kw):
     assert len(wgs) == info.workgroups and len(items) == info.items and sum(i[7] - i[6] for i in items) == info.key_tiles
     seen, parts = {}, {}
     page0 = [0]
-    for L in kv:
+    for L in kv:   # (entries of page_ids)
         page0.append(page0[-1] + -(-L // P))
     first = {sum(q[:b]): b for b in reversed(range(len(q))) if q[b]}
     for tok0, n, L, pg, row0, kvh, t0, t1, part, _ in items:
@@ -43,7 +43,8 @@ def check(cas, q, kv, **kw):
         seen.setdefault((b, row0, kvh), []).append((t0, t1, last // TILE + 1))
         parts.setdefault((b, row0, kvh), []).append(part)
     want = {(b, r, k) for b, n in enumerate(q) for r in range(0, n * g, ROWS) for k in range(Hkv)}
-    assert set(seen) == want
+    gone = {b for b, _, _ in want - set(seen)}                     # requests that the decode kernels take
+    assert set(seen) == {w for w in want if w[0] not in gone} and all(q[b] == 1 for b in gone) and len(gone) == info.decode_tokens
     all_parts = []
     for k, v in seen.items():
         v.sort()
@@ -84,6 +85,30 @@ def test_workgroups_have_equal_shares(cas):
     many, n = loads(cas, problem(cas, [2000] * 16, [4500] * 16, **kw))
     assert many.partials == 0 and many.workgroups == many.items
     assert loads(cas, problem(cas, [1], [64], **kw))[0].partials == 0
+
+
+def test_shared_single_tokens_go_to_the_decode_kernels(cas):
+    """Runs of single-token requests that read the same cartridges, and only those."""
+    kw = dict(Hkv=8, g=4, D=128)
+    carts = [list(range(64 * c, 64 * c + 64)) for c in range(16)]
+    nxt = iter(range(1024, 9999))
+
+    def req(cs, own):
+        return [p for c in cs for p in carts[c]] + [next(nxt) for _ in range(-(-own // 16))], len(cs) * 1024 + own
+
+    shared = [req(range(8), 5 + i) for i in range(20)]
+    alone = [req([], 4000) for _ in range(20)]
+    chunk = [req([0, 1], 300)]
+    def info(reqs, q):
+        return check(cas, q, [L for _, L in reqs], pages=[p for p, _ in reqs], **kw)
+    i = info(shared, [1] * 20)
+    assert (i.decode_parts, i.decode_tokens, i.workgroups) == (1, 20, 0)
+    assert info(alone, [1] * 20).decode_parts == 0
+    i = info(shared[:10] + chunk + shared[10:] + alone, [1] * 10 + [300] + [1, 0] * 5 + [1] * 20)
+    assert i.decode_parts in (1, 2) and 10 <= i.decode_tokens <= 35 and i.workgroups > 0
+    assert info(shared, [2] * 20).decode_parts == 0
+    assert info(shared[:1], [1]).decode_parts == 0
+    assert check(cas, [1] * 20, [L for _, L in shared], pages=[p for p, _ in shared], Hkv=1, g=40, D=64).decode_parts == 0
 
 
 def test_heads_keep_to_their_xcds(cas):

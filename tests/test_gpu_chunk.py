@@ -118,6 +118,43 @@ def test_single_tokens(gpu_lib):
     run(gpu_lib, [1], [5000], 16, 8, 5, 128)
 
 
+@pytest.mark.parametrize("D,Hkv,g", [(128, 4, 4), (64, 8, 3)])
+def test_single_tokens_over_shared_cartridges(gpu_lib, D, Hkv, g):
+    """Runs of decode requests that read the same cartridges, before, between and
+    behind chunks: through the decode kernels, with and without LSE, captured, and
+    with a workspace that holds something else before."""
+    t = _t()
+    share = [[0, 1, 2, 3], [2, 0, 3, 1], [3], [1, 2]] * 4
+    carts = share + [[0, 1]] + share[:9] + [[], [2]] + share[3:] + [[]]
+    counts = [1] * 16 + [150] + [1] * 8 + [0] + [40, 300] + [1] * 13 + [2]
+    kv = [512 * len(c) + 9 + 5 * i + n for i, (c, n) in enumerate(zip(carts, counts))]
+    prob, q, kp, vp, o, lse, pages = run(gpu_lib, counts, kv, 16, Hkv, g, D, carts=carts, cart_pages=32, pad=2)
+    info = gpu_lib.chunk_plan(prob)[0]
+    assert info.decode_parts == 0 or info.decode_tokens >= 8
+    many = [1] * 40
+    mkv = [512 * 4 * 4 + 1 + 3 * i for i in range(40)]
+    prob, q, kp, vp, o, lse, pages = run(gpu_lib, many, mkv, 16, Hkv, g, D, seed=9, carts=[list(range(16))] * 40, cart_pages=32, pad=1)
+    info = gpu_lib.chunk_plan(prob)[0]
+    assert (info.decode_parts, info.decode_tokens, info.workgroups) == (1, 40, 0)
+    ws = t.full((info.ws_bytes,), 255, dtype=t.uint8, device="cuda")
+    a, none = gpu_lib.paged_chunk_fwd(q, kp, vp, prob, need_lse=False, workspace=ws)
+    assert none is None and t.equal(a[:40], o[:40])
+    mixed, mk = [1] * 20 + [70] + [1] * 20, mkv[:20] + [512 * 16 + 70] + mkv[20:]
+    prob, q, kp, vp, o, lse, pages = run(gpu_lib, mixed, mk, 16, Hkv, g, D, seed=11, carts=[list(range(16))] * 41, cart_pages=32)
+    info = gpu_lib.chunk_plan(prob)[0]
+    assert (info.decode_parts, info.decode_tokens) == (2, 40) and info.workgroups > 0
+    o2, lse2 = t.zeros_like(o), t.zeros_like(lse)
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        gpu_lib.paged_chunk_fwd(q, kp, vp, prob, o=o2, lse=lse2)
+    for i in range(3):
+        q.copy_(_rand(q.shape, 1.0, 70 + i))
+        graph.replay()
+        want = gpu_lib.paged_chunk_fwd(q, kp, vp, prob)
+        t.cuda.synchronize()
+        assert t.equal(o2, want[0]) and t.equal(lse2, want[1])
+
+
 def test_shared_cartridges_and_a_long_chunk(gpu_lib):
     run(gpu_lib, [700, 1, 33, 300], [700 + 1024 + 60, 512 + 5, 1024 + 512 + 33, 300], 32, 2, 4, 128, seed=3,
         carts=[[2, 0], [1], [0, 1, 2], []], cart_pages=16)
