@@ -175,6 +175,11 @@ def test_rope_in_a_graph_and_on_a_stream(gpu_lib):
     z, = gpu_lib.rope_fwd([x], pos, rope, stream=s)
     s.synchronize()
     check(z, x, np.arange(40), rope, "bf16")
+    # (a rope that is dropped at once, on another stream than its own)
+    outs = [gpu_lib.rope_fwd([x], pos, gpu_lib.Rope(128, 1e6 + i), stream=s)[0] for i in range(8)]
+    s.synchronize()
+    for i, z in enumerate(outs):
+        check(z, x, np.arange(40), gpu_lib.Rope(128, 1e6 + i), "bf16")
     g = t.cuda.CUDAGraph()
     with t.cuda.graph(g):
         gpu_lib.rope_fwd([x], pos, rope, outs=[y])
@@ -265,6 +270,11 @@ def test_append_variants(gpu_lib):
     A([700, 1], [700, 20], 16, 1, 1, 64, 64, "half", 6, pages=[list(range(43, -1, -1)), [50, 44]])
     A([1] * 300, [17 + i for i in range(300)], 32, 2, 1, 64, 32, "interleaved", 7)       # more requests than one launch holds
     A([9] * 260, [9 + i for i in range(260)], 16, 2, 1, 128, 128, "half", 8)
+    for D, P in ((64, 16), (128, 32), (64, 128)):
+        # sixteen tokens to a workgroup, that begin and end inside pages; one request over several launches
+        A([700, 3, 341, 1], [707, 40, 341 + 11, 5], P, 2, 3, D, 32, "half", 9 + D)
+        A([300, 5], [309, 7], P, 1, 2, D, 16, "interleaved", 10 + D, pad=1)
+    A([12000, 5, 9000], [12003, 5, 9000 + 29], 16, 1, 1, 64, 64, "half", 11)
 
 
 def test_append_past_4_gib(gpu_lib):
