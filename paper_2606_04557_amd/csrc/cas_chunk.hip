@@ -7,8 +7,8 @@
 // and a workgroup of eight waves takes 256 of them, 32 per wave, over a range of
 // 64-key tiles, with the phases of the prefix forward: the two waves of a SIMD
 // take turns, one in a matrix phase (O += V^T P of the tile before, S = K Q^T of
-// this one) while the other is in its softmax phase (cas_bf16.hip has the
-// schedule). Here the tiles are gathered page by page, and the second pass for
+// this one) while the other is in its softmax phase (cas_bf16.hip). Here the tiles
+// are gathered page by page, each group copies its share, and the second pass for
 // rows that the fixed softmax reference does not fit is a plain loop. A workgroup
 // works through a list of items (blocks of rows, or pieces of their keys), which
 // the host makes equally long for all compute units.
@@ -65,7 +65,7 @@ void chunk_bf16_kernel(ChunkParams) {
   constexpr int NSTEP = D / 16, DT = D / 32;
   constexpr int TB = kKT * D * 2;
   constexpr int CPR = D / 8, RPI = 64 / CPR;   // 16-byte chunks of a key row, key rows of a copy instruction
-  constexpr int PER = kKT / RPI / 4;           // copy instructions of a tile for each of group B's four waves
+  constexpr int PER = kKT / RPI / 4;           // copy instructions of a K or V tile for each of a group's four waves
   __shared__ __attribute__((aligned(1024))) char kb0[TB];
   __shared__ __attribute__((aligned(1024))) char kb1[TB];
   __shared__ __attribute__((aligned(1024))) char kb2[TB];
@@ -89,8 +89,6 @@ void chunk_bf16_kernel(ChunkParams) {
     ro.init(n, G);
     TrOffsets<D> to;
     to.init(lane);
-    const int page_shift = __builtin_ctz(p.page_size), row_elems = Hkv * D;
-    const int lane_off = (lane / CPR) * row_elems * 2 + (((lane % CPR) ^ swz<D>(w4 * RPI + lane / CPR)) << 4);
     const DevChunkItem it = load_const(p.items, at);
     const int nrows = it.len * g;
     const int row0 = it.row0 + wave * kFastRowsPerWave, my_row = row0 + n;
@@ -101,41 +99,45 @@ void chunk_bf16_kernel(ChunkParams) {
     const int my_t = my_row / g;
     const int nt = it.tile1 - it.tile0;
 
-    // Copies. Instruction i of wave w4 moves key rows r0 .. r0 + RPI - 1 of a tile,
-    // r0 = RPI (w4 + 4 i), which lie in one page (pages are multiples of 16 rows).
-    // It has a resource of its own, which ends behind the request's last key: later
-    // rows read as zero, and are masked. Rows 16 apart share their swizzle, so one
-    // lane offset serves every instruction.
+    // Copies: group A's waves copy the K tiles, group B's the V tiles. Instruction
+    // i of wave w4 moves key rows r0 .. r0 + RPI - 1 of a tile, r0 = RPI (w4 + 4 i),
+    // which lie in one granule of 16 rows, and a granule in one page. It has a
+    // resource of its own, which ends behind the request's last key: later rows
+    // read as zero, and are masked. (With the scalar work of looking up pages and
+    // of one group copying both, 215 instructions beside the 120 of the softmax
+    // phase, a tile took 1.94 us.) Rows 16 apart share their swizzle, so one lane
+    // offset serves every instruction.
     static_assert(4 * RPI % 16 == 0, "the swizzle of a wave's rows is the same for every instruction");
+    const int row_bytes = Hkv * D * 2;
+    const int lane_off = (lane / CPR) * row_bytes + (((lane % CPR) ^ swz<D>(w4 * RPI + lane / CPR)) << 4);
+    const uint64_t pool = (uint64_t)(grp == 0 ? p.k_pages : p.v_pages) + it.kvh * (D * 2) + (w4 * RPI % 16) * row_bytes;
+    const int full = (RPI - 1) * row_bytes + D * 2;   // bytes of an instruction's rows
     struct Tile {
-      int key0;        // first key of the wave's first instruction
-      int page[PER];
+      uint32_t at[PER];   // its granules, from the pool's start on, in 2 KiB
     };
     auto tile_at = [&](int j) __attribute__((always_inline)) {
       Tile t;
-      t.key0 = (it.tile0 + j) * kKT + w4 * RPI;
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-        t.page[i] = load_const(p.page_ids, it.page0 + (min(t.key0 + 4 * RPI * i, it.kv_len - 1) >> page_shift));
+        t.at[i] = load_const(p.granules, it.granule0 + 4 * (it.tile0 + j) + (w4 * RPI) / 16 + i * (4 * RPI / 16));
       return t;
     };
-    auto copy = [&](char *buf, const void *pool, const Tile &t, bool has, int i) __attribute__((always_inline)) {
-      const int key = t.key0 + 4 * RPI * i;
-      const int64_t row = ((int64_t)t.page[i] << page_shift) + (key & ((1 << page_shift) - 1));
-      const int valid = has ? min(RPI, it.kv_len - key) : 0;
-      dma16(make_rsrc((const __bf16 *)pool + row * row_elems + it.kvh * D, valid > 0 ? ((valid - 1) * row_elems + D) * 2 : 0),
-            lane_off, buf + (w4 + 4 * i) * 1024);
+    // Bytes of tile j's rows from the wave's first one on, up to the last key (none past the last tile).
+    auto bytes_left = [&](int j) __attribute__((always_inline)) {
+      return j < nt ? min(it.kv_len - (it.tile0 + j) * kKT - w4 * RPI, kKT) * row_bytes - (row_bytes - D * 2) : 0;
     };
-    // On their way together: the first K tile, the queries, then the first V and
-    // the second K.
-    Tile tk, tn;   // of the K copied last, whose V is copied next, and of the next K
-    if (grp == 1) {
-      wait_vmcnt<0>();   // (the item before's stores: the partial counts below are of copies alone)
-      tk = tile_at(0);
-      tn = tile_at(min(1, nt - 1));
+    auto copy = [&](char *buf, const Tile &t, int left, int i) __attribute__((always_inline)) {
+      dma16(make_rsrc((const void *)(pool + ((uint64_t)t.at[i] << 11)), min(max(left - i * 4 * RPI * row_bytes, 0), full)), lane_off,
+            buf + (w4 + 4 * i) * 1024);
+    };
+    auto copy_tile = [&](char *buf, const Tile &t, int j) __attribute__((always_inline)) {
+      const int left = bytes_left(j);
 #pragma unroll
-      for (int i = 0; i < PER; ++i) copy(kb0, p.k_pages, tk, true, i);
-    }
+      for (int i = 0; i < PER; ++i) copy(buf, t, left, i);
+    };
+    // On their way together: the first K tile, the queries, the second K and the first V.
+    wait_vmcnt<0>();   // (the item before's stores: the partial counts below are of copies alone)
+    if (grp == 0) copy_tile(kb0, tile_at(0), 0);
     bf16x8 qf[NSTEP];
     if (my_row < nrows) {
       const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + it.kvh * g + (my_row - my_t * g)) * D;
@@ -145,22 +147,15 @@ void chunk_bf16_kernel(ChunkParams) {
 #pragma unroll
       for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
     }
-    if (grp == 1) {
-#pragma unroll
-      for (int i = 0; i < PER; ++i) copy(vb0, p.v_pages, tk, true, i);
-#pragma unroll
-      for (int i = 0; i < PER; ++i) copy(kb1, p.k_pages, tn, nt > 1, i);
-      tk = tn;
-      tn = tile_at(min(2, nt - 1));
-      wait_vmcnt<2 * PER>();   // the first K and the queries
-    } else {
-      wait_vmcnt<0>();
-    }
+    if (grp == 0) copy_tile(kb1, tile_at(min(1, nt - 1)), 1);
+    else copy_tile(vb0, tile_at(0), 0);
+    Tile next = tile_at(min(grp == 0 ? 2 : 1, nt - 1));   // of the tile copied next (granules, a tile ahead of their use)
+    wait_vmcnt<PER>();   // the first K and the queries
 
     f32x16 oacc[DT];
     float m_run = -INFINITY, l_run = 0.0f;   // exponent offset of this lane's row, row sum of its keys
     auto live = [&](int j) __attribute__((always_inline)) { return wave_active && (it.tile0 + j) * kKT <= last_hi; };
-    constexpr int kPieces = 2 * PER;         // copy instructions of a softmax phase
+    constexpr int kPieces = PER;             // copy instructions of a softmax phase
     static_assert(16 % kPieces == 0, "copies spread over the 16 exponential pairs");
 
     {
@@ -206,47 +201,47 @@ void chunk_bf16_kernel(ChunkParams) {
         if (key0 + kKT - 1 > last_lo) softmax(std::true_type{}, before + my_t - key0, piece);
         else softmax(std::false_type{}, kKT - 1, piece);
       };
-      auto no_piece = [](int) {};
-      auto even_b = [&](int i, char *kbn, char *vbn) __attribute__((always_inline)) {
-        const Tile tv = tk, tc = tn;
-        tn = tile_at(min(i + 3, nt - 1));   // (page ids, a tile ahead of their use)
-        const bool has_v = i + 1 < nt, has_k = i + 2 < nt;
-        xphase(i - 1, [&](int n) __attribute__((always_inline)) {
-          if (n < PER) copy(vbn, p.v_pages, tv, has_v, n);
-          else copy(kbn, p.k_pages, tc, has_k, n - PER);
-        });
-        tk = tc;
-        wait_vmcnt<2 * PER>();
+      // The softmax of tile j, with the copies of this group's tile jc spread over
+      // it; at its end the copies of the phase before are waited for.
+      auto xcopy = [&](int j, int jc, char *buf) __attribute__((always_inline)) {
+        const Tile t = next;
+        next = tile_at(min(jc + 1, nt - 1));
+        const int left = bytes_left(jc);
+        xphase(j, [&](int n) __attribute__((always_inline)) { copy(buf, t, left, n); });
+        wait_vmcnt<PER>();
       };
 
       // (At least one tile: the host lists no empty range.) G_0 multiplies V
       // buffer 2 by P = 0: clear it so no stale bit pattern (a NaN) can reach O.
       for (int i = tid; i < TB / 16; i += kFastThreads) reinterpret_cast<uint4 *>(vb2)[i] = uint4{0, 0, 0, 0};
       lds_barrier();
-      // Six phases per iteration (three tiles), so every buffer is a fixed LDS
-      // address: G_i reads K_i from kb[i%3] and V_{i-1} from vb[(i-1)%3]; the
-      // copies of phase 2i go to kb[(i+2)%3] and vb[(i+1)%3].
+      // Phase 2i: G_i beside X_{i-1}, phase 2i+1: X_i beside G_i. G_i reads K_i from
+      // kb[i%3] and V_{i-1} from vb[(i-1)%3]. V_{i+1} is copied in phase 2i, to where
+      // V_{i-2} was read until phase 2i-1, and waited for in phase 2i+2; K_{i+2} in
+      // phase 2i+1, to where K_{i-1} was read until phase 2i-1, and waited for in
+      // phase 2i+3. Six phases per iteration (three tiles), so every buffer is a
+      // fixed LDS address.
       auto run = [&](auto GROUP_A) __attribute__((always_inline)) {
         constexpr bool A = decltype(GROUP_A)::value;
-        auto even = [&](int i, const char *kbi, const char *vbp, char *kbn, char *vbn) __attribute__((always_inline)) {
+        auto even = [&](int i, const char *kbi, const char *vbp, char *vbn) __attribute__((always_inline)) {
           if constexpr (A) gphase(i, kbi, vbp);
-          else even_b(i, kbn, vbn);
+          else xcopy(i - 1, i + 1, vbn);
           lds_barrier();
         };
-        auto odd = [&](int i, const char *kbi, const char *vbp) __attribute__((always_inline)) {
-          if constexpr (A) xphase(i, no_piece);
+        auto odd = [&](int i, const char *kbi, const char *vbp, char *kbn) __attribute__((always_inline)) {
+          if constexpr (A) xcopy(i, i + 2, kbn);
           else gphase(i, kbi, vbp);
           lds_barrier();
         };
         for (int i = 0; i <= nt; i += 3) {
-          even(i, kb0, vb2, kb2, vb1);
-          odd(i, kb0, vb2);
+          even(i, kb0, vb2, vb1);
+          odd(i, kb0, vb2, kb2);
           if (i + 1 > nt) break;
-          even(i + 1, kb1, vb0, kb0, vb2);
-          odd(i + 1, kb1, vb0);
+          even(i + 1, kb1, vb0, vb2);
+          odd(i + 1, kb1, vb0, kb0);
           if (i + 2 > nt) break;
-          even(i + 2, kb2, vb1, kb1, vb0);
-          odd(i + 2, kb2, vb1);
+          even(i + 2, kb2, vb1, vb0);
+          odd(i + 2, kb2, vb1, kb1);
         }
       };
       if (grp == 0) run(std::true_type{});
@@ -271,15 +266,8 @@ void chunk_bf16_kernel(ChunkParams) {
 #pragma unroll 1
       for (int j = 0; j < nt; ++j) {
         lds_barrier();   // every wave is done with the tile before
-        if (grp == 1) {
-          const Tile t = tile_at(j);
-#pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            copy(kb0, p.k_pages, t, true, i);
-            copy(vb0, p.v_pages, t, true, i);
-          }
-          wait_vmcnt<0>();
-        }
+        copy_tile(grp == 0 ? kb0 : vb0, tile_at(j), j);
+        wait_vmcnt<0>();
         lds_barrier();
         if (!live(j)) continue;
         const int key0 = (it.tile0 + j) * kKT, lim = before + my_t - key0;

@@ -322,10 +322,10 @@ static_assert(sizeof(AppendParams) <= 4096, "kernel arguments");
 // Chunk attention over pages. One item: up to 256 packed rows from row0 on
 // (row r of a request is its token r / g, head r % g of the KV head's group) of
 // a request with `len` new tokens from tok0 on, its last of kv_len keys, in the
-// pages page_ids[page0 ..], over 64-key tiles [tile0, tile1). part: which
+// granules granules[granule0 ..], over 64-key tiles [tile0, tile1). part: which
 // partial it writes, or -1: no other item has these rows.
 struct DevChunkItem {
-  int32_t tok0, len, kv_len, page0, row0, kvh, tile0, tile1, part;
+  int32_t tok0, len, kv_len, granule0, row0, kvh, tile0, tile1, part;
   int32_t next;   // the workgroup's next item, or -1; its first is its own index
 };
 // A block of rows whose keys were split: partials part0 .. part0 + nparts - 1.
@@ -341,10 +341,10 @@ struct ChunkParams {
   float *lse;                  // [Hq][Tq] or null
   const DevChunkItem *items;
   const DevChunkMerge *merges;
-  const int32_t *page_ids;
+  const uint32_t *granules;    // 16 key rows of a request each: where they are in the pools, in 2 KiB (4 per tile)
   float *part_o;               // [partial][256][D], normalised
   float *part_lse;             // [partial][256]
-  int32_t Hkv, g, page_size, Tq;
+  int32_t Hkv, g, Tq;
   float scale_log2;
 };
 

@@ -402,10 +402,11 @@ struct ChunkPlan {
   std::vector<DecodePart> decode;
   std::vector<DevChunkItem> items;   // the first ones of the workgroups, in dispatch order, then the others
   int32_t wgs = 0;
+  std::vector<uint32_t> granules;
   std::vector<DevChunkMerge> merges;   // the blocks of few rows first
   int32_t parts = 0, max_parts = 1, few = 0;
   int64_t tiles = 0;
-  size_t off_merges = 0, off_pages = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
+  size_t off_merges = 0, off_granules = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -548,6 +549,8 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   if (s != CAS_OK) return s;
   if (!std::isfinite(p->softmax_scale) || !(p->softmax_scale > 0.0f))
     return set_error(CAS_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
+  const int64_t granule = (int64_t)16 * p->num_kv_heads * p->head_dim * 2 / 2048;   // in 2 KiB
+  if (p->num_pages > (int64_t)UINT32_MAX / (granule * (p->page_size / 16))) return set_error(CAS_ERR_UNSUPPORTED, "page pool above 8 TiB");
   const int B = p->batch, g = p->group_size, Hkv = p->num_kv_heads, D = p->head_dim;
   std::vector<uint8_t> elsewhere(B, 0);   // requests that the decode kernels take
   bool chunks = false;
@@ -632,6 +635,17 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
       }
     if (few) pl.few = (int32_t)pl.merges.size();
   }
+  // The granules of the requests, whole tiles of them.
+  std::vector<int32_t> granule0(B, 0);
+  const int per_page = p->page_size / 16;
+  for (int b = 0; b < B; ++b) {
+    if (p->q_offsets[b + 1] == p->q_offsets[b] || elsewhere[b]) continue;
+    if (pl.granules.size() > (size_t)INT32_MAX / 2) return set_error(CAS_ERR_UNSUPPORTED, "too many pages");
+    granule0[b] = (int32_t)pl.granules.size();
+    for (int32_t e = p->page_offsets[b]; e < p->page_offsets[b + 1]; ++e)
+      for (int j = 0; j < per_page; ++j) pl.granules.push_back((uint32_t)(((int64_t)p->page_ids[e] * per_page + j) * granule));
+    pl.granules.resize((pl.granules.size() + 3) & ~(size_t)3, 0);
+  }
   // Groups in turn, so that workgroup i belongs to group i mod groups.
   auto item = [&](const ChunkPiece &y, int gr) {
     const ChunkBlock &x = blocks[y.block];
@@ -639,7 +653,7 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
     const auto &c = cut[y.block];
     const int32_t part = part0[y.block] < 0 ? -1 : gr * parts + part0[y.block] + (int32_t)(std::lower_bound(c.begin(), c.end(), y.t0) - c.begin());
     pl.tiles += y.t1 - y.t0;
-    return DevChunkItem{tok0, len, p->kv_lens[x.b], p->page_offsets[x.b], x.row0, x.kvh + gr, y.t0, y.t1, part, -1};
+    return DevChunkItem{tok0, len, p->kv_lens[x.b], granule0[x.b], x.row0, x.kvh + gr, y.t0, y.t1, part, -1};
   };
   pl.wgs = (int32_t)wgs.size() * groups;
   for (const auto &w : wgs)
@@ -654,8 +668,8 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
       }
     }
   pl.off_merges = align256(pl.items.size() * sizeof(DevChunkItem));
-  pl.off_pages = align256(pl.off_merges + pl.merges.size() * sizeof(DevChunkMerge));
-  pl.table_bytes = align256(pl.off_pages + (size_t)p->page_offsets[B] * sizeof(int32_t));
+  pl.off_granules = align256(pl.off_merges + pl.merges.size() * sizeof(DevChunkMerge));
+  pl.table_bytes = align256(pl.off_granules + pl.granules.size() * sizeof(uint32_t));
   pl.off_plse = pl.table_bytes;
   pl.off_po = align256(pl.off_plse + (size_t)pl.parts * kChunkRows * 4);
   pl.bytes = align256(pl.off_po + (size_t)pl.parts * kChunkRows * p->head_dim * 4);
@@ -744,7 +758,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   auto fill = [&](char *h) {
     std::memcpy(h, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
     if (!pl.merges.empty()) std::memcpy(h + pl.off_merges, pl.merges.data(), pl.merges.size() * sizeof(DevChunkMerge));
-    std::memcpy(h + pl.off_pages, p->page_ids, (size_t)p->page_offsets[p->batch] * sizeof(int32_t));
+    std::memcpy(h + pl.off_granules, pl.granules.data(), pl.granules.size() * sizeof(uint32_t));
   };
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (stream && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
@@ -773,12 +787,11 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   c.lse = lse;
   c.items = (const DevChunkItem *)ws;
   c.merges = (const DevChunkMerge *)(ws + pl.off_merges);
-  c.page_ids = (const int32_t *)(ws + pl.off_pages);
+  c.granules = (const uint32_t *)(ws + pl.off_granules);
   c.part_lse = (float *)(ws + pl.off_plse);
   c.part_o = (float *)(ws + pl.off_po);
   c.Hkv = p->num_kv_heads;
   c.g = p->group_size;
-  c.page_size = p->page_size;
   c.Tq = p->q_offsets[p->batch];
   c.scale_log2 = p->softmax_scale * 1.4426950408889634f;
   hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, pl.wgs, stream); });

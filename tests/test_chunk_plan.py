@@ -31,13 +31,15 @@ def check(cas, q, kv, **kw):
     items = [i for w in wgs for i in w]
     assert len(wgs) == info.workgroups and len(items) == info.items and sum(i[7] - i[6] for i in items) == info.key_tiles
     seen, parts = {}, {}
-    page0 = [0]
-    for L in kv:   # (entries of page_ids)
-        page0.append(page0[-1] + -(-L // P))
+    granule0, at = {}, 0
+    listed = {i[0] for i in items}
+    for b, L in enumerate(kv):
+        if q[b] and sum(q[:b]) in listed:
+            granule0[b], at = at, at + -(-(-(-L // P) * (P // 16)) // 4) * 4
     first = {sum(q[:b]): b for b in reversed(range(len(q))) if q[b]}
     for tok0, n, L, pg, row0, kvh, t0, t1, part, _ in items:
         b = first[tok0]
-        assert (n, L, pg) == (q[b], kv[b], page0[b]) and row0 % ROWS == 0 and row0 < n * g and 0 <= kvh < Hkv
+        assert (n, L, pg) == (q[b], kv[b], granule0[b]) and row0 % ROWS == 0 and row0 < n * g and 0 <= kvh < Hkv
         last = L - n + (min(n * g, row0 + ROWS) - 1) // g      # of the block's rows
         assert 0 <= t0 < t1 <= last // TILE + 1
         seen.setdefault((b, row0, kvh), []).append((t0, t1, last // TILE + 1))
