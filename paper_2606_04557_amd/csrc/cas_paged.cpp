@@ -411,13 +411,14 @@ struct ChunkPlan {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Costs, in 64-key tiles of 256 rows with d = 128 (1.94 us). A tile of few rows
-// costs more than its share (a phase waits for its copies and barriers): 1.14 us
-// for 32 rows, 1.38 for 128; with d = 64 0.88 to 1.30 us. kWgCost: what a
+// Costs, in 64-key tiles of 256 rows with d = 128 (1.79 us). A tile of few rows
+// costs more than its share (a phase waits for its copies and barriers): 1.06 us
+// for 32 rows, 1.27 for 128; with d = 64 0.80, 0.86 and 1.30 us. kWgCost: what a
 // workgroup costs beside its tiles (dispatch, first loads, pipeline fill and
 // drain, epilogue), kItemCost: a further item of a workgroup; kMergeCost: a
-// merge's launch; the partials' bytes, written and read, at kBytesPerTile.
-double tile_cost(int D, int rows) { return D == 128 ? 0.57 + 0.43 * rows / 256 : 0.45 + 0.22 * rows / 256; }
+// merge's launch; the partials' bytes, written and read, at kBytesPerTile. (Over
+// 30 mixes, each of them 20-50 % higher or lower changes the time by 1 %.)
+double tile_cost(int D, int rows) { return D == 128 ? 0.57 + 0.43 * rows / 256 : 0.42 + 0.30 * rows / 256; }
 constexpr double kWgCost = 5.0, kItemCost = 3.0, kMergeCost = 3.0, kBytesPerTile = 5e6;
 constexpr double kWorthIt = 0.97;   // of the cost without cuts: below it, blocks are cut
 constexpr int kMinPiece = 2;        // tiles
@@ -494,10 +495,10 @@ double fill_bins(const std::vector<ChunkBlock> &blocks, int n_bins, std::vector<
 // with the decode kernels, which stream a run of pages once for all requests that
 // read it: 32 requests over 8 of 16 cartridges of 1,024 tokens take 52 us there
 // and 163 us here, over 4 of 256 (nothing shared) 122 and 101 us. In us, with
-// launches and merge: 17 + 3.0 ns a 32-key tile there, 15 + 4.5 ns a 64-key tile
-// here, or beside chunks, with which they fill the compute units, 3.8 ns (30
+// launches and merge: 17 + 3.0 ns a 32-key tile there, 15 + 4.2 ns a 64-key tile
+// here, or beside chunks, with which they fill the compute units, 3.6 ns (30
 // requests over 4 of 64 beside two chunks: 177 and 170 us). Half the bytes with
-// d = 64: 1.5, 3.4 and 2.9 ns.
+// d = 64: 1.5, 3.1 and 2.7 ns.
 cas_status_t plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, bool beside_chunks, std::vector<DecodePart> &out,
                               bool &taken) {
   taken = false;
@@ -528,7 +529,7 @@ cas_status_t plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, boo
   decode_plan_counts(plan, &decode_tiles, &shared);
   const bool d64 = p->head_dim == 64;
   const double there = 17.0 + (d64 ? 1.5e-3 : 3.0e-3) * (double)decode_tiles;
-  const double here = beside_chunks ? (d64 ? 2.9e-3 : 3.8e-3) * (double)tiles : 15.0 + (d64 ? 3.4e-3 : 4.5e-3) * (double)tiles;
+  const double here = beside_chunks ? (d64 ? 2.7e-3 : 3.6e-3) * (double)tiles : 15.0 + (d64 ? 3.1e-3 : 4.2e-3) * (double)tiles;
   if (shared == 0 || there > here) return CAS_OK;
   part.tok0 = p->q_offsets[b0];
   part.tokens = sub.batch;
