@@ -269,15 +269,15 @@ struct DecodeParams {
   float scale_log2;
 };
 
-// Rotary positions of up to four tensors of the same tokens. Workgroup (x, y,
-// z) takes tokens 256 / (head_dim / 16) / slots each from tensor z, heads y *
-// slots + i, and from there every gridDim.y * slots.
+// Rotary positions of up to four tensors of the same tokens. Workgroup (x, z)
+// takes 256 / (head_dim / 16) / slots tokens of tensor z, its threads heads i,
+// i + slots, ... of one.
 struct DevRopeTensor {
   const void *x;
   void *y;
   int64_t x_tok, x_head, y_tok, y_head;   // strides in elements
   int32_t heads;
-  int32_t pad_;
+  int32_t slots;            // heads of a token that threads take at a time, a power of two
 };
 struct DevRope {
   const double *turns;
@@ -291,7 +291,6 @@ struct RopeParams {
   DevRopeTensor t[4];
   const int32_t *positions;
   int64_t tokens;
-  int32_t slots;            // threads' heads of one token at a time, a power of two
 };
 
 // Appending to the paged cache. A workgroup (of each tensor and head group)
@@ -386,7 +385,7 @@ hipError_t launch_bwd_prologue_bf16(const PreParams &p, int D, hipStream_t s);
 hipError_t launch_adam_bf16(const AdamParams &p, int D, int n_chunks, hipStream_t s);
 hipError_t launch_decode_bf16(const DecodeParams &p, int D, int n_work, int row_blocks, hipStream_t s);
 hipError_t launch_decode_merge_bf16(const DecodeParams &p, int D, int max_split, hipStream_t s);
-hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_groups, hipStream_t s);
+hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, hipStream_t s);
 hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_wgs, hipStream_t s);
 // n_merges blocks, of which the first `few` have at most kChunkFewRows rows.
 hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_merges, int max_parts, hipStream_t s);

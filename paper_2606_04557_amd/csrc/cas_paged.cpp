@@ -90,7 +90,7 @@ bool apart(const Footprint &a, const Footprint &b) {
 }
 
 constexpr int64_t kMaxStride = (int64_t)1 << 31;   // (with the limits on tokens and heads, spans fit 64 bits)
-constexpr int64_t kMaxRopeTokens = (int64_t)1 << 26;
+constexpr int64_t kMaxRopeTokens = (int64_t)1 << 24;   // (two or more to a workgroup of 256: under 2^32 threads)
 
 cas_status_t check_strides(const char *what, int64_t st, int64_t sh, int es) {
   if (st < 0 || sh < 0 || st > kMaxStride || sh > kMaxStride)
@@ -99,24 +99,28 @@ cas_status_t check_strides(const char *what, int64_t st, int64_t sh, int es) {
   return CAS_OK;
 }
 
-// Heads of one token that the threads of a workgroup take at a time. The
-// angles of a token are computed once for every thread that works on it, so few
-// slots save arithmetic and many spread a few tokens over more threads.
-int head_slots(int64_t tokens, int D, int heads) {
-  const int all = 256 / (D / 16);
-  int slots = tokens >= 1024 ? 8 : all;
+// Heads of one token that the threads of a workgroup take at a time, no more
+// than its tensor has (rounded up). Every thread computes its angles, so few
+// slots save arithmetic and many spread a few tokens over more threads. us with
+// 32 / 16 / 8 / 4 slots, 32 query and 8 key heads of 128 in one call: bf16 2.7 /
+// 3.0 / 3.1 / 3.9 at 64 tokens, 3.4 / 3.3 / 3.4 / 4.1 at 256, 4.5 / 4.3 / 3.7 / 5.2
+// at 512, 38.3 / 34.4 / 32.9 / 33.7 at 8192; fp32, whose threads have twice the
+// bytes for their angles, 3.1 / 3.4 / 3.9 / 5.2, 4.5 / 4.3 / 5.4 / 7.0, 6.8 / 6.7 /
+// 7.0 / 7.9 and 61.4 / 61.6 / 64.3 / 68.2.
+int head_slots(int64_t tokens, int D, int es, int heads) {
+  int slots = tokens < 512 ? 256 / (D / 16) : 4 * es;
   while (slots > 1 && slots / 2 >= heads) slots /= 2;
   return slots;
 }
 
-cas_status_t rope_call(const cas_rope_t *rope, cas_dtype_t dtype, int32_t D, int64_t tokens, const int32_t *positions,
+cas_status_t rope_call(const cas_rope_t *rope, int32_t dtype, int32_t D, int64_t tokens, const int32_t *positions,
                        const cas_rope_tensor_t *ts, int32_t n, int32_t inverse, hipStream_t stream) {
   if (dtype != CAS_DTYPE_BF16 && dtype != CAS_DTYPE_FP32) return set_error(CAS_ERR_UNSUPPORTED, "dtype must be bf16 or fp32");
   if (D != 64 && D != 128) return set_error(CAS_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
   cas_status_t s = check_rope(rope, D);
   if (s != CAS_OK) return s;
   if (tokens < 0) return set_error(CAS_ERR_INVALID_ARGUMENT, "tokens must be >= 0");
-  if (tokens > kMaxRopeTokens) return set_error(CAS_ERR_UNSUPPORTED, "more than 2^26 tokens");
+  if (tokens > kMaxRopeTokens) return set_error(CAS_ERR_UNSUPPORTED, "more than 2^24 tokens");
   if (n < 1 || n > 4 || !ts) return set_error(CAS_ERR_INVALID_ARGUMENT, "1 to 4 tensors");
   if (tokens == 0) return CAS_OK;
   if (!positions) return set_error(CAS_ERR_INVALID_ARGUMENT, "positions is NULL");
@@ -124,7 +128,6 @@ cas_status_t rope_call(const cas_rope_t *rope, cas_dtype_t dtype, int32_t D, int
   const int es = dtype == CAS_DTYPE_BF16 ? 2 : 4;
   RopeParams p{};
   Footprint in[4], out[4];
-  int heads = 1;
   for (int i = 0; i < n; ++i) {
     const cas_rope_tensor_t &t = ts[i];
     auto refuse = [&](cas_status_t code, const char *why) { return set_error(code, "tensor " + str(i) + ": " + why); };
@@ -136,8 +139,8 @@ cas_status_t rope_call(const cas_rope_t *rope, cas_dtype_t dtype, int32_t D, int
     in[i] = footprint(t.x, tokens, t.heads, t.x_stride_tok, t.x_stride_head, D, es);
     out[i] = footprint(t.y, tokens, t.heads, t.y_stride_tok, t.y_stride_head, D, es);
     if (!out[i].distinct) return refuse(CAS_ERR_INVALID_ARGUMENT, "y overlaps itself");
-    p.t[i] = DevRopeTensor{t.x, t.y, t.x_stride_tok, t.x_stride_head, t.y_stride_tok, t.y_stride_head, t.heads, 0};
-    heads = std::max(heads, t.heads);
+    p.t[i] = DevRopeTensor{t.x, t.y, t.x_stride_tok, t.x_stride_head, t.y_stride_tok, t.y_stride_head, t.heads,
+                            head_slots(tokens, D, es, t.heads)};
   }
   const Footprint pos{(uintptr_t)positions, (uintptr_t)positions + (uintptr_t)tokens * 4, 0, (uint64_t)tokens * 4, true};
   const Footprint turns{(uintptr_t)rope->turns, (uintptr_t)rope->turns + (uintptr_t)rope->rotary_dim * 4, 0,
@@ -157,8 +160,7 @@ cas_status_t rope_call(const cas_rope_t *rope, cas_dtype_t dtype, int32_t D, int
   p.rope = dev_rope(rope, inverse != 0);
   p.positions = positions;
   p.tokens = tokens;
-  p.slots = head_slots(tokens, D, heads);
-  const hipError_t e = timed_launch("rope", stream, [&] { return launch_rope(p, dtype == CAS_DTYPE_BF16 ? kBF16 : kFP32, D, n, 1, stream); });
+  const hipError_t e = timed_launch("rope", stream, [&] { return launch_rope(p, dtype == CAS_DTYPE_BF16 ? kBF16 : kFP32, D, n, stream); });
   return e == hipSuccess ? CAS_OK : set_hip_error("rope launch", e);
 }
 
@@ -499,9 +501,7 @@ double fill_bins(const std::vector<ChunkBlock> &blocks, int n_bins, std::vector<
 // here, or beside chunks, with which they fill the compute units, 3.6 ns (30
 // requests over 4 of 64 beside two chunks: 177 and 170 us). Half the bytes with
 // d = 64: 1.5, 3.1 and 2.7 ns.
-cas_status_t plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, bool beside_chunks, std::vector<DecodePart> &out,
-                              bool &taken) {
-  taken = false;
+bool plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, bool beside_chunks, std::vector<DecodePart> &out) {
   std::vector<int32_t> qo{0}, kv, po{0}, ids;
   int64_t tiles = 0;
   for (int b = b0; b < b1; ++b) {
@@ -512,7 +512,7 @@ cas_status_t plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, boo
     po.push_back((int32_t)ids.size());
     tiles += ceil_div(p->kv_lens[b], kChunkTile) * p->num_kv_heads;
   }
-  if (kv.size() < 2) return CAS_OK;
+  if (kv.size() < 2) return false;
   cas_decode_problem_t sub = *p;
   sub.batch = (int32_t)kv.size();
   sub.q_offsets = qo.data();
@@ -521,8 +521,7 @@ cas_status_t plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, boo
   sub.page_ids = ids.data();
   cas_decode_plan_t *plan = nullptr;
   DecodePart part;
-  const cas_status_t s = cas_paged_decode_plan_create(&sub, &plan, &part.bytes);
-  if (s != CAS_OK) return s;
+  if (cas_paged_decode_plan_create(&sub, &plan, &part.bytes) != CAS_OK) return false;   // (too large for those kernels)
   part.plan.reset(plan);
   int64_t decode_tiles = 0;
   int32_t shared = 0;
@@ -530,12 +529,11 @@ cas_status_t plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, boo
   const bool d64 = p->head_dim == 64;
   const double there = 17.0 + (d64 ? 1.5e-3 : 3.0e-3) * (double)decode_tiles;
   const double here = beside_chunks ? (d64 ? 2.7e-3 : 3.6e-3) * (double)tiles : 15.0 + (d64 ? 3.1e-3 : 4.2e-3) * (double)tiles;
-  if (shared == 0 || there > here) return CAS_OK;
+  if (shared == 0 || there > here) return false;
   part.tok0 = p->q_offsets[b0];
   part.tokens = sub.batch;
   out.push_back(std::move(part));
-  taken = true;
-  return CAS_OK;
+  return true;
 }
 
 // The launch plan. Either a workgroup per block, longest first, which the
@@ -559,11 +557,7 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   for (int b = 0; b < B && g <= 2 * kDecRows;) {
     int e = b;
     while (e < B && p->q_offsets[e + 1] - p->q_offsets[e] <= 1) ++e;
-    if (e > b) {
-      bool taken = false;
-      if ((s = plan_decode_part(p, b, e, chunks, pl.decode, taken)) != CAS_OK) return s;
-      std::fill(elsewhere.begin() + b, elsewhere.begin() + e, taken);
-    }
+    if (e > b && plan_decode_part(p, b, e, chunks, pl.decode)) std::fill(elsewhere.begin() + b, elsewhere.begin() + e, 1);
     b = std::max(e, b + 1);
   }
   const Topology topo = device_topology();
@@ -845,7 +839,7 @@ cas_status_t cas_rope_frequencies(int32_t rotary_dim, double base, int32_t scali
   return CAS_OK;
 }
 
-cas_status_t cas_rope(const cas_rope_t *rope, cas_dtype_t dtype, int32_t head_dim, int64_t tokens, const int32_t *positions,
+cas_status_t cas_rope(const cas_rope_t *rope, int32_t dtype, int32_t head_dim, int64_t tokens, const int32_t *positions,
                       const cas_rope_tensor_t *tensors, int32_t n, int32_t inverse, void *hip_stream) {
   return guarded([&] { return rope_call(rope, dtype, head_dim, tokens, positions, tensors, n, inverse, (hipStream_t)hip_stream); });
 }

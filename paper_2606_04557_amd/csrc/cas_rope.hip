@@ -11,6 +11,8 @@
 //
 // Bound by HBM: an element is read once and written once, and the angles cost
 // about 30 operations for each pair and thread.
+#include <algorithm>
+
 #include "cas_device.h"
 
 namespace cas {
@@ -132,12 +134,12 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams p) {
   constexpr int U = D / 16;
   const int u = threadIdx.x % U, w = threadIdx.x / U;
   const DevRopeTensor t = p.t[blockIdx.z];
-  const int64_t tok = (int64_t)blockIdx.x * (kRopeThreads / U / p.slots) + w / p.slots;
-  const int h0 = blockIdx.y * p.slots + w % p.slots;
+  const int64_t tok = (int64_t)blockIdx.x * (kRopeThreads / U / t.slots) + w / t.slots;
+  const int h0 = w % t.slots;
   if (tok >= p.tokens || h0 >= t.heads) return;
   RopeUnit<T, IL> r;
   r.init(p.rope, u, p.positions[tok]);
-  r.heads((const T *)t.x + tok * t.x_tok, t.x_head, (T *)t.y + tok * t.y_tok, t.y_head, h0, gridDim.y * p.slots, t.heads);
+  r.heads((const T *)t.x + tok * t.x_tok, t.x_head, (T *)t.y + tok * t.y_tok, t.y_head, h0, t.slots, t.heads);
 }
 
 // z: 0 the keys, 1 the values, 2 the queries.
@@ -189,9 +191,11 @@ void launch_append_t(const AppendParams &p, dim3 grid, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, int head_groups, hipStream_t s) {
-  const int64_t per_wg = kRopeThreads / (D / 16) / p.slots;
-  const dim3 grid((unsigned)((p.tokens + per_wg - 1) / per_wg), (unsigned)head_groups, (unsigned)n);
+hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, hipStream_t s) {
+  int slots = 1;   // (the grid is as wide as the tensor with the most workgroups needs)
+  for (int i = 0; i < n; ++i) slots = std::max(slots, p.t[i].slots);
+  const int64_t per_wg = kRopeThreads / (D / 16) / slots;
+  const dim3 grid((unsigned)((p.tokens + per_wg - 1) / per_wg), 1, (unsigned)n);
   if (dt == kBF16) {
     if (D == 64) launch_rope_t<__bf16, 64>(p, grid, s);
     else launch_rope_t<__bf16, 128>(p, grid, s);

@@ -141,7 +141,7 @@ def rope_call(cas, L, tokens=10, D=128, dtype=0, positions=A, n=1, inverse=0, ro
 
 
 @pytest.mark.parametrize("kw,code", [
-    (dict(dtype=2), UNSUPPORTED), (dict(D=96), UNSUPPORTED), (dict(tokens=-1), INVALID), (dict(tokens=(1 << 26) + 1), UNSUPPORTED),
+    (dict(dtype=2), UNSUPPORTED), (dict(D=96), UNSUPPORTED), (dict(tokens=-1), INVALID), (dict(tokens=(1 << 24) + 1), UNSUPPORTED),
     (dict(n=0), INVALID), (dict(n=5), INVALID), (dict(positions=None), INVALID), (dict(positions=A + 2), ALIGN),
     (dict(rope=dict(layout=2)), INVALID), (dict(rope=dict(rotary_dim=8)), UNSUPPORTED), (dict(rope=dict(rotary_dim=40)), UNSUPPORTED),
     (dict(rope=dict(rotary_dim=144)), UNSUPPORTED), (dict(rope=dict(turns=None)), INVALID), (dict(rope=dict(turns=A + 4)), ALIGN),
