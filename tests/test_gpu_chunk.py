@@ -285,6 +285,60 @@ def test_pages_past_4_gib(gpu_lib):
     compare(o, lse, q, kp, vp, [140], [300], pages, 0.09, 1)
 
 
+@pytest.mark.parametrize("seed", range(24))
+def test_random_problems(gpu_lib, seed):
+    """Seeded problems: head layouts, page sizes, cartridges in common, ragged
+    chunks, single tokens and empty requests in any order."""
+    r = np.random.default_rng(5000 + seed)
+    P, D = int(r.choice([16, 32, 64, 128])), int(r.choice([64, 128]))
+    Hkv, g, B = int(r.choice([1, 2, 3, 4, 6, 8])), int(r.choice([1, 2, 3, 4, 5, 7, 8])), int(r.integers(1, 14))
+    cart_pages = int(r.integers(1, 700 // P + 2))
+    carts, counts, kv = [], [], []
+    for _ in range(B):
+        c = r.permutation(5)[: int(r.integers(0, 5))].tolist()
+        n = int(r.choice([0, 1, 1, 1, int(r.integers(2, 40)), int(r.integers(40, 500))]))
+        own = n + int(r.choice([0, int(r.integers(0, 70)), int(r.integers(0, 900))]))
+        carts.append(c)
+        counts.append(n)
+        kv.append(len(c) * cart_pages * P + own)
+    if not sum(counts):
+        counts[0], kv[0] = 1, kv[0] + 1
+    run(gpu_lib, counts, kv, P, Hkv, g, D, seed=seed, carts=carts, cart_pages=cart_pages, pad=int(r.integers(0, 3)))
+
+
+def test_host_threads(gpu_lib):
+    """Four threads with a stream each: attention on one shared problem, and
+    appending to pools of their own."""
+    import threading
+    t = _t()
+    prob, q, kp, vp, o, lse, pages = run(gpu_lib, [300, 1, 40], [2000, 900, 777], 16, 2, 4, 128)
+    rope = gpu_lib.Rope(128, 1e4)
+    aprob = gpu_lib.DecodeProblem([3, 1], [20, 33], [[0, 1], [2, 3, 4]], 5, 16, 2, 4, 128, 0.1)
+    x = _rand((4, 2, 128), 1.0, 5)
+    pools = [[t.zeros((5, 16, 2, 128), dtype=t.bfloat16, device="cuda") for _ in range(2)] for _ in range(5)]
+    gpu_lib.paged_append(x, x, *pools[4], aprob, rope=rope)
+    t.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        try:
+            s = t.cuda.Stream()
+            for _ in range(20):
+                a, b = gpu_lib.paged_chunk_fwd(q, kp, vp, prob, stream=s)
+                gpu_lib.paged_append(x, x, *pools[i], aprob, rope=rope, stream=s)
+                s.synchronize()
+                if not (t.equal(a, o) and t.equal(b, lse) and t.equal(pools[i][0], pools[4][0])):
+                    bad.append(i)
+        except Exception as e:   # noqa: BLE001
+            bad.append(e)
+    ths = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for th in ths:
+        th.start()
+    for th in ths:
+        th.join()
+    assert not bad
+
+
 def test_serving_steps(gpu_lib):
     """Prompts prefilled in two chunks, then decoded token by token, positions and
     cache through paged_append: every step's attention against the whole
