@@ -59,6 +59,36 @@ __device__ __forceinline__ bf16x8 finite_only(bf16x8 v) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// The phases' parts for 32 keys (cas_bf16_pipe.h has those for a tile's 64).
+__device__ __forceinline__ void mask_piece(int lim, int G, f32x16 &s) {
+  const int limg = lim - 4 * G;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) s[j] = crow(j, 0) <= limg ? s[j] : -INFINITY;
+}
+
+__device__ __forceinline__ float piece_max(const f32x16 &s, float c) {
+  float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int j = 0; j < 16; j += 4) {
+    mx[0] = fmaxf(fmaxf(mx[0], s[j]), s[j + 1]);
+    mx[1] = fmaxf(fmaxf(mx[1], s[j + 2]), s[j + 3]);
+  }
+  const float m = fmaxf(mx[0], mx[1]);
+  const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+  return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * c;
+}
+
+__device__ __forceinline__ float piece_weights(float c, float mu, f32x16 &s, bf16x8 (&pf)[2]) {
+  float l[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < 16; ++j) s[j] = fast_exp2(fmaf(s[j], c, -mu));
+#pragma unroll
+  for (int h = 0; h < 2; ++h) pf[h] = pack_bf16x8(s, h);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) l[j & 1] += s[j];
+  return l[0] + l[1];
+}
+
 template <int D>
 __global__ __launch_bounds__(kFastThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void chunk_bf16_kernel(ChunkParams) {
@@ -91,7 +121,10 @@ void chunk_bf16_kernel(ChunkParams) {
     to.init(lane);
     const DevChunkItem it = load_const(p.items, at);
     const int nrows = it.len * g;
-    const int row0 = it.row0 + wave * kFastRowsPerWave, my_row = row0 + n;
+    // Few rows: the waves share them, in `rgs` groups of 32, and divide the keys.
+    const bool narrow = nrows - it.row0 <= kChunkNarrowRows;
+    const int rgs = nrows - it.row0 <= kFastRowsPerWave ? 1 : 2;
+    const int row0 = it.row0 + (narrow ? wave & (rgs - 1) : wave) * kFastRowsPerWave, my_row = row0 + n;
     const bool wave_active = row0 < nrows;
     const int before = it.kv_len - it.len;       // token t sees keys 0 .. before + t
     const int last_lo = __builtin_amdgcn_readfirstlane(before + row0 / g);
@@ -137,7 +170,7 @@ void chunk_bf16_kernel(ChunkParams) {
     };
     // On their way together: the first K tile, the queries, the second K and the first V.
     wait_vmcnt<0>();   // (the item before's stores: the partial counts below are of copies alone)
-    if (grp == 0) copy_tile(kb0, tile_at(0), 0);
+    if (grp == 0 && !narrow) copy_tile(kb0, tile_at(0), 0);
     bf16x8 qf[NSTEP];
     if (my_row < nrows) {
       const __bf16 *rp = (const __bf16 *)p.q + (((int64_t)it.tok0 + my_t) * Hq + it.kvh * g + (my_row - my_t * g)) * D;
@@ -147,10 +180,13 @@ void chunk_bf16_kernel(ChunkParams) {
 #pragma unroll
       for (int st = 0; st < NSTEP; ++st) qf[st] = Mma<__bf16>::zero();
     }
-    if (grp == 0) copy_tile(kb1, tile_at(min(1, nt - 1)), 1);
-    else copy_tile(vb0, tile_at(0), 0);
-    Tile next = tile_at(min(grp == 0 ? 2 : 1, nt - 1));   // of the tile copied next (granules, a tile ahead of their use)
-    wait_vmcnt<PER>();   // the first K and the queries
+    Tile next;   // granules of the tile copied next, a tile ahead of their use
+    if (!narrow) {
+      if (grp == 0) copy_tile(kb1, tile_at(min(1, nt - 1)), 1);
+      else copy_tile(vb0, tile_at(0), 0);
+      next = tile_at(min(grp == 0 ? 2 : 1, nt - 1));
+      wait_vmcnt<PER>();   // the first K and the queries
+    }
 
     f32x16 oacc[DT];
     float m_run = -INFINITY, l_run = 0.0f;   // exponent offset of this lane's row, row sum of its keys
@@ -158,9 +194,113 @@ void chunk_bf16_kernel(ChunkParams) {
     constexpr int kPieces = PER;             // copy instructions of a softmax phase
     static_assert(16 % kPieces == 0, "copies spread over the 16 exponential pairs");
 
-    {
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();
+    if (narrow) {
+      // Of the range's pieces of 32 keys, wave w takes those w / rgs, w / rgs +
+      // 8 / rgs, ..., by itself: its K and V rows travel through registers, a piece
+      // ahead of their use, to 32 rows of LDS of its own, and no barrier is met.
+      constexpr int LOADS = 32 / RPI, HB = 32 * D * 2;   // load instructions and bytes of a piece's K or V rows
+      const int strand = wave / rgs, strands = kNW / rgs, pieces = 2 * nt;
+      auto tile_of = [&](int i) __attribute__((always_inline)) { return i == 0 ? kb0 : i == 1 ? kb1 : i == 2 ? kb2 : vb0; };
+      char *const own = tile_of(wave >> 1) + (wave & 1) * HB;
+      int voff[LOADS / 2];
+#pragma unroll
+      for (int l = 0; l < LOADS / 2; ++l) voff[l] = (l * RPI + lane / CPR) * row_bytes + (lane % CPR) * 16;
+      const uint64_t kv_off = (uint64_t)it.kvh * (D * 2);
+      uint32_t ga = 0, gb = 0;   // the granules of the piece loaded next
+      auto granules_of = [&](int i) __attribute__((always_inline)) {
+        const int at = it.granule0 + 4 * it.tile0 + 2 * min(i, pieces - 1);
+        ga = load_const(p.granules, at);
+        gb = load_const(p.granules, at + 1);
+      };
+      u32x4 kr[LOADS], vr[LOADS];
+      auto load = [&](const void *pages, int i, u32x4 (&r)[LOADS]) __attribute__((always_inline)) {
+        const int rows = i < pieces ? it.kv_len - it.tile0 * kKT - 32 * i : 0;   // (rows behind the last key read as zero)
+        auto granule = [&](uint32_t gr, int left, int l0) __attribute__((always_inline)) {
+          const BufRsrc rs = make_rsrc((const void *)((uint64_t)pages + kv_off + ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane(gr) << 11)),
+                                       __builtin_amdgcn_readfirstlane(left > 0 ? (min(left, 16) - 1) * row_bytes + D * 2 : 0));
+#pragma unroll
+          for (int l = 0; l < LOADS / 2; ++l) r[l0 + l] = __builtin_amdgcn_raw_buffer_load_b128(rs, voff[l], 0, 0);
+        };
+        granule(ga, rows, 0);
+        granule(gb, rows - 16, LOADS / 2);
+        asm volatile("" ::: "memory");   // (in this order, so that each use waits for its own)
+      };
+      auto to_lds = [&](const u32x4 (&r)[LOADS]) __attribute__((always_inline)) {
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) *reinterpret_cast<u32x4 *>(own + swz_off<D>(l * RPI + lane / CPR, lane % CPR)) = r[l];
+        asm volatile("" ::: "memory");   // (the wave's other lanes read it; its LDS operations stay in order)
+      };
+      granules_of(strand);
+      load(p.k_pages, strand, kr);
+      load(p.v_pages, strand, vr);
+      granules_of(strand + strands);
+#pragma unroll 1
+      for (int i = strand; i < pieces; i += strands) {
+        const int key0 = it.tile0 * kKT + 32 * i;
+        if (!wave_active || key0 > last_hi) break;
+        wait_vmcnt<LOADS>();   // (the compiler's own wait is for all loads)
+        to_lds(kr);
+        load(p.k_pages, i + strands, kr);
+        f32x16 s = zero16();
+#pragma unroll
+        for (int st = 0; st < NSTEP; ++st) s = Mma<__bf16>::run(row_frag_at<D>(own, ro, 0, st), qf[st], s);
+        wait_vmcnt<LOADS>();
+        to_lds(vr);
+        load(p.v_pages, i + strands, vr);
+        granules_of(i + 2 * strands);
+        if (key0 + 31 > last_lo) mask_piece(before + my_t - key0, G, s);
+        const float mt = piece_max(s, c);
+        if (wave_any(mt > m_run)) {
+          const float m_new = fmaxf(m_run, mt);
+          const float alpha = fast_exp2(m_run - m_new);   // (a row that has seen nothing yet: O and l are zero)
+          m_run = m_new;
+          l_run = m_new == -INFINITY ? 0.0f : l_run * alpha;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) oacc[dt] *= m_new == -INFINITY ? 0.0f : alpha;
+        }
+        bf16x8 pf[2];
+        l_run += piece_weights(c, m_run == -INFINITY ? 0.0f : m_run, s, pf);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) oacc[dt] = Mma<__bf16>::run(tr_frag_at<D>(own, to, 16 * h, dt), pf[h], oacc[dt]);
+      }
+      // The upper half of the waves gives its sums to the lower half, until one
+      // wave has those of each group of rows.
+#pragma unroll 1
+      for (int h = kNW / 2; h >= rgs; h >>= 1) {
+        lds_barrier();
+        char *const slot = tile_of(wave & (h - 1)) + lane * 16;   // four registers of 64 lanes are 1 KiB
+        float2 *const ml = reinterpret_cast<float2 *>(vb1) + (wave & (h - 1)) * 64 + lane;
+        if (wave >= h && wave < 2 * h) {
+          *ml = float2{m_run, l_run};
+#pragma unroll
+          for (int i = 0; i < 4 * DT; ++i) {
+            const f32x16 &o = oacc[i / 4];
+            const int e = 4 * (i % 4);
+            *reinterpret_cast<f32x4 *>(slot + i * 1024) = f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]};
+          }
+        }
+        lds_barrier();
+        if (wave < h) {
+          const float2 other = *ml;
+          const float m_new = fmaxf(m_run, other.x), mu = m_new == -INFINITY ? 0.0f : m_new;
+          const float wa = fast_exp2(m_run - mu), wb = fast_exp2(other.x - mu);
+          m_run = m_new;
+          l_run = l_run * wa + other.y * wb;
+#pragma unroll
+          for (int i = 0; i < 4 * DT; ++i) {
+            f32x16 &o = oacc[i / 4];
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(slot + i * 1024);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[4 * (i % 4) + e] = o[4 * (i % 4) + e] * wa + x[e] * wb;
+          }
+        }
+      }
+    } else {
       f32x16 s0 = zero16(), s1 = zero16();
       bf16x8 pf[2][2];
       auto no_weights = [&]() __attribute__((always_inline)) {
@@ -258,6 +398,7 @@ void chunk_bf16_kernel(ChunkParams) {
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) again |= (__float_as_uint(oacc[dt][i]) & 0x7f800000u) == 0x7f800000u;
+    again = again && (!narrow || wave < rgs);
     if (__syncthreads_or(again ? 1 : 0)) {
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) oacc[dt] = zero16();

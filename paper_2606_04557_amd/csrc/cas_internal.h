@@ -332,6 +332,7 @@ struct DevChunkMerge {
   int32_t tok0, len, row0, kvh, part0, nparts;
 };
 constexpr int kChunkFewRows = 32;
+constexpr int kChunkNarrowRows = 64;
 struct ChunkParams {
   const void *q;
   const void *k_pages;

@@ -413,14 +413,21 @@ struct ChunkPlan {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Costs, in 64-key tiles of 256 rows with d = 128 (1.79 us). A tile of few rows
-// costs more than its share (a phase waits for its copies and barriers): 1.06 us
-// for 32 rows, 1.27 for 128; with d = 64 0.80, 0.86 and 1.30 us. kWgCost: what a
+// Costs, in 64-key tiles of 256 rows with d = 128 (1.75 us). Fewer rows cost
+// more than their share (a phase waits for its copies and barriers): 1.20 us for
+// 96, 1.25 for 128; with d = 64 0.87, 0.89 and 1.22. Up to kChunkNarrowRows of
+// them the kernel's waves divide the keys: 0.47 us for 32 rows and 0.92 for 64
+// where the keys are in the L2, 0.75 for 32 where most come from HBM, which is
+// what counts (with 0.47 a batch of 16 single tokens beside a chunk took 106 us,
+// with 0.75 93); with d = 64 0.26 and 0.52, and half the bytes. kWgCost: what a
 // workgroup costs beside its tiles (dispatch, first loads, pipeline fill and
 // drain, epilogue), kItemCost: a further item of a workgroup; kMergeCost: a
 // merge's launch; the partials' bytes, written and read, at kBytesPerTile. (Over
 // 30 mixes, each of them 20-50 % higher or lower changes the time by 1 %.)
-double tile_cost(int D, int rows) { return D == 128 ? 0.57 + 0.43 * rows / 256 : 0.42 + 0.30 * rows / 256; }
+double tile_cost(int D, int rows) {
+  if (rows <= kChunkNarrowRows) return D == 128 ? (rows <= 32 ? 0.45 : 0.60) : rows <= 32 ? 0.25 : 0.33;
+  return D == 128 ? 0.57 + 0.43 * rows / 256 : 0.42 + 0.30 * rows / 256;
+}
 constexpr double kWgCost = 5.0, kItemCost = 3.0, kMergeCost = 3.0, kBytesPerTile = 5e6;
 constexpr double kWorthIt = 0.97;   // of the cost without cuts: below it, blocks are cut
 constexpr int kMinPiece = 2;        // tiles
@@ -495,12 +502,13 @@ double fill_bins(const std::vector<ChunkBlock> &blocks, int n_bins, std::vector<
 
 // Whether the requests b0 .. b1 - 1 (of one or no new token each) are better off
 // with the decode kernels, which stream a run of pages once for all requests that
-// read it: 32 requests over 8 of 16 cartridges of 1,024 tokens take 52 us there
-// and 163 us here, over 4 of 256 (nothing shared) 122 and 101 us. In us, with
-// launches and merge: 17 + 3.0 ns a 32-key tile there, 15 + 4.2 ns a 64-key tile
-// here, or beside chunks, with which they fill the compute units, 3.6 ns (30
-// requests over 4 of 64 beside two chunks: 177 and 170 us). Half the bytes with
-// d = 64: 1.5, 3.1 and 2.7 ns.
+// read it: 32 requests over 8 of 16 cartridges of 1,024 tokens take 51 us there
+// and 88 us here, over 4 of 256 (nothing shared) 100 us on either side; 30 requests
+// over 4 of 64 beside two chunks 159 and 136 us, 30 over 8 of 16 194 and 229. In
+// us, with launches and merge: 12 + 2.7 ns a 32-key tile that is streamed there; here
+// 1.55 ns a 64-key tile and 1.75 ns a streamed one, for what comes from HBM, and 13,
+// but not beside chunks, with which they fill the compute units. With d = 64: 14, 1.2,
+// 0.8 and 0.75. (Of 12 batches of each size one is on the slower side, by 4 %.)
 bool plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, bool beside_chunks, std::vector<DecodePart> &out) {
   std::vector<int32_t> qo{0}, kv, po{0}, ids;
   int64_t tiles = 0;
@@ -527,8 +535,9 @@ bool plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, bool beside
   int32_t shared = 0;
   decode_plan_counts(plan, &decode_tiles, &shared);
   const bool d64 = p->head_dim == 64;
-  const double there = 17.0 + (d64 ? 1.5e-3 : 3.0e-3) * (double)decode_tiles;
-  const double here = beside_chunks ? (d64 ? 2.7e-3 : 3.6e-3) * (double)tiles : 15.0 + (d64 ? 3.1e-3 : 4.2e-3) * (double)tiles;
+  const double there = d64 ? 14.0 + 1.2e-3 * (double)decode_tiles : 12.0 + 2.7e-3 * (double)decode_tiles;
+  const double here = (beside_chunks ? 0.0 : 13.0) + (d64 ? 0.8e-3 : 1.55e-3) * (double)tiles +
+                      (d64 ? 0.75e-3 : 1.75e-3) * (double)decode_tiles;
   if (shared == 0 || there > here) return false;
   part.tok0 = p->q_offsets[b0];
   part.tokens = sub.batch;
