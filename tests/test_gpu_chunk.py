@@ -213,6 +213,54 @@ def test_values_past_a_query_do_not_reach_it(gpu_lib, D):
     assert t.isfinite(o[:70]).all() and t.isfinite(o[:, 2:]).all() and t.isfinite(lse[:, :70]).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("P,Hkv,g", [(16, 2, 1), (32, 1, 4), (128, 3, 5)])
+def test_few_rows(gpu_lib, P, Hkv, g, D):
+    """Blocks of 1 to 65 rows, which divide the keys among the waves up to 64:
+    fewer keys than waves, ends inside a tile's halves, pieces of long ones."""
+    for rows in (1, 31, 32, 33, 63, 64, 65):
+        n = max(1, rows // g)
+        counts = [n, 1, n, n, n + 1, n]
+        kv = [n, 33, n + 31, n + 64, n + 257, 6000]
+        run(gpu_lib, counts, kv, P, Hkv, g, D, seed=rows)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [12, 28])
+def test_few_rows_rising_and_not_finite(gpu_lib, n, D):
+    """24 and 56 rows: scores 40 to 170 above those before them, in keys of every
+    wave; NaN and infinities in keys and values of a new token reach the queries
+    from it on and no other."""
+    t = _t()
+    L = 700 + n
+    pages, npages = tables([n], [L], 16, 5)
+    at = lambda key: (pages[0][key // 16], key % 16)
+    prob = gpu_lib.DecodeProblem([n], [L], pages, npages, 16, 1, 2, D, 1.0)
+    q = t.full((n, 2, D), 0.25, dtype=t.bfloat16, device="cuda")
+    kp, vp = _rand((npages, 16, 1, D), 0.05, 6), _rand((npages, 16, 1, D), 1.0, 7)
+    for key, score in ((100, 40.0), (350, 150.0), (600, 160.0), (705, 170.0)):
+        kp[at(key)] = score * 4 / D
+    o, lse = gpu_lib.paged_chunk_fwd(q, kp, vp, prob)
+    compare(o, lse, q, kp, vp, [n], [L], pages, 1.0, 2)
+    kp = _rand((npages, 16, 1, D), 0.7, 6)
+    q = _rand((n, 2, D), 1.0, 8)
+    prob = gpu_lib.DecodeProblem([n], [L], pages, npages, 16, 1, 2, D, 0.1)
+    bad = 7
+    before = [bad], [700 + bad]   # the queries ahead of it, as a request of their own
+    for value in ("nan", "inf", "-inf"):
+        v2, k2 = vp.clone(), kp.clone()
+        v2[at(700 + bad)][0, 3] = float(value)
+        k2[at(700 + bad)][0, 2] = float(value)
+        o, lse = gpu_lib.paged_chunk_fwd(q, kp, v2, prob)
+        compare(o[:bad], lse[:, :bad], q[:bad], kp, vp, *before, pages, 0.1, 2)
+        assert (t.isnan(o[bad:, :, 3]) if value == "nan" else o[bad:, :, 3] == float(value)).all()
+        assert t.isfinite(o[:, :, [c for c in range(D) if c != 3]]).all()
+        o, lse = gpu_lib.paged_chunk_fwd(q, k2, vp, prob)
+        compare(o[:bad], lse[:, :bad], q[:bad], kp, vp, *before, pages, 0.1, 2)
+        if value == "nan":
+            assert t.isnan(o[bad:]).all() and t.isnan(lse[:, bad:]).all()
+
+
 def test_agrees_with_decode_and_repeats(gpu_lib):
     """The same problem through paged_decode_fwd (both within half a step of the
     weights and of the result), and the same bits on a second call."""
