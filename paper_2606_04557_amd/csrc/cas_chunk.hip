@@ -556,10 +556,18 @@ hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_wgs, hipStream_t
   return hipGetLastError();
 }
 
-// Eight groups a row where each takes two partials or more (few rows, then), else two.
+// Groups a row: eight where each takes two partials or more (few rows, then), one
+// where there are few partials but many rows (15.5 us with two and 12.3 with one for
+// 16 requests' 15 MB in up to 3 partials; 7.0 and 7.5 for 132 rows in 9).
 hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_merges, int max_parts, hipStream_t s) {
-  if (D == 64) max_parts >= 16 ? launch_chunk_merge_t<64, 8>(p, few, n_merges, s) : launch_chunk_merge_t<64, 2>(p, few, n_merges, s);
-  else max_parts >= 16 ? launch_chunk_merge_t<128, 8>(p, few, n_merges, s) : launch_chunk_merge_t<128, 2>(p, few, n_merges, s);
+  auto launch = [&](auto G) {
+    constexpr int GR = decltype(G)::value;
+    if (D == 64) launch_chunk_merge_t<64, GR>(p, few, n_merges, s);
+    else launch_chunk_merge_t<128, GR>(p, few, n_merges, s);
+  };
+  if (max_parts >= 16) launch(std::integral_constant<int, 8>{});
+  else if (max_parts >= 6) launch(std::integral_constant<int, 2>{});
+  else launch(std::integral_constant<int, 1>{});
   return hipGetLastError();
 }
 
