@@ -526,12 +526,12 @@ cas_status_t cas_paged_chunk_plan_destroy(cas_chunk_plan_t *plan);
 
 /*
  * A plan's launch table (host only; for tests and profiling tools). items may be
- * NULL; otherwise it receives 10 values per item: first token and token count of
+ * NULL; otherwise it receives 11 values per item: first token and token count of
  * the request, its key count, its first granule (16 key rows; counted over the
  * requests of the table, whole tiles of four each), the block's first row
  * (tokens x group heads), KV head, first and one past the last 64-key tile, the
- * partial that it writes (-1: the result), and its workgroup's next item (-1:
- * none). Workgroup i, in dispatch order, begins with item i.
+ * partial that it writes (-1: the result), its workgroup's next item (-1: none),
+ * and one past the block's last row. Workgroup i, in dispatch order, begins with item i.
  */
 typedef struct {
   int32_t workgroups;

@@ -751,9 +751,9 @@ def chunk_plan(problem: DecodeProblem):
     and the items of every workgroup (a tuple each)."""
     plan, info = problem.chunk_plan(), _lib.ChunkPlanInfo()
     _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), None))
-    flat = (ctypes.c_int32 * (10 * max(info.items, 1)))()
+    flat = (ctypes.c_int32 * (11 * max(info.items, 1)))()
     _check(load().cas_paged_chunk_plan_info(plan.handle, ctypes.byref(info), flat))
-    items, wgs = list(zip(*[iter(flat)] * 10)), []
+    items, wgs = list(zip(*[iter(flat)] * 11)), []
     for i in range(info.workgroups):
         wgs.append([])
         while i >= 0:

@@ -120,7 +120,7 @@ void chunk_bf16_kernel(ChunkParams) {
     TrOffsets<D> to;
     to.init(lane);
     const DevChunkItem it = load_const(p.items, at);
-    const int nrows = it.len * g;
+    const int nrows = it.row1;   // (the rows of its request that end here)
     // Few rows: the waves share them, in `rgs` groups of 32, and divide the keys.
     const bool narrow = nrows - it.row0 <= kChunkNarrowRows;
     const int rgs = nrows - it.row0 <= kFastRowsPerWave ? 1 : 2;
@@ -453,7 +453,7 @@ void chunk_bf16_kernel(ChunkParams) {
     int te = threadIdx.x;
     asm volatile("" : "+v"(te));
     const int ge = pe.g, r = ie.row0 + (te >> 6) * kFastRowsPerWave + (te & 31), Ge = te >> 5 & 1;
-    if (r >= ie.len * ge) continue;
+    if (r >= ie.row1) continue;
     const int t = r / ge, h = ie.kvh * ge + (r - t * ge);
     // (A piece of a split may hold no key that the row sees. A NaN sum stays NaN.)
     const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
@@ -469,7 +469,7 @@ void chunk_bf16_kernel(ChunkParams) {
       store((__bf16 *)pe.o + (((int64_t)ie.tok0 + t) * (pe.Hkv * ge) + h) * D);
       if (Ge == 0 && pe.lse != nullptr) pe.lse[(int64_t)h * pe.Tq + ie.tok0 + t] = lse;
     } else {
-      const int64_t R = (int64_t)ie.part * kFastRowsPerWg + (r - ie.row0);
+      const int64_t R = (int64_t)ie.part * pe.part_rows + (r - ie.row0);
       store(pe.part_o + R * D);
       if (Ge == 0) pe.part_lse[R] = lse;
     }
@@ -492,23 +492,23 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkParams p, int few
   const int which = bid < few * UF ? bid / UF : few + (bid - few * UF) / UA;
   const int unit = bid < few * UF ? bid % UF : (bid - few * UF) % UA;
   const DevChunkMerge mg = load_const(p.merges, which);
-  const int nrows = min(mg.len * p.g - mg.row0, kFastRowsPerWg);
+  const int nrows = mg.row1 - mg.row0;
   if (unit * RPW >= nrows) return;
   const int r = unit * RPW + tid / (CPR * GR);
-  const int64_t R = (int64_t)mg.part0 * kFastRowsPerWg + min(r, nrows - 1);
+  const int64_t R = (int64_t)mg.part0 * p.part_rows + min(r, nrows - 1);
   const float *lses = p.part_lse + R;
   float mx = -INFINITY;
-  for (int i = c4; i < mg.nparts; i += CPR) mx = fmaxf(mx, lses[i * kFastRowsPerWg]);
+  for (int i = c4; i < mg.nparts; i += CPR) mx = fmaxf(mx, lses[i * p.part_rows]);
 #pragma unroll
   for (int m = CPR / 2; m >= 1; m >>= 1) mx = fmaxf(mx, __shfl_xor(mx, m, CPR));
   f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
   float w_sum = 0.0f;
 #pragma unroll 4
   for (int i = gr; i < mg.nparts; i += GR) {
-    const float ls = lses[i * kFastRowsPerWg];
+    const float ls = lses[i * p.part_rows];
     const float w = ls == -INFINITY ? 0.0f : expf(ls - mx);
     w_sum += w;
-    acc += w * *reinterpret_cast<const f32x4 *>(p.part_o + (R + (int64_t)i * kFastRowsPerWg) * D + 4 * c4);
+    acc += w * *reinterpret_cast<const f32x4 *>(p.part_o + (R + (int64_t)i * p.part_rows) * D + 4 * c4);
   }
   if constexpr (GR > 1) {
     acc_l[tid] = acc;

@@ -318,18 +318,19 @@ struct AppendParams {
 };
 static_assert(sizeof(AppendParams) <= 4096, "kernel arguments");
 
-// Chunk attention over pages. One item: up to 256 packed rows from row0 on
-// (row r of a request is its token r / g, head r % g of the KV head's group) of
+// Chunk attention over pages. One item: up to 256 packed rows, row0 to row1 - 1
+// (row r of a request is its token r / g, head r % g of the KV head's group), of
 // a request with `len` new tokens from tok0 on, its last of kv_len keys, in the
 // granules granules[granule0 ..], over 64-key tiles [tile0, tile1). part: which
 // partial it writes, or -1: no other item has these rows.
 struct DevChunkItem {
   int32_t tok0, len, kv_len, granule0, row0, kvh, tile0, tile1, part;
   int32_t next;   // the workgroup's next item, or -1; its first is its own index
+  int32_t row1;
 };
 // A block of rows whose keys were split: partials part0 .. part0 + nparts - 1.
 struct DevChunkMerge {
-  int32_t tok0, len, row0, kvh, part0, nparts;
+  int32_t tok0, row0, row1, kvh, part0, nparts;
 };
 constexpr int kChunkFewRows = 32;
 constexpr int kChunkNarrowRows = 64;
@@ -342,9 +343,9 @@ struct ChunkParams {
   const DevChunkItem *items;
   const DevChunkMerge *merges;
   const uint32_t *granules;    // 16 key rows of a request each: where they are in the pools, in 2 KiB (4 per tile)
-  float *part_o;               // [partial][256][D], normalised
-  float *part_lse;             // [partial][256]
-  int32_t Hkv, g, Tq;
+  float *part_o;               // [partial][part_rows][D], normalised
+  float *part_lse;             // [partial][part_rows]
+  int32_t Hkv, g, Tq, part_rows;
   float scale_log2;
 };
 

@@ -406,7 +406,7 @@ struct ChunkPlan {
   int32_t wgs = 0;
   std::vector<uint32_t> granules;
   std::vector<DevChunkMerge> merges;   // the blocks of few rows first
-  int32_t parts = 0, max_parts = 1, few = 0;
+  int32_t parts = 0, max_parts = 1, few = 0, part_rows = 0;
   int64_t tiles = 0;
   size_t off_merges = 0, off_granules = 0, table_bytes = 0, off_plse = 0, off_po = 0, bytes = 0;
 };
@@ -417,20 +417,24 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // more than their share (a phase waits for its copies and barriers): 1.20 us for
 // 96, 1.25 for 128; with d = 64 0.87, 0.89 and 1.22. Up to kChunkNarrowRows of
 // them the kernel's waves divide the keys: 0.47 us for 32 rows and 0.92 for 64
-// where the keys are in the L2, 0.75 for 32 where most come from HBM, which is
-// what counts (with 0.47 a batch of 16 single tokens beside a chunk took 106 us,
-// with 0.75 93); with d = 64 0.26 and 0.52, and half the bytes. kWgCost: what a
-// workgroup costs beside its tiles (dispatch, first loads, pipeline fill and
-// drain, epilogue), kItemCost: a further item of a workgroup; kMergeCost: a
-// merge's launch; the partials' bytes, written and read, at kBytesPerTile. (Over
-// 30 mixes, each of them 20-50 % higher or lower changes the time by 1 %.)
-double tile_cost(int D, int rows) {
-  if (rows <= kChunkNarrowRows) return D == 128 ? (rows <= 32 ? 0.45 : 0.60) : rows <= 32 ? 0.25 : 0.33;
+// (d = 64: 0.26 and 0.52) where the keys are in the L2, as those of a request with
+// several blocks are, `shared`; else most come from HBM, 0.75 us a tile where every
+// unit asks for some (with 0.47 a batch of 16 single tokens beside a chunk took 106
+// us, with 0.75 93). kWgCost: what a workgroup costs beside its tiles (dispatch,
+// first loads, pipeline fill and drain, epilogue), kItemCost: a further item of a
+// workgroup; kMergeCost: a merge's launch; the partials' bytes, written and read, at
+// kBytesPerTile. (Over 30 mixes, each of them 20-50 % higher or lower changes the
+// time by 1 %.)
+double tile_cost(int D, int rows, bool shared) {
+  if (rows <= kChunkNarrowRows) {
+    if (shared) return D == 128 ? (rows <= 32 ? 0.27 : 0.53) : rows <= 32 ? 0.15 : 0.30;
+    return D == 128 ? (rows <= 32 ? 0.45 : 0.60) : rows <= 32 ? 0.25 : 0.33;
+  }
   return D == 128 ? 0.57 + 0.43 * rows / 256 : 0.42 + 0.30 * rows / 256;
 }
 constexpr double kWgCost = 5.0, kItemCost = 3.0, kMergeCost = 3.0, kBytesPerTile = 5e6;
 constexpr double kWorthIt = 0.97;   // of the cost without cuts: below it, blocks are cut
-constexpr int kMinPiece = 2;        // tiles
+int min_piece(int rows) { return rows <= kChunkNarrowRows ? 4 : 2; }   // tiles (narrow: a piece for every wave)
 constexpr int kManyRounds = 8;
 
 struct ChunkBlock {
@@ -457,7 +461,7 @@ double fill_bins(const std::vector<ChunkBlock> &blocks, int n_bins, std::vector<
   std::stable_sort(order.begin(), order.end(), [&](int32_t x, int32_t y) { return whole(x) > whole(y); });
   // An equal share of all blocks, and a piece beside whole ones; at least a piece.
   double target = kWgCost + (sum + kItemCost * (double)blocks.size()) / n_bins;
-  for (const ChunkBlock &x : blocks) target = std::max(target, kWgCost + std::min<int>(kMinPiece, x.tiles) * x.cost);
+  for (const ChunkBlock &x : blocks) target = std::max(target, kWgCost + std::min<int>(min_piece(x.rows), x.tiles) * x.cost);
   std::vector<int32_t> left;
   auto later = [&](int x, int y) { return load[x] != load[y] ? load[x] > load[y] : x > y; };
   std::vector<int> heap(n_bins);
@@ -484,11 +488,11 @@ double fill_bins(const std::vector<ChunkBlock> &blocks, int n_bins, std::vector<
       int32_t take = rest;
       if (k < by_room.size()) {
         take = (int32_t)std::max(0.0, std::min((double)rest, (target - load[by_room[k]] - kItemCost) / blocks[i].cost + 0.5));
-        if (take < std::min(kMinPiece, rest)) {
+        if (take < std::min(min_piece(blocks[i].rows), rest)) {
           ++k;
           continue;
         }
-        if (rest - take < kMinPiece) take = rest;
+        if (rest - take < min_piece(blocks[i].rows)) take = rest;
       }
       const int x = k < by_room.size() ? by_room[k] : (int)(std::min_element(load.begin(), load.end()) - load.begin());
       bins[x].push_back({i, t, t + take});
@@ -548,7 +552,12 @@ bool plan_decode_part(const cas_decode_problem_t *p, int b0, int b1, bool beside
 // The launch plan. Either a workgroup per block, longest first, which the
 // hardware hands out as compute units become free; or, where that leaves some
 // idle, one workgroup per compute unit with an equal share, blocks cut along the
-// key axis as that needs and merged afterwards.
+// key axis as that needs and merged afterwards. Blocks have 256 rows, fewer where
+// the costs say so: one request of 64 tokens over 1,074 keys (d = 128, 8 KV heads of
+// 4) takes 26.4 us in blocks of 256 rows, 22.2 of 128, 22.2 of 64 and 19.3 of 32, over
+// 4,146 keys 43.4, 38.6, 32.6 and 25.5, 512 tokens over 1,536 keys 38.5, 40.8, 32.4 and
+// 37.6. Over 64 problems the choice is 0.5 % slower than the best of the four, at most
+// 7 %, and blocks of 256 alone 18 %, at most 71.
 //
 // Workgroup i goes to XCD i mod X, each with its own L2, so a KV head's workgroups
 // stay on one XCD (or on X / Hkv of them) where the heads divide evenly.
@@ -574,45 +583,70 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   // KV heads kvh with kvh mod groups == i share the XCDs x with x mod groups == i.
   const int groups = Hkv % X == 0 ? X : X % Hkv == 0 ? Hkv : 1;
   const int bins = cus / groups, heads = Hkv / groups;   // of a group
-  std::vector<ChunkBlock> blocks;                        // of the first group's heads
-  double sum = 0.0;
-  for (int h = 0; h < heads; ++h)
-    for (int b = 0; b < B; ++b) {
-      const int64_t n = p->q_offsets[b + 1] - p->q_offsets[b], nrows = n * g, before = p->kv_lens[b] - n;
-      for (int64_t r = 0; r < nrows && !elsewhere[b]; r += kChunkRows) {
-        const int64_t r1 = std::min<int64_t>(nrows, r + kChunkRows);
-        const int32_t nt = (int32_t)((before + (r1 - 1) / g) / kChunkTile + 1);   // up to its last query's own key
-        blocks.push_back({b, (int32_t)r, (int32_t)(r1 - r), nt, h * groups, tile_cost(D, (int)(r1 - r))});
-        sum += blocks.back().tiles * blocks.back().cost + kWgCost;
+  // In blocks of `rows` rows: those of the first group's heads, the group's
+  // workgroups in order, and what they cost.
+  struct Split {
+    std::vector<ChunkBlock> blocks;
+    std::vector<std::vector<ChunkPiece>> wgs;
+    double cost;
+  };
+  auto split = [&](int rows) {
+    Split x;
+    std::vector<ChunkBlock> &blocks = x.blocks;
+    double sum = 0.0;
+    for (int h = 0; h < heads; ++h)
+      for (int b = 0; b < B; ++b) {
+        const int64_t n = p->q_offsets[b + 1] - p->q_offsets[b], nrows = n * g, before = p->kv_lens[b] - n;
+        for (int64_t r = 0; r < nrows && !elsewhere[b]; r += rows) {
+          const int64_t r1 = std::min<int64_t>(nrows, r + rows);
+          const int32_t nt = (int32_t)((before + (r1 - 1) / g) / kChunkTile + 1);   // up to its last query's own key
+          blocks.push_back({b, (int32_t)r, (int32_t)(r1 - r), nt, h * groups, tile_cost(D, (int)(r1 - r), nrows > rows)});
+          sum += blocks.back().tiles * blocks.back().cost + kWgCost;
+        }
+      }
+    // First a block each.
+    std::stable_sort(blocks.begin(), blocks.end(), [](const ChunkBlock &x, const ChunkBlock &y) { return x.tiles * x.cost > y.tiles * y.cost; });
+    auto whole = [&](size_t i) { return blocks[i].tiles * blocks[i].cost + kWgCost; };
+    x.cost = sum / bins;
+    // (Of the k * bins + 1 longest blocks, one unit gets k + 1.)
+    for (size_t k = 0; k < 4 && k * bins < blocks.size(); ++k) {
+      double c = 0.0;
+      for (size_t i = k * bins - k; i <= k * bins; ++i) c += whole(i);
+      x.cost = std::max(x.cost, c);
+    }
+    for (size_t i = 0; i < blocks.size(); ++i) x.wgs.push_back({{(int32_t)i, 0, blocks[i].tiles}});
+    // Units differ in speed by a few per cent, which evens out where each gets
+    // several blocks from the hardware: with kManyRounds of them nothing is cut.
+    if (!blocks.empty() && blocks.size() < (size_t)(kManyRounds * bins)) {
+      std::vector<std::vector<ChunkPiece>> equal;
+      double even = fill_bins(blocks, bins, equal) + kMergeCost;
+      std::vector<int32_t> n_pieces(blocks.size(), 0);
+      for (const auto &w : equal)
+        for (const ChunkPiece &y : w) ++n_pieces[y.block];
+      double bytes = 0.0;
+      for (size_t i = 0; i < blocks.size(); ++i)
+        if (n_pieces[i] > 1) bytes += (double)n_pieces[i] * blocks[i].rows * D * 4;
+      even += bytes * groups / kBytesPerTile;
+      if (even < kWorthIt * x.cost) {
+        x.wgs.swap(equal);
+        x.cost = even;
       }
     }
+    return x;
+  };
+  Split best = split(kChunkRows);
+  pl.part_rows = kChunkRows;
+  // Smaller blocks cost more a row and are done sooner; not where every unit has one.
+  for (int rows = kChunkRows / 2; rows >= kChunkFewRows && best.blocks.size() < (size_t)bins; rows /= 2) {
+    Split x = split(rows);
+    if (x.cost < best.cost) {
+      best = std::move(x);
+      pl.part_rows = rows;
+    }
+  }
+  auto &blocks = best.blocks;
+  auto &wgs = best.wgs;
   if ((int64_t)blocks.size() * groups > INT32_MAX / 256) return set_error(CAS_ERR_UNSUPPORTED, "too many workgroups");
-  // A group's workgroups, in order, and what they cost; first a block each.
-  std::vector<std::vector<ChunkPiece>> wgs;
-  std::stable_sort(blocks.begin(), blocks.end(), [](const ChunkBlock &x, const ChunkBlock &y) { return x.tiles * x.cost > y.tiles * y.cost; });
-  auto whole = [&](size_t i) { return blocks[i].tiles * blocks[i].cost + kWgCost; };
-  double alone = sum / bins;
-  // (Of the k * bins + 1 longest blocks, one unit gets k + 1.)
-  for (size_t k = 0; k < 4 && k * bins < blocks.size(); ++k) {
-    double c = 0.0;
-    for (size_t i = k * bins - k; i <= k * bins; ++i) c += whole(i);
-    alone = std::max(alone, c);
-  }
-  for (size_t i = 0; i < blocks.size(); ++i) wgs.push_back({{(int32_t)i, 0, blocks[i].tiles}});
-  // Units differ in speed by a few per cent, which evens out where each gets
-  // several blocks from the hardware: with kManyRounds of them nothing is cut.
-  if (!blocks.empty() && blocks.size() < (size_t)(kManyRounds * bins)) {
-    std::vector<std::vector<ChunkPiece>> equal;
-    double even = fill_bins(blocks, bins, equal) + kMergeCost;
-    std::vector<int32_t> n_pieces(blocks.size(), 0);
-    for (const auto &w : equal)
-      for (const ChunkPiece &x : w) ++n_pieces[x.block];
-    double bytes = 0.0;
-    for (size_t i = 0; i < blocks.size(); ++i)
-      if (n_pieces[i] > 1) bytes += (double)n_pieces[i] * blocks[i].rows * D * 4;
-    even += bytes * groups / kBytesPerTile;
-    if (even < kWorthIt * alone) wgs.swap(equal);
-  }
   wgs.erase(std::remove_if(wgs.begin(), wgs.end(), [](const std::vector<ChunkPiece> &w) { return w.empty(); }), wgs.end());
   // Partials: a block's lie together, in the order of its keys.
   std::vector<std::vector<int32_t>> cut(blocks.size());
@@ -634,8 +668,7 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
       for (size_t i = 0; i < blocks.size(); ++i) {
         const ChunkBlock &x = blocks[i];
         if (part0[i] < 0 || (x.rows <= kChunkFewRows) != (few == 1)) continue;
-        pl.merges.push_back({p->q_offsets[x.b], p->q_offsets[x.b + 1] - p->q_offsets[x.b], x.row0, x.kvh + gr, gr * parts + part0[i],
-                             (int32_t)cut[i].size()});
+        pl.merges.push_back({p->q_offsets[x.b], x.row0, x.row0 + x.rows, x.kvh + gr, gr * parts + part0[i], (int32_t)cut[i].size()});
       }
     if (few) pl.few = (int32_t)pl.merges.size();
   }
@@ -657,7 +690,7 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
     const auto &c = cut[y.block];
     const int32_t part = part0[y.block] < 0 ? -1 : gr * parts + part0[y.block] + (int32_t)(std::lower_bound(c.begin(), c.end(), y.t0) - c.begin());
     pl.tiles += y.t1 - y.t0;
-    return DevChunkItem{tok0, len, p->kv_lens[x.b], granule0[x.b], x.row0, x.kvh + gr, y.t0, y.t1, part, -1};
+    return DevChunkItem{tok0, len, p->kv_lens[x.b], granule0[x.b], x.row0, x.kvh + gr, y.t0, y.t1, part, -1, x.row0 + x.rows};
   };
   pl.wgs = (int32_t)wgs.size() * groups;
   for (const auto &w : wgs)
@@ -675,8 +708,8 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   pl.off_granules = align256(pl.off_merges + pl.merges.size() * sizeof(DevChunkMerge));
   pl.table_bytes = align256(pl.off_granules + pl.granules.size() * sizeof(uint32_t));
   pl.off_plse = pl.table_bytes;
-  pl.off_po = align256(pl.off_plse + (size_t)pl.parts * kChunkRows * 4);
-  pl.bytes = align256(pl.off_po + (size_t)pl.parts * kChunkRows * p->head_dim * 4);
+  pl.off_po = align256(pl.off_plse + (size_t)pl.parts * pl.part_rows * 4);
+  pl.bytes = align256(pl.off_po + (size_t)pl.parts * pl.part_rows * p->head_dim * 4);
   for (DecodePart &d : pl.decode) {
     d.off = pl.bytes;
     pl.bytes = align256(pl.bytes + d.bytes);
@@ -797,6 +830,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   c.Hkv = p->num_kv_heads;
   c.g = p->group_size;
   c.Tq = p->q_offsets[p->batch];
+  c.part_rows = pl.part_rows;
   c.scale_log2 = p->softmax_scale * 1.4426950408889634f;
   hipError_t e = timed_launch("chunk", stream, [&] { return launch_chunk_bf16(c, p->head_dim, pl.wgs, stream); });
   if (e != hipSuccess) return set_hip_error("chunk launch", e);
@@ -951,7 +985,7 @@ cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_p
   info->decode_parts = (int32_t)pl.decode.size();
   for (const DecodePart &d : pl.decode) info->decode_tokens += d.tokens;
   info->ws_bytes = pl.bytes;
-  static_assert(sizeof(DevChunkItem) == 40, "a table of 32-bit values");
+  static_assert(sizeof(DevChunkItem) == 44, "a table of 32-bit values");
   if (items && !pl.items.empty()) std::memcpy(items, pl.items.data(), pl.items.size() * sizeof(DevChunkItem));
   return CAS_OK;
 }

@@ -30,6 +30,9 @@ def check(cas, q, kv, **kw):
     info, wgs = cas.chunk_plan(prob)
     items = [i for w in wgs for i in w]
     assert len(wgs) == info.workgroups and len(items) == info.items and sum(i[7] - i[6] for i in items) == info.key_tiles
+    # Blocks of one size (the largest of them: 256, or what a half of it holds).
+    rows = next((r for r in (32, 64, 128) if all(i[10] - i[4] <= r for i in items) and all(i[4] % r == 0 for i in items) and
+                 all(i[10] == min(i[1] * g, i[4] + r) for i in items)), ROWS)
     seen, parts = {}, {}
     granule0, at = {}, 0
     listed = {i[0] for i in items}
@@ -37,14 +40,15 @@ def check(cas, q, kv, **kw):
         if q[b] and sum(q[:b]) in listed:
             granule0[b], at = at, at + -(-(-(-L // P) * (P // 16)) // 4) * 4
     first = {sum(q[:b]): b for b in reversed(range(len(q))) if q[b]}
-    for tok0, n, L, pg, row0, kvh, t0, t1, part, _ in items:
+    for tok0, n, L, pg, row0, kvh, t0, t1, part, _, row1 in items:
         b = first[tok0]
-        assert (n, L, pg) == (q[b], kv[b], granule0[b]) and row0 % ROWS == 0 and row0 < n * g and 0 <= kvh < Hkv
-        last = L - n + (min(n * g, row0 + ROWS) - 1) // g      # of the block's rows
+        assert row1 == min(n * g, row0 + rows)
+        assert (n, L, pg) == (q[b], kv[b], granule0[b]) and row0 % rows == 0 and row0 < n * g and 0 <= kvh < Hkv
+        last = L - n + (row1 - 1) // g      # of the block's rows
         assert 0 <= t0 < t1 <= last // TILE + 1
         seen.setdefault((b, row0, kvh), []).append((t0, t1, last // TILE + 1))
         parts.setdefault((b, row0, kvh), []).append(part)
-    want = {(b, r, k) for b, n in enumerate(q) for r in range(0, n * g, ROWS) for k in range(Hkv)}
+    want = {(b, r, k) for b, n in enumerate(q) for r in range(0, n * g, rows) for k in range(Hkv)}
     gone = {b for b, _, _ in want - set(seen)}                     # requests that the decode kernels take
     assert set(seen) == {w for w in want if w[0] not in gone} and all(q[b] == 1 for b in gone) and len(gone) == info.decode_tokens
     all_parts = []
@@ -55,7 +59,7 @@ def check(cas, q, kv, **kw):
         assert p == [-1] if len(p) == 1 else p == list(range(p[0], p[0] + len(p))) and p[0] >= 0
         all_parts += [x for x in p if x >= 0]
     assert sorted(all_parts) == list(range(info.partials))
-    assert cas.paged_chunk_workspace_size(prob) == info.ws_bytes >= info.partials * ROWS * (prob.c.head_dim + 1) * 4
+    assert cas.paged_chunk_workspace_size(prob) == info.ws_bytes >= info.partials * rows * (prob.c.head_dim + 1) * 4
     return info
 
 
