@@ -89,9 +89,36 @@ __device__ __forceinline__ float piece_weights(float c, float mu, f32x16 &s, bf1
   return l[0] + l[1];
 }
 
-template <int D>
+struct NoTables {};
+
+// The kernel's parameters, with DIRECT the granules' place among them.
+template <bool DIRECT>
+__device__ __forceinline__ ChunkParams chunk_params() {
+  ChunkParams p = load_kernarg<ChunkParams>();
+  if constexpr (DIRECT) {
+    const ChunkDirect *d = kernarg_at<ChunkDirect>(sizeof(ChunkParams));
+    p.granules = d->words + load_const(&d->n, 0) * (int)(sizeof(ChunkDirectRequest) / 4);
+  }
+  return p;
+}
+
+template <bool DIRECT>
+__device__ __forceinline__ DevChunkItem chunk_item(const ChunkParams &p, int at) {
+  if constexpr (!DIRECT) return load_const(p.items, at);
+  const ChunkDirect *d = kernarg_at<ChunkDirect>(sizeof(ChunkParams));
+  const auto *requests = reinterpret_cast<const ChunkDirectRequest *>(d->words);
+  const int n = load_const(&d->n, 0), rows = load_const(&d->rows, 0);
+  const int block = at / p.Hkv;
+  int i = 0;
+  while (i + 1 < n && block >= load_const(requests, i + 1).block0) ++i;
+  const ChunkDirectRequest r = load_const(requests, i);
+  const int row0 = (block - r.block0) * rows, row1 = min(r.len * p.g, row0 + rows);
+  return DevChunkItem{r.tok0, r.len, r.kv_len, r.granule0, row0, at - block * p.Hkv, 0, (r.kv_len - r.len + (row1 - 1) / p.g) / kKT + 1, -1, -1, row1};
+}
+
+template <int D, bool DIRECT>
 __global__ __launch_bounds__(kFastThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void chunk_bf16_kernel(ChunkParams) {
+void chunk_bf16_kernel(ChunkParams, std::conditional_t<DIRECT, ChunkDirect, NoTables>) {
   constexpr int NSTEP = D / 16, DT = D / 32;
   constexpr int TB = kKT * D * 2;
   constexpr int CPR = D / 8, RPI = 64 / CPR;   // 16-byte chunks of a key row, key rows of a copy instruction
@@ -109,7 +136,7 @@ void chunk_bf16_kernel(ChunkParams) {
     // across items would be held in registers through the tile loop.
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));
-    const ChunkParams p = load_kernarg<ChunkParams>();
+    const ChunkParams p = chunk_params<DIRECT>();
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int grp = wave >> 2, w4 = wave & 3;
     const int G = lane >> 5, n = lane & 31;
@@ -119,7 +146,7 @@ void chunk_bf16_kernel(ChunkParams) {
     ro.init(n, G);
     TrOffsets<D> to;
     to.init(lane);
-    const DevChunkItem it = load_const(p.items, at);
+    const DevChunkItem it = chunk_item<DIRECT>(p, at);
     const int nrows = it.row1;   // (the rows of its request that end here)
     // Few rows: the waves share them, in `rgs` groups of 32, and divide the keys.
     const bool narrow = nrows - it.row0 <= kChunkNarrowRows;
@@ -448,7 +475,7 @@ void chunk_bf16_kernel(ChunkParams) {
     const float m_out = m_run;
     // (Read anew, again: nothing of this is held through the tile loop.)
     const ChunkParams pe = load_kernarg<ChunkParams>();
-    const DevChunkItem ie = load_const(pe.items, at);
+    const DevChunkItem ie = chunk_item<DIRECT>(pe, at);
     at = __builtin_amdgcn_readfirstlane(ie.next);
     int te = threadIdx.x;
     asm volatile("" : "+v"(te));
@@ -550,9 +577,15 @@ void launch_chunk_merge_t(const ChunkParams &p, int few, int n_merges, hipStream
 
 }  // namespace
 
-hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_wgs, hipStream_t s) {
-  if (D == 64) hipLaunchKernelGGL(chunk_bf16_kernel<64>, dim3((unsigned)n_wgs), dim3(kFastThreads), 0, s, p);
-  else hipLaunchKernelGGL(chunk_bf16_kernel<128>, dim3((unsigned)n_wgs), dim3(kFastThreads), 0, s, p);
+hipError_t launch_chunk_bf16(const ChunkParams &p, const ChunkDirect *direct, int D, int n_wgs, hipStream_t s) {
+  const dim3 grid((unsigned)n_wgs), threads(kFastThreads);
+  if (direct) {
+    if (D == 64) hipLaunchKernelGGL((chunk_bf16_kernel<64, true>), grid, threads, 0, s, p, *direct);
+    else hipLaunchKernelGGL((chunk_bf16_kernel<128, true>), grid, threads, 0, s, p, *direct);
+  } else {
+    if (D == 64) hipLaunchKernelGGL((chunk_bf16_kernel<64, false>), grid, threads, 0, s, p, NoTables{});
+    else hipLaunchKernelGGL((chunk_bf16_kernel<128, false>), grid, threads, 0, s, p, NoTables{});
+  }
   return hipGetLastError();
 }
 

@@ -338,7 +338,7 @@ __device__ __forceinline__ T load_const(const T *base, int i) {
   return r;
 }
 
-// The kernel's only parameter, read from the kernel argument segment at this
+// The kernel's first parameter, read from the kernel argument segment at this
 // point and not kept from an earlier read.
 template <typename T>
 __device__ __forceinline__ T load_kernarg() {
@@ -351,6 +351,12 @@ __device__ __forceinline__ T load_kernarg() {
 #pragma unroll
   for (int k = 0; k < (int)(sizeof(T) / 4); ++k) rw[k] = w[k];
   return r;
+}
+
+// Address of what lies `off` bytes into the kernel arguments (for load_const).
+template <typename T>
+__device__ __forceinline__ const T *kernarg_at(int off) {
+  return (const T *)((uint64_t)__builtin_amdgcn_kernarg_segment_ptr() + off);
 }
 
 }  // namespace cas

@@ -349,6 +349,20 @@ struct ChunkParams {
   float scale_log2;
 };
 
+// A plan of few whole blocks as kernel arguments, instead of tables in the
+// workspace: workgroup i has KV head i mod Hkv and block i / Hkv of the listed
+// requests' blocks of `rows` rows, counted on from block0 of each. Behind the
+// requests lie the granules.
+struct ChunkDirectRequest {
+  int32_t block0, tok0, len, kv_len, granule0;
+};
+constexpr int kChunkDirectWords = 960;
+struct ChunkDirect {
+  int32_t n, rows;
+  uint32_t words[kChunkDirectWords];
+};
+static_assert(sizeof(ChunkParams) % 8 == 0 && sizeof(ChunkParams) + sizeof(ChunkDirect) <= 4096, "kernel arguments");
+
 // Forward shared by cas_prefix_attn_fwd (scratch == nullptr: the caller's
 // workspace, tables through the pinned staging ring) and the no-allocation
 // forward (scratch != nullptr: after validation, scratch() yields the device
@@ -388,7 +402,8 @@ hipError_t launch_adam_bf16(const AdamParams &p, int D, int n_chunks, hipStream_
 hipError_t launch_decode_bf16(const DecodeParams &p, int D, int n_work, int row_blocks, hipStream_t s);
 hipError_t launch_decode_merge_bf16(const DecodeParams &p, int D, int max_split, hipStream_t s);
 hipError_t launch_rope(const RopeParams &p, DType dt, int D, int n, hipStream_t s);
-hipError_t launch_chunk_bf16(const ChunkParams &p, int D, int n_wgs, hipStream_t s);
+// direct: null, or what stands in for p's tables.
+hipError_t launch_chunk_bf16(const ChunkParams &p, const ChunkDirect *direct, int D, int n_wgs, hipStream_t s);
 // n_merges blocks, of which the first `few` have at most kChunkFewRows rows.
 hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_merges, int max_parts, hipStream_t s);
 // Copies `bytes` (a multiple of 16) of pinned host memory to device memory; when

@@ -191,3 +191,16 @@ def test_binding_refusals(cas):
     for over in (dict(q=q.float()), dict(k_pages=kp.float()), dict(lse=torch.zeros(4, 3, dtype=bf))):
         with pytest.raises(TypeError):
             cas.paged_chunk_fwd(**{**ok, **over})
+
+
+def test_few_whole_blocks_need_no_workspace(cas):
+    """What fits the kernel's arguments: one block for a compute unit at most, and
+    requests and granules within 960 words."""
+    def needs(q, kv):
+        own = [[100 * b + j for j in range(-(-L // 16))] for b, L in enumerate(kv)]
+        return check(cas, q, kv, pages=own, Hkv=8, g=4, D=128).ws_bytes
+
+    assert needs([33, 0, 5], [1100, 0, 70]) == needs([1] * 24, [300 + i for i in range(24)]) == 0
+    assert needs([1] * 40, [300 + i for i in range(40)]) > 0      # 320 blocks
+    assert needs([1] * 30, [600 + i for i in range(30)]) > 0      # 30 * (5 + 40) words
+    assert needs([200], [9000]) > 0                               # cut
