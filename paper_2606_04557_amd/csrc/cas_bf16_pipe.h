@@ -185,9 +185,8 @@ __device__ __forceinline__ float fwd_tile_max(const f32x16 &s0, const f32x16 &s1
 }
 
 // Weights of a tile from its scores, offset by mu: bf16 for the next product
-// (half a step, 2^-8 of a weight, which all the rows' values share at random; an
-// fp32 product would run at an eighth of the rate), fp32 for the row sum, which
-// the LSE needs to better than that. piece(n), n < PIECES: copy instruction n of
+// (off by up to half a step, 2^-8 of a weight; fp32 products run at a sixteenth of
+// the rate), fp32 for the row sum, which the LSE needs to better than that. piece(n), n < PIECES: copy instruction n of
 // the phase, spread evenly over the exponentials.
 template <int PIECES, typename Piece>
 __device__ __forceinline__ float fwd_weights(float c, float mu, f32x16 &s0, f32x16 &s1, bf16x8 (&pf)[2][2], Piece &&piece) {

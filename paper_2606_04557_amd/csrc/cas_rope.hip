@@ -10,7 +10,11 @@
 // once and walks several heads.
 //
 // Bound by HBM: an element is read once and written once, and the angles cost
-// about 30 operations for each pair and thread.
+// about 30 operations for each pair and thread. 8,192 tokens of 32 query and 8 key
+// heads of 128 (bf16, 168 MB): 27 us, 6.2 TB/s where a 1 GiB device copy reaches
+// 5.1 (what the caches still hold counts); 8 requests' 1,000 to 1,024 new tokens
+// appended with their queries (198 MB): 34 us, 5.8 TB/s. One new token: 2.7 us, a
+// launch's latency.
 #include <algorithm>
 
 #include "cas_device.h"
