@@ -320,6 +320,33 @@ def test_graphs(gpu_lib):
             assert t.equal(o, o2) and t.equal(lse, lse2)
 
 
+@pytest.mark.parametrize("D,Hkv,g", [(128, 8, 4), (64, 3, 5)])
+def test_calls_without_tables(gpu_lib, D, Hkv, g):
+    """Few whole blocks, whose tables are kernel arguments: an empty workspace, calls
+    on two streams at once, and a captured call replayed with other inputs."""
+    t = _t()
+    counts, kv = [0, 33, 1, 0, 20, 5], [9, 500, 260, 0, 20, 70]
+    prob, q, kp, vp, o, lse, _ = run(gpu_lib, counts, kv, 16, Hkv, g, D, pad=2)
+    assert gpu_lib.paged_chunk_workspace_size(prob) == 0
+    a, b = gpu_lib.paged_chunk_fwd(q, kp, vp, prob, workspace=t.empty(0, dtype=t.uint8, device="cuda"))
+    ss = [t.cuda.Stream() for _ in range(2)]
+    t.cuda.synchronize()
+    outs = [gpu_lib.paged_chunk_fwd(q, kp, vp, prob, stream=ss[i % 2]) for i in range(6)] + [(a, b)]
+    t.cuda.synchronize()
+    n = sum(counts)
+    assert all(t.equal(x[:n], o[:n]) and t.equal(y, lse) for x, y in outs)
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        gpu_lib.paged_chunk_fwd(q, kp, vp, prob, o=o, lse=lse)
+    for i in range(3):
+        q.copy_(_rand(q.shape, 1.0, 30 + i))
+        lse.zero_()
+        graph.replay()
+        x, y = gpu_lib.paged_chunk_fwd(q, kp, vp, prob)
+        t.cuda.synchronize()
+        assert t.equal(x[:n], o[:n]) and t.equal(y, lse)
+
+
 def test_pages_past_4_gib(gpu_lib):
     t = _t()
     P, Hkv, D, n = 128, 64, 128, 2600
