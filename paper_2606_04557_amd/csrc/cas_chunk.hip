@@ -345,15 +345,18 @@ void chunk_bf16_kernel(ChunkParams, std::conditional_t<DIRECT, ChunkDirect, NoTa
           for (int s = 0; s < 2; ++s) pf[a][s] = Mma<__bf16>::zero();
       };
       no_weights();
+      // (Works on a copy of the scores, as nothing needs them afterwards: written in
+      // place they were moved between registers where the variants meet, 2-3 % of all.)
       auto softmax = [&](auto MASK, int lim, auto &&piece) __attribute__((always_inline)) {
-        if constexpr (decltype(MASK)::value) fwd_mask(lim, G, s0, s1);
+        f32x16 t0 = s0, t1 = s1;
+        if constexpr (decltype(MASK)::value) fwd_mask(lim, G, t0, t1);
         // Only until every row of the wave has seen a key.
         if (wave_any(m_run == -INFINITY)) {
-          const float mt = fwd_tile_max(s0, s1, c);
+          const float mt = fwd_tile_max(t0, t1, c);
           m_run = (m_run == -INFINITY) ? mt : m_run;
         }
         const float mu = (m_run == -INFINITY) ? 0.0f : m_run;
-        l_run += fwd_weights<kPieces>(c, mu, s0, s1, pf, piece);
+        l_run += fwd_weights<kPieces>(c, mu, t0, t1, pf, piece);
       };
       auto gphase = [&](int j, const char *kb, const char *vbp) __attribute__((always_inline)) {
         if (j <= nt && wave_active) fwd_matrix_phase<D>(kb, vbp, ro, to, qf, pf, s0, s1, oacc);
