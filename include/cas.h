@@ -501,15 +501,17 @@ cas_status_t cas_paged_append_plan_destroy(cas_append_plan_t *plan);
  * cas_paged_decode_fwd (the new tokens' K/V already in their pages:
  * cas_paged_append); requests without new tokens are allowed. That call streams
  * the keys once for every 32 rows (tokens x heads of a group) and is for steps
- * of a few tokens per request; this one takes 256 rows at a time on the matrix
- * cores. Requests of one new token next to each other whose pages are shared go
- * through that call's kernels. Rows of q and o behind the last request's are neither read nor
- * written; lse is [Hq, Tq]. Keys past a query's own position do not reach it,
- * whatever they and their values hold (NaN and infinities included).
+ * of a few tokens per request; this one takes up to 256 rows at a time on the
+ * matrix cores. Requests of one new token next to each other whose pages are
+ * shared go through that call's kernels. Rows of q and o behind the last
+ * request's are neither read nor written; lse is [Hq, Tq]. Keys past a query's
+ * own position do not reach it, whatever they and their values hold (NaN and
+ * infinities included).
  *
- * Under stream capture the launch tables travel as kernel arguments; a captured
- * call uses its workspace at every replay, so graphs that may run at the same
- * time need one each.
+ * A short problem needs no workspace: its size is 0 then, and NULL will do. Calls
+ * that run at the same time need a workspace each. Under stream capture the
+ * launch tables travel as kernel arguments; a captured call uses its workspace at
+ * every replay, so graphs that may run at the same time need one each, too.
  */
 cas_status_t cas_paged_chunk_workspace_size(const cas_decode_problem_t *p, size_t *bytes);
 cas_status_t cas_paged_chunk_fwd(const cas_decode_problem_t *p, const void *q, const void *k_pages, const void *v_pages,
