@@ -696,9 +696,12 @@ def paged_append(k, v, k_pages, v_pages, problem: DecodeProblem, rope: Optional[
         sp = starts.buffer_info()[0]
     _gpu("k", k)
     packed = _APPEND.pack(kp, vp, kt, kh, vt, vh, qp, qt, qh, op, sp)
-    _on_device(index, stream, lambda handle: load().cas_paged_append_run(
-        problem.append_plan().handle, None if rope is None else rope._on(index, handle), packed, k_pages.data_ptr(),
-        v_pages.data_ptr(), handle))
+
+    def call(handle):
+        plan = problem.append_plan()   # (held through the call: another thread may put its own into the problem)
+        return load().cas_paged_append_run(plan.handle, None if rope is None else rope._on(index, handle), packed,
+                                           k_pages.data_ptr(), v_pages.data_ptr(), handle)
+    _on_device(index, stream, call)
     return q_out
 
 

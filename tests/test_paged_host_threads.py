@@ -1,0 +1,79 @@
+"""Calls of the binding from several host threads at once, without a GPU: the
+library's launches are stood in for, and CPU tensors say that they are on GPU 0.
+
+A plan or a table that one thread uses must live until its call has returned,
+whatever the others put in its place meanwhile.
+"""
+import gc
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+class OnGpu(torch.Tensor):
+    """A CPU tensor that says it is on GPU 0."""
+
+    def get_device(self):
+        return 0
+
+
+def on_gpu(*shape, dtype=torch.bfloat16):
+    return torch.zeros(shape, dtype=dtype).as_subclass(OnGpu)
+
+
+class Library:
+    """The library with some of its entries replaced."""
+
+    def __init__(self, lib, **entries):
+        self._lib = lib
+        self.__dict__.update(entries)
+
+    def __getattr__(self, name):
+        return getattr(self._lib, name)
+
+
+@pytest.fixture
+def cas(monkeypatch):
+    import paper_2606_04557_amd as cas
+    cas.load()
+
+    def on_device(index, stream, call):
+        status = call(0)
+        assert status == 0, status
+    monkeypatch.setattr(cas, "_on_device", on_device)
+    return cas
+
+
+def replace_entries(cas, monkeypatch, **entries):
+    lib = Library(cas.load(), **entries)
+    monkeypatch.setattr(cas, "load", lambda: lib)
+
+
+@pytest.mark.parametrize("call", ["append", "chunk"])
+def test_a_plan_outlives_the_call_that_runs_it(cas, monkeypatch, call):
+    """Another thread, which found no plan either, puts its own in the place of
+    the one that the library is working on."""
+    run, destroy = f"cas_paged_{call}_run", f"cas_paged_{call}_plan_destroy"
+    real, destroyed, alive = getattr(cas.load(), destroy), [], []
+    problem = cas.DecodeProblem([2, 1], [18, 5], [[0, 1], [2]], 4, 16, 2, 2, 64, 0.125)
+
+    def run_stub(handle, *_):
+        setattr(problem, f"_{call}_plan", None)
+        gc.collect()
+        alive.append(handle.value not in destroyed)
+        return 0
+
+    def destroy_stub(handle):
+        destroyed.append(handle.value)
+        return real(handle)
+    replace_entries(cas, monkeypatch, **{run: run_stub, destroy: destroy_stub})
+    pools = on_gpu(4, 16, 2, 64), on_gpu(4, 16, 2, 64)
+    if call == "append":
+        cas.paged_append(on_gpu(3, 2, 64), on_gpu(3, 2, 64), *pools, problem)
+    else:
+        cas.paged_chunk_fwd(on_gpu(3, 4, 64), *pools, problem, o=on_gpu(3, 4, 64), lse=on_gpu(4, 3, dtype=torch.float32),
+                            workspace=on_gpu(1 << 20, dtype=torch.uint8))
+    gc.collect()
+    assert alive == [True]
+    assert len(destroyed) == 1   # (and it is freed afterwards)
