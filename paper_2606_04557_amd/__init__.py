@@ -510,7 +510,8 @@ class Rope:
             if got is None:
                 t = torch.tensor(self.turns, dtype=torch.float64, device=torch.device("cuda", index))
                 c = _lib.Rope(self._LAYOUTS[self.layout], self.rotary_dim, t.data_ptr(), self.scale)
-                got = self._device[index] = (c, t, {torch.cuda.current_stream(index).cuda_stream})
+                # (Threads that get here at the same time each have an upload; the first one is kept, for all of them.)
+                got = self._device.setdefault(index, (c, t, {torch.cuda.current_stream(index).cuda_stream}))
             if handle not in got[2]:
                 # (Freed with this object, the memory waits for what was launched on that stream.)
                 got[1].record_stream(torch.cuda.ExternalStream(handle, device=torch.device("cuda", index)))

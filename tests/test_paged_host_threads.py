@@ -77,3 +77,48 @@ def test_a_plan_outlives_the_call_that_runs_it(cas, monkeypatch, call):
     gc.collect()
     assert alive == [True]
     assert len(destroyed) == 1   # (and it is freed afterwards)
+
+
+def test_frequencies_outlive_every_call_that_reads_them(cas, monkeypatch):
+    """Two threads whose first calls with one Rope come at the same time both
+    upload its frequencies: each call has to get an upload that is kept."""
+    import threading
+    import weakref
+    both, uploads, read = threading.Barrier(2, timeout=30), [], []
+
+    class Stream:
+        cuda_stream = 0
+
+    def upload(*args, **kw):
+        t = torch.zeros(32, dtype=torch.float64)
+        uploads.append((t.data_ptr(), weakref.ref(t)))
+        both.wait()          # (neither has stored its own yet)
+        return t
+
+    def rope_stub(c, *_):
+        both.wait()          # (both have)
+        gc.collect()
+        read.append(any(ref() is not None and at == c.turns for at, ref in uploads))
+        both.wait()
+        return 0
+    rope = cas.Rope(64)
+    replace_entries(cas, monkeypatch, cas_rope=rope_stub)
+    monkeypatch.setattr(torch, "tensor", upload)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda index=None: Stream)
+    failed = []
+
+    def work():
+        try:
+            x = on_gpu(4, 2, 64)
+            cas.rope_fwd([x], on_gpu(4, dtype=torch.int32), rope, outs=[x])
+        except BaseException as e:   # noqa: BLE001
+            failed.append(e)
+            both.abort()
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    assert len(uploads) == 2 and read == [True, True]
+    assert sum(ref() is not None for _, ref in uploads) == 1   # (one is kept)
