@@ -509,9 +509,11 @@ cas_status_t cas_paged_append_plan_destroy(cas_append_plan_t *plan);
  * infinities included).
  *
  * A short problem needs no workspace: its size is 0 then, and NULL will do. Calls
- * that run at the same time need a workspace each. Under stream capture the
- * launch tables travel as kernel arguments; a captured call uses its workspace at
- * every replay, so graphs that may run at the same time need one each, too.
+ * that run at the same time need a workspace each. A call made while the launch
+ * tables of sixteen before it have not reached the device yet may wait for one of
+ * them, for 10 ms at most. Under stream capture the launch tables travel as kernel
+ * arguments; a captured call uses its workspace at every replay, so graphs that may
+ * run at the same time need one each, too.
  */
 cas_status_t cas_paged_chunk_workspace_size(const cas_decode_problem_t *p, size_t *bytes);
 cas_status_t cas_paged_chunk_fwd(const cas_decode_problem_t *p, const void *q, const void *k_pages, const void *v_pages,

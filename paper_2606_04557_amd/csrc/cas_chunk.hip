@@ -616,9 +616,12 @@ hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_m
 }
 
 hipError_t launch_table_flags(void *dst, const void *src, size_t bytes, uint32_t *flags, int n_flags, uint32_t value, hipStream_t s) {
-  hipLaunchKernelGGL(table_flag_kernel, dim3((unsigned)n_flags), dim3(256), 0, s, (uint4 *)dst, (const uint4 *)src,
-                     (int64_t)(bytes / 16), flags, value);
-  return hipGetLastError();
+  int64_t n16 = (int64_t)(bytes / 16);
+  void *args[] = {&dst, &src, &n16, &flags, &value};
+  // (This launch's own status, not an error that was left before: the caller counts on the flags if it succeeds.)
+  const hipError_t e = hipLaunchKernel((const void *)table_flag_kernel, dim3((unsigned)n_flags), dim3(256), args, 0, s);
+  if (e != hipSuccess) (void)hipGetLastError();
+  return e;
 }
 
 }  // namespace cas

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <chrono>
 #include <cmath>
 #include <cstring>
 #include <exception>
@@ -744,58 +745,112 @@ cas_status_t build_chunk(const cas_decode_problem_t *p, ChunkPlan &pl) {
   return CAS_OK;
 }
 
-// Pinned slots for launch tables on their way to a workspace, one ring per
-// device. A slot is free once the kernel that read it has set its flags.
-struct TableRing {
+// Pinned slots for launch tables on their way to a workspace. A slot is free once
+// the kernel that read it has set its flags.
+struct TableSlots {
   static constexpr int kSlots = 16, kFlags = 16;
   static constexpr size_t kFlagBytes = kSlots * kFlags * sizeof(uint32_t);
   char *host = nullptr;              // kSlots slots, then their flags
   size_t slot_bytes = 0;
   uint32_t want[kSlots] = {};        // value of the slot's flags when it is free
   int used[kSlots] = {};             // flags of the slot's last upload
+  bool taken[kSlots] = {};           // a thread is filling it
   int next = 0;
   uint32_t *flags(int i) const { return (uint32_t *)(host + kSlots * slot_bytes) + i * kFlags; }
-  void wait(int i) const {
+  bool free(int i) const {
+    if (taken[i]) return false;
     for (int f = 0; f < used[i]; ++f)
-      while (__atomic_load_n(flags(i) + f, __ATOMIC_ACQUIRE) != want[i]) std::this_thread::yield();
+      if (__atomic_load_n(flags(i) + f, __ATOMIC_ACQUIRE) != want[i]) return false;
+    return true;
   }
 };
-std::mutex g_tables_mu;
-std::map<int, TableRing> g_tables;
+
+// The slots of a device, of its largest tables so far; those of smaller tables
+// stay (less memory together than the current ones), since kernels may not have
+// read them yet and freeing pinned memory waits for them.
+struct TableRing {
+  std::mutex mu;
+  std::vector<std::unique_ptr<TableSlots>> slots;
+};
+
+TableRing &table_ring(int dev) {
+  static std::mutex mu;
+  static std::map<int, TableRing> rings;
+  std::lock_guard<std::mutex> lk(mu);
+  return rings[dev];
+}
+
+// A free slot of at least `bytes`, taken for the caller, or -1.
+cas_status_t take_slot(TableRing &r, size_t bytes, TableSlots *&s, int &slot) {
+  std::lock_guard<std::mutex> lk(r.mu);
+  slot = -1;
+  if (r.slots.empty() || bytes > r.slots.back()->slot_bytes) {
+    auto fresh = std::make_unique<TableSlots>();
+    fresh->slot_bytes = r.slots.empty() ? 64 << 10 : 2 * r.slots.back()->slot_bytes;
+    while (fresh->slot_bytes < bytes) fresh->slot_bytes *= 2;
+    r.slots.reserve(r.slots.size() + 1);
+    // Coherent: the kernel reads slots that the host has just rewritten, and the
+    // host the flags that it writes.
+    const size_t all = fresh->slot_bytes * TableSlots::kSlots;
+    const hipError_t e = hipHostMalloc((void **)&fresh->host, all + TableSlots::kFlagBytes, hipHostMallocCoherent);
+    if (e != hipSuccess) return set_hip_error("hipHostMalloc", e);
+    std::memset(fresh->host + all, 0, TableSlots::kFlagBytes);
+    r.slots.push_back(std::move(fresh));
+  }
+  s = r.slots.back().get();
+  for (int k = 0; k < TableSlots::kSlots && slot < 0; ++k) {
+    const int i = (s->next + k) % TableSlots::kSlots;
+    if (s->free(i)) slot = i;
+  }
+  if (slot >= 0) {
+    s->taken[slot] = true;
+    s->next = (slot + 1) % TableSlots::kSlots;
+  }
+  return CAS_OK;
+}
+
+// Tables as kernel arguments, 3.9 KiB to a launch.
+template <typename Fill>
+cas_status_t upload_as_arguments(size_t bytes, void *ws, hipStream_t stream, Fill &&fill) {
+  std::vector<char> h((bytes + 15) & ~(size_t)15, 0);
+  fill(h.data());
+  const hipError_t e = launch_table_args_upload(h.data(), h.size(), ws, stream);
+  return e == hipSuccess ? CAS_OK : set_hip_error("table upload launch", e);
+}
+
+// Copies launch tables through a pinned slot. With all slots on their way the host
+// is 16 calls ahead of the GPU and waits for the first of them, without the lock,
+// but no longer than kSlotWait: what they wait for may be work that this thread, or
+// one that waits with it, has yet to enqueue, and after a device error they never
+// end. Then the tables go as kernel arguments, whose launches (28 us more for 57 KB,
+// 12 us for 14 KB) are little beside a GPU that took that long for a call.
+constexpr std::chrono::microseconds kSlotWait{10000}, kSlotSpin{100}, kSlotSleep{50};
 
 template <typename Fill>
 cas_status_t upload_tables(size_t bytes, void *ws, hipStream_t stream, Fill &&fill) {
-  int dev = 0;
+  int dev = 0, slot = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return set_hip_error("hipGetDevice", e);
-  std::lock_guard<std::mutex> lk(g_tables_mu);
-  TableRing &r = g_tables[dev];
-  if (bytes > r.slot_bytes) {
-    size_t sb = 64 << 10;
-    while (sb < bytes) sb *= 2;
-    char *host = nullptr;
-    // Coherent: the kernel reads slots that the host has just rewritten, and the
-    // host the flags that it writes.
-    e = hipHostMalloc((void **)&host, sb * TableRing::kSlots + TableRing::kFlagBytes, hipHostMallocCoherent);
-    if (e != hipSuccess) return set_hip_error("hipHostMalloc", e);
-    for (int i = 0; r.host && i < TableRing::kSlots; ++i) r.wait(i);
-    char *old = r.host;
-    r = TableRing{};
-    r.host = host;
-    r.slot_bytes = sb;
-    std::memset(host + sb * TableRing::kSlots, 0, TableRing::kFlagBytes);
-    if (old && (e = hipHostFree(old)) != hipSuccess) return set_hip_error("hipHostFree", e);
+  TableRing &r = table_ring(dev);
+  TableSlots *s = nullptr;
+  cas_status_t st = take_slot(r, bytes, s, slot);
+  for (const auto t0 = std::chrono::steady_clock::now(); st == CAS_OK && slot < 0; st = take_slot(r, bytes, s, slot)) {
+    const auto waited = std::chrono::steady_clock::now() - t0;
+    if (waited >= kSlotWait) return upload_as_arguments(bytes, ws, stream, fill);
+    if (waited < kSlotSpin) std::this_thread::yield();
+    else std::this_thread::sleep_for(kSlotSleep);
   }
-  const int slot = r.next;
-  r.wait(slot);
-  char *h = r.host + (size_t)slot * r.slot_bytes;
+  if (st != CAS_OK) return st;
+  char *h = s->host + (size_t)slot * s->slot_bytes;
   fill(h);
-  const int n = (int)std::min<size_t>(TableRing::kFlags, (bytes + 4095) / 4096);
-  e = launch_table_flags(ws, h, bytes, r.flags(slot), n, r.want[slot] + 1, stream);
+  const int n = (int)std::min<size_t>(TableSlots::kFlags, (bytes + 4095) / 4096);
+  const uint32_t value = s->want[slot] + 1;
+  e = launch_table_flags(ws, h, bytes, s->flags(slot), n, value, stream);
+  std::lock_guard<std::mutex> lk(r.mu);
+  s->taken[slot] = false;
   if (e != hipSuccess) return set_hip_error("table upload launch", e);
-  ++r.want[slot];
-  r.used[slot] = n;
-  r.next = (slot + 1) % TableRing::kSlots;
+  s->want[slot] = value;
+  s->used[slot] = n;
   return CAS_OK;
 }
 
@@ -828,12 +883,8 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   if (stream && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
   const bool capturing = capture == hipStreamCaptureStatusActive;
   const TableUpload upload = [&](size_t bytes, void *dst, hipStream_t st, const std::function<void(char *)> &write) {
-    if (!capturing) return upload_tables(bytes, dst, st, write);
     // A graph keeps kernel arguments, but not what the pinned slots hold now.
-    std::vector<char> h((bytes + 15) & ~(size_t)15, 0);
-    write(h.data());
-    const hipError_t e = launch_table_args_upload(h.data(), h.size(), dst, st);
-    return e == hipSuccess ? CAS_OK : set_hip_error("table upload launch", e);
+    return capturing ? upload_as_arguments(bytes, dst, st, write) : upload_tables(bytes, dst, st, write);
   };
   const int64_t row = (int64_t)p->num_kv_heads * p->group_size * p->head_dim * 2, Tq = p->q_offsets[p->batch];
   for (const DecodePart &d : pl.decode) {
