@@ -443,9 +443,11 @@ typedef struct {
  * in one launch. dtype: a cas_dtype_t. positions: device array of `tokens` (at
  * most 2^24) int32 (any sign). inverse != 0 gives the gradient: the same with
  * -a, so that for y = R x and a gradient dy the call returns dx = R^T dy.
- * head_dim is 64 or 128; x and y are 16-byte aligned with strides of multiples of 16 bytes. An output may overlap
- * no other tensor of the call. Nothing is allocated and no workspace is used,
- * so the call can be captured into a HIP graph.
+ * head_dim is 64 or 128; x and y are 16-byte aligned with strides of multiples of
+ * 16 bytes. An output may overlap no other tensor of the call; rows or heads that
+ * interleave (slices of one projection's output, [tokens, Hq + 2 Hkv, d] or
+ * [tokens, heads, 3, d]) do not. Nothing is allocated and no workspace is used, so
+ * the call can be captured into a HIP graph.
  */
 cas_status_t cas_rope(const cas_rope_t *rope, int32_t dtype, int32_t head_dim, int64_t tokens, const int32_t *positions,
                       const cas_rope_tensor_t *tensors, int32_t n, int32_t inverse, void *hip_stream);

@@ -12,6 +12,7 @@
 #include <map>
 #include <memory>
 #include <mutex>
+#include <numeric>
 #include <string>
 #include <thread>
 #include <tuple>
@@ -59,10 +60,11 @@ DevRope dev_rope(const cas_rope_t *r, bool inverse) {
 }
 
 // What a strided [tokens, heads, head_dim] tensor covers, in bytes: rows of
-// `ext` bytes (of one or several heads or tokens), `stride` apart.
+// `ext` bytes (of one or several heads or tokens), `stride` apart, made of pieces of
+// `width` bytes (a head), `inner` apart (0: one piece).
 struct Footprint {
   uintptr_t base, end;
-  uint64_t stride, ext;
+  uint64_t stride, ext, inner, width;
   bool distinct;   // no two elements share an address
 };
 
@@ -75,20 +77,33 @@ Footprint footprint(const void *x, int64_t tokens, int64_t heads, int64_t st, in
   const int64_t in = n_inner > 1 ? inner : 0, out = n_outer > 1 ? outer : 0;
   Footprint f;
   f.base = (uintptr_t)x;
-  f.ext = (uint64_t)((n_inner - 1) * in + D) * es;
+  f.width = (uint64_t)D * es;
+  f.inner = (uint64_t)in * es;
+  f.ext = (uint64_t)(n_inner - 1) * f.inner + f.width;
   f.stride = (uint64_t)out * es;
   f.end = f.base + (uint64_t)(n_outer - 1) * f.stride + f.ext;
   f.distinct = (n_inner == 1 || in >= D) && (n_outer == 1 || f.stride >= f.ext);
   return f;
 }
 
+// The footprint of `bytes` bytes in a row.
+Footprint span_of(const void *x, uint64_t bytes) {
+  return Footprint{(uintptr_t)x, (uintptr_t)x + bytes, 0, bytes, 0, bytes, true};
+}
+
 // Two tensors that share a range of addresses are still apart when their rows
-// interleave (slices of one projection's output).
+// interleave (slices of one projection's output, [tokens, Hq + 2 Hkv, d]), or their
+// heads do ([tokens, heads, 3, d]): counted modulo a step that divides all their
+// strides, every row (or head) of a tensor lies in the same place.
 bool apart(const Footprint &a, const Footprint &b) {
   if (a.end <= b.base || b.end <= a.base) return true;
-  if (a.stride != b.stride || a.stride == 0 || a.ext > a.stride || b.ext > a.stride) return false;
-  const uint64_t S = a.stride, delta = b.base >= a.base ? (b.base - a.base) % S : (S - (a.base - b.base) % S) % S;
-  return delta >= a.ext && delta + b.ext <= S;
+  auto modulo = [&](uint64_t step, uint64_t wa, uint64_t wb) {
+    if (step == 0) return false;
+    const uint64_t delta = b.base >= a.base ? (b.base - a.base) % step : (step - (a.base - b.base) % step) % step;
+    return delta >= wa && delta + wb <= step;
+  };
+  const uint64_t rows = std::gcd(a.stride, b.stride);
+  return modulo(rows, a.ext, b.ext) || modulo(std::gcd(rows, std::gcd(a.inner, b.inner)), a.width, b.width);
 }
 
 constexpr int64_t kMaxStride = (int64_t)1 << 31;   // (with the limits on tokens and heads, spans fit 64 bits)
@@ -144,9 +159,7 @@ cas_status_t rope_call(const cas_rope_t *rope, int32_t dtype, int32_t D, int64_t
     p.t[i] = DevRopeTensor{t.x, t.y, t.x_stride_tok, t.x_stride_head, t.y_stride_tok, t.y_stride_head, t.heads,
                             head_slots(tokens, D, es, t.heads)};
   }
-  const Footprint pos{(uintptr_t)positions, (uintptr_t)positions + (uintptr_t)tokens * 4, 0, (uint64_t)tokens * 4, true};
-  const Footprint turns{(uintptr_t)rope->turns, (uintptr_t)rope->turns + (uintptr_t)rope->rotary_dim * 4, 0,
-                        (uint64_t)rope->rotary_dim * 4, true};
+  const Footprint pos = span_of(positions, (uint64_t)tokens * 4), turns = span_of(rope->turns, (uint64_t)rope->rotary_dim * 4);
   for (int i = 0; i < n; ++i) {
     auto refuse = [&](const std::string &what) {
       return set_error(CAS_ERR_INVALID_ARGUMENT, "tensor " + str(i) + ": y overlaps " + what);
