@@ -393,8 +393,10 @@ int32_t cas_paged_decode_plan_matches(const cas_decode_plan_t *plan, const cas_d
  *   (x, y) -> scale (x cos a - y sin a, x sin a + y cos a).
  * The pair is channels (i, rotary_dim/2 + i) in the HALF layout and (2i, 2i+1)
  * in the INTERLEAVED one; the channels from rotary_dim on are copied. The
- * angle is taken modulo a turn in double precision (far positions lose
- * nothing); cos, sin and the products are fp32, rounded once to the dtype.
+ * angle is taken modulo a turn in double precision with the exact product, so at any
+ * int32 position it is that of the given turns (whose own rounding to doubles is up
+ * to 2^-53 of the whole angle, 2.4e-7 at 2^31 radians); cos, sin and the products
+ * are fp32, rounded once to the dtype.
  *
  * turns: device array of rotary_dim / 2 doubles, 8-byte aligned, which
  *   cas_rope_frequencies fills in host memory, or any others.

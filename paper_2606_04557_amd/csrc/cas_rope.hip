@@ -25,12 +25,13 @@ namespace {
 
 constexpr int kRopeThreads = 256;
 
-// cos and sin of t turns. The turns are reduced in double precision (exact up to
-// 2^52 of them), so what is left, at most an eighth of a turn, is rounded to
-// fp32 once; there the Taylor series are within 2e-9 (sin, to a^9) and 1e-10
-// (cos, to a^10).
-__device__ __forceinline__ void cos_sin_turns(double t, float &c, float &s) {
-  t -= __builtin_rint(t);
+// cos and sin of position * turn turns. Whole turns are taken off with the exact
+// product (one fused multiply-add in double precision: a rounded one would be off by
+// up to 2^-53 of the whole angle, 2.4e-7 at 2^31 radians), so what is left, at most an
+// eighth of a turn, is rounded to fp32 once; there the Taylor series are within 2e-9
+// (sin, to a^9) and 1e-10 (cos, to a^10).
+__device__ __forceinline__ void cos_sin_turns(double position, double turn, float &c, float &s) {
+  const double t = __builtin_fma(position, turn, -__builtin_rint(position * turn));
   const double q = __builtin_rint(4.0 * t);
   const float a = (float)((t - 0.25 * q) * 6.283185307179586477);
   const float z = a * a;
@@ -84,7 +85,7 @@ struct RopeUnit {
     if (!rot) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      cos_sin_turns((double)position * r.turns[8 * u + e], c[e], s[e]);
+      cos_sin_turns((double)position, r.turns[8 * u + e], c[e], s[e]);
       c[e] *= r.scale;
       s[e] *= r.inverse ? -r.scale : r.scale;
     }
