@@ -115,8 +115,8 @@ int hipLaunchKernel(const void *f, Dim3 grid, Dim3 block, void **args, size_t, v
 
 namespace {
 
-decltype(&cas_paged_chunk_fwd) chunk_fwd;
-decltype(&cas_paged_chunk_workspace_size) chunk_size;
+decltype(&cas_paged_chunk_plan_create) plan_create;
+decltype(&cas_paged_chunk_run) chunk_run;
 decltype(&cas_last_error_message) last_error;
 
 #define CHECK(x)                                                                         \
@@ -130,8 +130,9 @@ decltype(&cas_last_error_message) last_error;
 struct Case {
   std::vector<int32_t> q{0}, kv, po{0}, ids;
   cas_decode_problem_t p;
-  size_t bytes = 0;
-  std::vector<char> first;   // workspace of the first call
+  cas_chunk_plan_t *plan = nullptr;
+  size_t bytes = 0, tables = 0;   // of the workspace, and of its start, which holds the tables
+  std::vector<char> first;        // that start after the first call
 
   Case(int batch, int keys) {
     for (int b = 0; b < batch; ++b) {
@@ -152,19 +153,23 @@ struct Case {
     p.kv_lens = kv.data();
     p.page_offsets = po.data();
     p.page_ids = ids.data();
-    CHECK(chunk_size(&p, &bytes) == CAS_OK && bytes > 4096);
+    CHECK(plan_create(&p, &plan, &bytes) == CAS_OK && bytes > 4096);
+    tables = bytes < (512 << 10) ? bytes : 512 << 10;
   }
-  // One call on the current device; its workspace holds the same as after the first call.
+  // One call on the current device; its workspace holds the same tables as after the first call.
   cas_status_t call() {
-    std::vector<char> ws(bytes + 256, 0);
+    thread_local std::map<const Case *, std::vector<char>> workspaces;
+    std::vector<char> &ws = workspaces[this];
+    if (ws.empty()) ws.resize(bytes + 256);
     char *at = (char *)(((uintptr_t)ws.data() + 255) & ~(uintptr_t)255);
+    memset(at, 0, tables);
     const uintptr_t far = (uintptr_t)1 << 44;   // (never touched)
-    const cas_status_t s = chunk_fwd(&p, (void *)far, (void *)(2 * far), (void *)(3 * far), (void *)(4 * far), nullptr, at, bytes,
+    const cas_status_t s = chunk_run(plan, (void *)far, (void *)(2 * far), (void *)(3 * far), (void *)(4 * far), nullptr, at, bytes,
                                      (void *)0x10);
     if (s == CAS_OK) {
       std::lock_guard<std::mutex> lk(mu);
-      if (first.empty()) first.assign(at, at + bytes);
-      CHECK(memcmp(first.data(), at, bytes) == 0);
+      if (first.empty()) first.assign(at, at + tables);
+      CHECK(memcmp(first.data(), at, tables) == 0);
     }
     return s;
   }
@@ -177,10 +182,10 @@ int main(int argc, char **argv) {
   void *lib = dlopen(argv[1], RTLD_NOW | RTLD_GLOBAL);
   if (!lib) fprintf(stderr, "%s\n", dlerror());
   CHECK(lib);
-  chunk_fwd = (decltype(chunk_fwd))dlsym(lib, "cas_paged_chunk_fwd");
-  chunk_size = (decltype(chunk_size))dlsym(lib, "cas_paged_chunk_workspace_size");
+  plan_create = (decltype(plan_create))dlsym(lib, "cas_paged_chunk_plan_create");
+  chunk_run = (decltype(chunk_run))dlsym(lib, "cas_paged_chunk_run");
   last_error = (decltype(last_error))dlsym(lib, "cas_last_error_message");
-  CHECK(chunk_fwd && chunk_size && last_error);
+  CHECK(plan_create && chunk_run && last_error);
   const std::string scenario = argv[2];
   Case small(20, 1000), large(60, 20000);   // (tables of about 12 KB and 330 KB)
   if (scenario == "usual") {
@@ -206,7 +211,8 @@ int main(int argc, char **argv) {
     for (int i = 0; i < 40; ++i) CHECK(small.call() == CAS_OK);
     CHECK(by_slot == 41 && by_argument == 0);
   } else if (scenario == "devices") {
-    // One device whose uploads never end does not hold up another.
+    // One device whose uploads never end does not hold up another (100 calls there take a few ms, the
+    // waiting thread's 10 ms each).
     stuck[0] = true;
     std::atomic<int> calls{0};
     std::atomic<bool> full{false}, done{false};
