@@ -462,7 +462,9 @@ class Rope:
     "interleaved" 2i and 2i + 1. ``frequencies`` (rotary_dim/2 radians per
     position) and ``scale`` (on cos and sin) stand in for what base and scaling
     give. The frequencies are copied to a GPU by the first call there (before a
-    graph is captured: call it, or device_turns, once)."""
+    graph is captured: call it, or device_turns, once). The object outlives the
+    graphs that were captured with it, and is outlived by the streams that it was
+    used on, whose work its memory waits for."""
 
     _LAYOUTS = {"half": _lib.CAS_ROPE_HALF, "interleaved": _lib.CAS_ROPE_INTERLEAVED}
     _KINDS = {"linear": _lib.CAS_ROPE_LINEAR, "ntk": _lib.CAS_ROPE_NTK, "by_parts": _lib.CAS_ROPE_BY_PARTS}

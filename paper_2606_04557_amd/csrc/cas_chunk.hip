@@ -14,9 +14,11 @@
 // the host makes equally long for all compute units.
 //
 // Bound by the matrix cores: 2,048 tokens of 32 heads over 18 to 20 thousand keys
-// (8 KV heads of 128) take 535 us, 1,220 TFLOP/s where an 8,192^3 library product
-// reaches 1,208; a 64-key tile of 256 rows takes 1.75 us. With d = 64 it is the
-// softmax (the same exponentials for half the products): 1.15 us. A block of at
+// (8 KV heads of 128) take 539 us a call in a long run of them, 1,212 TFLOP/s where an
+// 8,192^3 library product reaches 1,388; in turn with it at any pace (10 to 400 calls
+// in a row, which change the clock) 0.87 to 0.90 of its rate. A 64-key tile of 256 rows
+// takes 1.75 us. With d = 64 it is the softmax (the same exponentials for half the
+// products): 1.15 us. A block of at
 // most 64 rows would leave most waves idle and one wave's chain of dependent steps
 // would set the pace (1.08 us a tile of 32 rows), so there the waves divide the keys
 // (0.47 us), as far as memory brings them.

@@ -430,13 +430,15 @@ struct ChunkPlan {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Costs, in 64-key tiles of 256 rows with d = 128 (1.75 us). Fewer rows cost
-// more than their share (a phase waits for its copies and barriers): 1.20 us for
-// 96, 1.25 for 128; with d = 64 0.87, 0.89 and 1.22. Up to kChunkNarrowRows of
+// more than their share (a phase waits for its copies and barriers): measured 1.20 us
+// for 96 and 1.25 for 128, with d = 64 0.87, 0.89 and 1.22 for 256; the lines through
+// them here give 1.28, 1.37, 0.93, 1.00 and 1.26. Up to kChunkNarrowRows of
 // them the kernel's waves divide the keys: 0.47 us for 32 rows and 0.92 for 64
 // (d = 64: 0.26 and 0.52) where the keys are in the L2, as those of a request with
-// several blocks are, `shared`; else most come from HBM, 0.75 us a tile where every
-// unit asks for some (with 0.47 a batch of 16 single tokens beside a chunk took 106
-// us, with 0.75 93). kWgCost: what a workgroup costs beside its tiles (dispatch,
+// several blocks are, `shared`; else most come from HBM and are priced at what that
+// takes where every unit asks for some, 0.79 us for 32 rows and 1.05 for 64 (0.44 and
+// 0.58): with 0.47 a batch of 16 single tokens beside a chunk took 106 us, with 0.79
+// 93. kWgCost: what a workgroup costs beside its tiles (dispatch,
 // first loads, pipeline fill and drain, epilogue), kItemCost: a further item of a
 // workgroup; kMergeCost: a merge's launch; the partials' bytes, written and read, at
 // kBytesPerTile. (Over 30 mixes, each of them 20-50 % higher or lower changes the
