@@ -122,3 +122,49 @@ def test_frequencies_outlive_every_call_that_reads_them(cas, monkeypatch):
     assert not failed, failed
     assert len(uploads) == 2 and read == [True, True]
     assert sum(ref() is not None for _, ref in uploads) == 1   # (one is kept)
+
+
+@pytest.mark.gpu
+def test_first_calls_of_threads_on_the_gpu(gpu_lib):
+    """Four threads whose first calls on one problem and one Rope come together, each
+    with its own stream and pools: the bits of calls one after the other."""
+    import threading
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda").to(torch.bfloat16)
+    counts, kv, pages, n = [], [], [], 0
+    for b in range(30):
+        counts.append(1 + b % 7)
+        kv.append(counts[-1] + 61 * b)
+        pages.append(list(range(n, n + -(-kv[-1] // 16))))
+        n += len(pages[-1])
+    T = sum(counts)
+    x, base = rand(T, 12, 64), [rand(n, 16, 2, 64) for _ in range(2)]
+    q, k, v = x[:, :8], x[:, 8:10], x[:, 10:]
+
+    def step(problem, rope, pools, stream):
+        rotated = gpu_lib.paged_append(k, v, *pools, problem, rope=rope, q=q, stream=stream)
+        return gpu_lib.paged_chunk_fwd(rotated, *pools, problem, stream=stream)
+    make = lambda: (gpu_lib.DecodeProblem(counts, kv, pages, n, 16, 2, 4, 64, 0.125), gpu_lib.Rope(64, 1e4))
+    pools = [[p.clone() for p in base] for _ in range(5)]
+    want = step(*make(), pools[4], None)
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i, problem, rope, start):
+        try:
+            s = torch.cuda.Stream()
+            start.wait(30)
+            got = step(problem, rope, pools[i], s)
+            s.synchronize()
+            if not all(torch.equal(a, b) for a, b in zip((*got, *pools[i]), (*want, *pools[4]))):
+                bad.append(i)
+        except BaseException as e:   # noqa: BLE001
+            bad.append(e)
+    for _ in range(10):
+        start, shared = threading.Barrier(4), make()
+        threads = [threading.Thread(target=work, args=(i, *shared, start)) for i in range(4)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not bad, bad
