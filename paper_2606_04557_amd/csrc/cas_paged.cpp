@@ -834,25 +834,27 @@ cas_status_t upload_as_arguments(size_t bytes, void *ws, hipStream_t stream, Fil
 }
 
 // Copies launch tables through a pinned slot. With all slots on their way the host
-// is 16 calls ahead of the GPU and waits for the first of them, without the lock,
-// but no longer than kSlotWait: what they wait for may be work that this thread, or
+// is 16 tables ahead of the GPU and waits for the first of them, without the lock,
+// but no longer than until its call's deadline, kSlotWait: what they wait for may be work that this thread, or
 // one that waits with it, has yet to enqueue, and after a device error they never
 // end. Then the tables go as kernel arguments, whose launches (28 us more for 57 KB,
 // 12 us for 14 KB) are little beside a GPU that took that long for a call.
 constexpr std::chrono::microseconds kSlotWait{10000}, kSlotSpin{100}, kSlotSleep{50};
 
+using Clock = std::chrono::steady_clock;
+
 template <typename Fill>
-cas_status_t upload_tables(size_t bytes, void *ws, hipStream_t stream, Fill &&fill) {
+cas_status_t upload_tables(size_t bytes, void *ws, hipStream_t stream, Clock::time_point deadline, Fill &&fill) {
   int dev = 0, slot = -1;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return set_hip_error("hipGetDevice", e);
   TableRing &r = table_ring(dev);
   TableSlots *s = nullptr;
   cas_status_t st = take_slot(r, bytes, s, slot);
-  for (const auto t0 = std::chrono::steady_clock::now(); st == CAS_OK && slot < 0; st = take_slot(r, bytes, s, slot)) {
-    const auto waited = std::chrono::steady_clock::now() - t0;
-    if (waited >= kSlotWait) return upload_as_arguments(bytes, ws, stream, fill);
-    if (waited < kSlotSpin) std::this_thread::yield();
+  for (const auto t0 = Clock::now(); st == CAS_OK && slot < 0; st = take_slot(r, bytes, s, slot)) {
+    const auto now = Clock::now();
+    if (now >= deadline) return upload_as_arguments(bytes, ws, stream, fill);
+    if (now - t0 < kSlotSpin) std::this_thread::yield();
     else std::this_thread::sleep_for(kSlotSleep);
   }
   if (st != CAS_OK) return st;
@@ -897,9 +899,10 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
   hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
   if (stream && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
   const bool capturing = capture == hipStreamCaptureStatusActive;
+  const Clock::time_point deadline = Clock::now() + kSlotWait;
   const TableUpload upload = [&](size_t bytes, void *dst, hipStream_t st, const std::function<void(char *)> &write) {
     // A graph keeps kernel arguments, but not what the pinned slots hold now.
-    return capturing ? upload_as_arguments(bytes, dst, st, write) : upload_tables(bytes, dst, st, write);
+    return capturing ? upload_as_arguments(bytes, dst, st, write) : upload_tables(bytes, dst, st, deadline, write);
   };
   const int64_t row = (int64_t)p->num_kv_heads * p->group_size * p->head_dim * 2, Tq = p->q_offsets[p->batch];
   for (const DecodePart &d : pl.decode) {
