@@ -52,7 +52,8 @@ typedef enum {
   CAS_ERR_NOT_PINNED = 4,       /* staging source is pageable host memory */
   CAS_ERR_WORKSPACE = 5,        /* workspace NULL or smaller than the size query returned */
   CAS_ERR_HIP = 6,              /* a HIP runtime call failed; see cas_last_error_message */
-  CAS_ERR_IO = 7                /* a file operation of the pool's moment tier failed */
+  CAS_ERR_IO = 7,               /* a file operation of the pool's moment tier failed */
+  CAS_ERR_PAGES = 8             /* a page table has fewer free pages than the call needs */
 } cas_status_t;
 
 typedef enum {
@@ -553,6 +554,143 @@ typedef struct {
 } cas_chunk_plan_info_t;
 
 cas_status_t cas_paged_chunk_plan_info(const cas_chunk_plan_t *plan, cas_chunk_plan_info_t *info, int32_t *items);
+
+/*
+ * Pages of the cache. A page table says which pages of the paged cache (page_ids
+ * of cas_decode_problem_t) hold whose keys: sequences are lists of pages with a
+ * length, which share pages by reference (paper: Section "Inference" and
+ * paragraph "Cartridge RAG", requests over the same retrieved cartridges; the
+ * beams of a request over its prompt), and a page is free when no sequence has
+ * it. Host only: what has to move on the GPU comes back as a list for
+ * cas_pages_copy, which the caller enqueues before whatever writes or reads the
+ * pages next, in the order of the calls.
+ *
+ * Sequences are named by ids that are not given out again. New pages are the
+ * free ones with the lowest ids. Calls on one table must not overlap. On an error
+ * the table stays as it was; CAS_ERR_PAGES: too few pages are free.
+ */
+typedef struct cas_page_table cas_page_table_t;
+
+/* The first `rows` rows (tokens) of page src go to those of page dst. */
+typedef struct {
+  int32_t src, dst, rows;
+} cas_page_copy_t;
+
+typedef struct {
+  int64_t sequences;
+  int64_t pages_used;   /* by one sequence or more */
+  int64_t pages_free;
+  int64_t pages_end;    /* one past the highest page in use: a pool of that many pages holds everything */
+} cas_page_table_info_t;
+
+/* page_size is 16, 32, 64 or 128, num_pages in [1, 2^31). */
+cas_status_t cas_page_table_create(int64_t num_pages, int32_t page_size, cas_page_table_t **table);
+cas_status_t cas_page_table_destroy(cas_page_table_t *table);
+cas_status_t cas_page_table_info(const cas_page_table_t *table, cas_page_table_info_t *info);
+
+/* A new sequence of the keys of n others, one behind the other, by reference: none (an empty sequence), one (a fork of it,
+ * whatever its length), or several (cartridges ahead of a prompt), each of which but the last fills whole pages. */
+cas_status_t cas_page_table_add(cas_page_table_t *table, const int64_t *parts, int32_t n, int64_t *seq);
+/* Room for counts[i] >= 0 more keys at the end of each of n different sequences. Where they begin in a page that another
+ * sequence has, too, the sequence gets a page of its own for it and copies[] an entry (room for n of them). */
+cas_status_t cas_page_table_extend(cas_page_table_t *table, const int64_t *seqs, int32_t n, const int32_t *counts,
+                                   cas_page_copy_t *copies, int32_t *n_copies);
+/* Each of n different sequences gets the keys that seqs[parents[i]] has before the call, by reference (beams that go on
+ * from others). */
+cas_status_t cas_page_table_reorder(cas_page_table_t *table, const int64_t *seqs, int32_t n, const int32_t *parents);
+/* Leaves a sequence its first len keys. */
+cas_status_t cas_page_table_truncate(cas_page_table_t *table, int64_t seq, int64_t len);
+/* Removes n different sequences. */
+cas_status_t cas_page_table_free(cas_page_table_t *table, const int64_t *seqs, int32_t n);
+/* Moves at most `most` pages, highest first, to free ones below them, until the pages in use are the lowest ones. copies
+ * (room for `most` entries) are the moves, of the rows that hold keys. Page lists from before the call are void. */
+cas_status_t cas_page_table_compact(cas_page_table_t *table, int32_t most, cas_page_copy_t *copies, int32_t *n_copies);
+/* The tables of cas_decode_problem_t for n sequences (one may come several times): kv_lens [n], page_offsets [n + 1], and
+ * page_ids, unless NULL, of room for cap ids (ask for page_offsets first). */
+cas_status_t cas_page_table_lists(const cas_page_table_t *table, const int64_t *seqs, int32_t n, int32_t *kv_lens,
+                                  int32_t *page_offsets, int32_t *page_ids, int64_t cap);
+
+/*
+ * Copies rows of pages within each of n_pools pools (K and V of every layer): pools
+ * are device pointers to [num_pages, page_size, row_bytes] bytes, contiguous,
+ * 16-byte aligned, row_bytes a multiple of 16 (num_kv_heads * head_dim elements
+ * of any type). All copies are made as if at once: a page that is written is named
+ * once, and read by no copy of the call. Pages and rows that the list does not
+ * name stay as they are; rows behind a copy's `rows` too.
+ *
+ * The copies are host memory, read during the call. Up to 240 travel as kernel
+ * arguments. The list of more goes through a workspace of the size that
+ * cas_pages_copy_workspace_size gives for n copies (0 up to 240, where NULL will
+ * do); calls that run at the same time need a workspace each, as do captured
+ * graphs that may.
+ */
+cas_status_t cas_pages_copy_workspace_size(int32_t n, size_t *bytes);
+cas_status_t cas_pages_copy(void *const *pools, int32_t n_pools, int64_t num_pages, int32_t page_size, int64_t row_bytes,
+                            const cas_page_copy_t *copies, int32_t n, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * A step of beam search: of the candidates of a batch entry, every token after
+ * every one of its beams, the k with the best scores. For beam i with the logits x,
+ *   score(i, v) = scores[i] + (x_v - max x) - ln sum_w exp(x_w - max x).
+ * A beam with finished[i] != 0 has one candidate, pad_token at the score that it
+ * has, and its logits are not read. Every other candidate's score is -inf: those
+ * of a finished beam, of tokens whose logit is -inf (that the caller rules out),
+ * and of a beam without anything to choose from: one whose own score is not
+ * finite, whose logits are all -inf, or among whose logits is a NaN or +inf (such a
+ * beam leaves the search; the others of the batch entry go on).
+ *
+ * Candidates are ordered by their exact scores (compared in 64 bits where
+ * 32 do not tell them apart), equal ones by beam and then token, lowest first;
+ * out_scores are rounded once. Should there be fewer than k above -inf, the
+ * others follow in that order with the score -inf: parents and tokens are always
+ * in range.
+ *
+ * logits: [batch, beams, vocab] bf16 or fp32, device memory, aligned to its type,
+ *   rows row_stride >= vocab elements apart (any number: columns behind vocab are not read).
+ * scores: [batch, beams] fp32: sums of the tokens' log-probabilities so far (a
+ *   request's first step: 0 for one beam and -inf for the others).
+ * finished: [batch, beams] bytes, or NULL: none is.
+ * out_scores (fp32), out_parents (the beam, 0 .. beams - 1) and out_tokens
+ *   (int32): [batch, k].
+ * beams and k are at most 64, k at most beams * vocab, vocab at most 2^30, batch * beams
+ * at most 2^20. Outputs may not overlap the inputs or each other. The workspace is
+ * 16-byte aligned; calls that run at the same time need one each.
+ */
+typedef struct {
+  int32_t dtype;        /* of the logits: a cas_dtype_t */
+  int32_t batch;        /* >= 0 */
+  int32_t beams;
+  int32_t k;
+  int64_t vocab;
+  int64_t row_stride;
+  int32_t pad_token;    /* in [0, vocab) */
+} cas_beam_problem_t;
+
+cas_status_t cas_beam_select_workspace_size(const cas_beam_problem_t *p, size_t *bytes);
+cas_status_t cas_beam_select(const cas_beam_problem_t *p, const void *logits, const float *scores, const uint8_t *finished,
+                             float *out_scores, int32_t *out_parents, int32_t *out_tokens, void *workspace, size_t ws_bytes,
+                             void *hip_stream);
+
+/*
+ * States that are kept per beam (token histories, dense caches) follow the
+ * surviving beams: for every batch entry b and j < beams_out,
+ *   y[b, j] = x[b, parents[b, j]],
+ * for 1 to 8 tensors in one launch. parents: device array [batch, beams_out] of
+ * beams of the same batch entry, 0 .. beams_in - 1; a row with any other parent is
+ * left as it was. A row is row_bytes bytes (0 allowed) in a row; strides are
+ * bytes, of any alignment (16 is the fastest; the rest of a row goes byte by byte). beams_in
+ * and beams_out are at most 64. y == x with equal strides and beams_in ==
+ * beams_out reorders in place; any other overlap is refused.
+ */
+typedef struct {
+  const void *x;
+  void *y;
+  int64_t row_bytes;
+  int64_t x_stride_batch, x_stride_beam, y_stride_batch, y_stride_beam;
+} cas_beam_state_t;
+
+cas_status_t cas_beam_reorder(const int32_t *parents, int32_t batch, int32_t beams_in, int32_t beams_out,
+                              const cas_beam_state_t *states, int32_t n, void *hip_stream);
 
 /*
  * Budget manager (paper: paragraphs "Budget Manager" and "Pool rotation";

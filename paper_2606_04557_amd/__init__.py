@@ -24,7 +24,8 @@ __all__ = ["Segment", "Problem", "CasError", "load", "prefix_attn_fwd", "prefix_
            "timing_enable", "timing_reset", "timing_read", "AdamCartridge", "adam_lr_scale",
            "cartridge_adam", "DecodeProblem", "paged_decode_fwd", "decode_plan", "plan_rotation", "CartridgePool",
            "Rope", "RopeScaling", "rope_fwd", "rope_bwd", "paged_append", "paged_chunk_fwd",
-           "paged_chunk_workspace_size", "chunk_plan"]
+           "paged_chunk_workspace_size", "chunk_plan", "PageTable", "PagePools", "pages_copy", "beam_select",
+           "beam_select_workspace_size", "beam_reorder"]
 
 
 class CasError(RuntimeError):
@@ -386,11 +387,27 @@ class DecodeProblem:
             ids = [int(x) for pl in page_lists for x in pl]
         self._ids = (ctypes.c_int32 * max(len(ids), 1))(*ids) if not isinstance(ids, array.array) or not ids else \
             (ctypes.c_int32 * len(ids)).from_buffer(ids)
+        self._finish(B, num_pages, page_size, num_kv_heads, group_size, head_dim, softmax_scale)
+
+    def _finish(self, B, num_pages, page_size, num_kv_heads, group_size, head_dim, softmax_scale) -> None:
         self._plan = self._append_plan = self._chunk_plan = None
         I = ctypes.POINTER(ctypes.c_int32)
         self.c = _lib.DecodeProblem(B, num_kv_heads, group_size, head_dim, float(softmax_scale), page_size,
                                     int(num_pages), ctypes.cast(self._qo, I), ctypes.cast(self._kv, I),
                                     ctypes.cast(self._po, I), ctypes.cast(self._ids, I))
+
+    @classmethod
+    def from_tables(cls, q_counts: Sequence[int], kv_lens, page_offsets, page_ids, num_pages: int, page_size: int,
+                    num_kv_heads: int, group_size: int, head_dim: int, softmax_scale: float) -> DecodeProblem:
+        """A problem on C int32 arrays as PageTable.lists returns them, which it keeps."""
+        B = len(q_counts)
+        if len(page_offsets) != B + 1:
+            raise ValueError("one query count per sequence")
+        self = cls.__new__(cls)
+        self._qo = (ctypes.c_int32 * (B + 1))(0, *itertools.accumulate(int(n) for n in q_counts))
+        self.Tq, self._kv, self._po, self._ids = self._qo[B], kv_lens, page_offsets, page_ids
+        self._finish(B, num_pages, page_size, num_kv_heads, group_size, head_dim, softmax_scale)
+        return self
 
     def plan(self) -> _DecodePlan:
         # (Threads that plan at the same time each have a plan; one of them is kept.)
@@ -766,6 +783,304 @@ def chunk_plan(problem: DecodeProblem):
             wgs[-1].append(items[i])
             i = items[i][9]
     return info, wgs
+
+
+# ---------------------------------------------------------------------------
+# Pages of the cache: who has which, and copies between them
+# ---------------------------------------------------------------------------
+def _ints(kind: str, values) -> Tuple[array.array, int]:
+    """An array of C integers ("i" or "q") and its address."""
+    a = array.array(kind, values)
+    return a, a.buffer_info()[0]
+
+
+class PageTable:
+    """Which sequences have which pages of the paged cache (cas_page_table_t; host
+    only). Sequences share pages by reference: a request over retrieved cartridges
+    is ``add(cartridges)``, a beam ``fork(request)``. Calls that move something
+    on the GPU return their copies, an int32 array [n, 3] of source page,
+    destination page and rows, for pages_copy, which comes before whatever uses
+    the pages next. Calls on one table must not overlap."""
+
+    def __init__(self, num_pages: int, page_size: int = 16):
+        h = ctypes.c_void_p()
+        _check(load().cas_page_table_create(int(num_pages), int(page_size), ctypes.byref(h)))
+        self.h, self._destroy = h, load().cas_page_table_destroy
+        self.num_pages, self.page_size = int(num_pages), int(page_size)
+
+    def __del__(self):
+        if getattr(self, "h", None):
+            self._destroy(self.h)
+
+    def info(self) -> dict:
+        """sequences, pages_used, pages_free, and pages_end (one past the highest page in use)."""
+        i = _lib.PageTableInfo()
+        _check(load().cas_page_table_info(self.h, ctypes.byref(i)))
+        return {f: getattr(i, f) for f, _ in i._fields_}
+
+    def add(self, parts: Sequence[int] = (), tokens: int = 0) -> int:
+        """A new sequence of the parts' keys, one behind the other (all but the last
+        part fill whole pages), and with room for ``tokens`` more behind whole pages."""
+        a, at = _ints("q", parts)
+        seq = ctypes.c_int64()
+        _check(load().cas_page_table_add(self.h, at, len(a), ctypes.byref(seq)))
+        if tokens:
+            try:
+                if len(self.extend([seq.value], [tokens])):
+                    raise ValueError("tokens behind a part that ends inside a page: extend the sequence, and run its copies")
+            except BaseException:
+                self.free([seq.value])
+                raise
+        return seq.value
+
+    def fork(self, seq: int, n: int = 1) -> List[int]:
+        """n new sequences of the keys of one."""
+        return [self.add([seq]) for _ in range(n)]
+
+    def extend(self, seqs: Sequence[int], counts: Sequence[int]):
+        """Room for counts[i] more keys at the end of each sequence; returns the copies
+        of last pages that others have, too (of several such sequences one keeps it)."""
+        import numpy as np
+        a, at = _ints("q", seqs)
+        c, ct = _ints("i", counts)
+        if len(a) != len(c):
+            raise ValueError("one count per sequence")
+        copies, n = np.empty((len(a), 3), dtype=np.int32), ctypes.c_int32(0)
+        _check(load().cas_page_table_extend(self.h, at, len(a), ct, copies.ctypes.data, ctypes.byref(n)))
+        return copies[:n.value]
+
+    def reorder(self, seqs: Sequence[int], parents: Sequence[int]) -> None:
+        """Each sequence i gets the keys that seqs[parents[i]] has before the call."""
+        a, at = _ints("q", seqs)
+        p, pt = _ints("i", parents)
+        if len(a) != len(p):
+            raise ValueError("one parent per sequence")
+        _check(load().cas_page_table_reorder(self.h, at, len(a), pt))
+
+    def truncate(self, seq: int, length: int) -> None:
+        """Leaves the sequence its first ``length`` keys."""
+        _check(load().cas_page_table_truncate(self.h, int(seq), int(length)))
+
+    def free(self, seqs: Sequence[int]) -> None:
+        a, at = _ints("q", seqs)
+        _check(load().cas_page_table_free(self.h, at, len(a)))
+
+    def compact(self, most: Optional[int] = None):
+        """Moves the highest pages (at most ``most``) to free ones below; returns the
+        copies. Problems made before are void."""
+        import numpy as np
+        most = self.num_pages if most is None else int(most)
+        if most < 0:
+            raise ValueError("most must be >= 0")
+        i = self.info()   # (no more pages move than are free below the end)
+        most = min(most, i["pages_end"] - i["pages_used"])
+        copies, n = np.empty((most, 3), dtype=np.int32), ctypes.c_int32(0)
+        _check(load().cas_page_table_compact(self.h, most, copies.ctypes.data, ctypes.byref(n)))
+        return copies[:n.value]
+
+    def lists(self, seqs: Sequence[int]):
+        """(lengths, page offsets, page ids) of the sequences, int32 arrays."""
+        a, at = _ints("q", seqs)
+        n = len(a)
+        lens, offsets = (ctypes.c_int32 * max(n, 1))(), (ctypes.c_int32 * (n + 1))()
+        _check(load().cas_page_table_lists(self.h, at, n, lens, offsets, None, 0))
+        ids = (ctypes.c_int32 * max(offsets[n], 1))()
+        _check(load().cas_page_table_lists(self.h, at, n, lens, offsets, ids, len(ids)))
+        return lens, offsets, ids
+
+    def problem(self, seqs: Sequence[int], q_counts: Sequence[int], num_kv_heads: int, group_size: int, head_dim: int,
+                softmax_scale: float) -> DecodeProblem:
+        """The DecodeProblem of requests whose keys are these sequences', q_counts[i]
+        new tokens at the end of each."""
+        return DecodeProblem.from_tables(q_counts, *self.lists(seqs), self.num_pages, self.page_size, num_kv_heads,
+                                         group_size, head_dim, softmax_scale)
+
+
+class PagePools:
+    """The page pools of a model's layers for pages_copy: tensors [num_pages,
+    page_size, ..] of one shape, dtype and GPU, contiguous (K and V of every layer).
+    The object keeps them; their memory must not be exchanged while it is in use."""
+
+    def __init__(self, pools: Sequence[object]):
+        pools = list(pools)
+        if not pools:
+            raise ValueError("at least one pool")
+        x = pools[0]
+        if x.dim() < 2:
+            raise ValueError("pools must be [num_pages, page_size, ..]")
+        self.index = _gpu("a pool", x)
+        for t in pools:
+            _same_kind("a pool", t, x.shape, x.dtype, self.index)
+            if not t.is_contiguous():
+                raise ValueError("pools must be contiguous")
+        self.pools, self.num_pages, self.page_size = pools, x.shape[0], x.shape[1]
+        self.row_bytes = math.prod(x.shape[2:]) * x.element_size()
+        self._table, self._at = _ints("Q", [t.data_ptr() for t in pools])
+
+
+def _copy_list(copies) -> Tuple[object, int, int]:
+    """(what keeps the memory, address, entries) of a list of copies."""
+    import numpy as np
+    a = np.ascontiguousarray(copies, dtype=np.int32) if not (isinstance(copies, np.ndarray) and copies.dtype == np.int32
+                                                             and copies.flags.c_contiguous) else copies
+    if a.size == 0:
+        return a, 0, 0
+    if a.ndim != 2 or a.shape[1] != 3:
+        raise ValueError("copies must be [n, 3]: source page, destination page, rows")
+    return a, a.__array_interface__["data"][0], a.shape[0]
+
+
+def pages_copy(pools, copies, stream=None, workspace=None) -> None:
+    """Copies the first rows of pages to other pages, in every pool (a PagePools, or
+    tensors to make one of): ``copies`` is what the PageTable's calls return. A page
+    is written once, and none that is written is read."""
+    if not isinstance(pools, PagePools):
+        pools = PagePools(pools)
+    keep, at, n = _copy_list(copies)
+    lib, index = load(), pools.index
+    need = ctypes.c_size_t(0)
+    if workspace is None:
+        _check(lib.cas_pages_copy_workspace_size(n, ctypes.byref(need)))
+        if need.value:
+            import torch
+            workspace = _empty(stream, (need.value,), torch.uint8, pools.pools[0].device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the pools' device")
+    ws, ws_bytes = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    _on_device(index, stream, lambda handle: lib.cas_pages_copy(pools._at, len(pools.pools), pools.num_pages, pools.page_size,
+                                                                pools.row_bytes, at, n, ws, ws_bytes, handle))
+
+
+# ---------------------------------------------------------------------------
+# Beam search
+# ---------------------------------------------------------------------------
+_BEAM_PROBLEM = struct.Struct("@iiiiqqi4x")
+_BEAM_STATE = struct.Struct("@PPqqqqq")
+assert _BEAM_PROBLEM.size == ctypes.sizeof(_lib.BeamProblem) and _BEAM_STATE.size == ctypes.sizeof(_lib.BeamState)
+
+
+def _beam_problem(logits, k, pad_token) -> Tuple[bytes, int, int, int]:
+    if logits.dim() != 3:
+        raise ValueError("logits must be [batch, beams, vocab]")
+    batch, beams, vocab = logits.shape
+    sb, si, sv = logits.stride()
+    if vocab > 1 and sv != 1:
+        raise ValueError("logits: the vocabulary's stride must be 1")
+    if beams <= 1:
+        si = sb if batch > 1 else vocab
+    elif batch > 1 and sb != beams * si:
+        raise ValueError("logits: batch entries and beams have no common row stride")
+    k = 2 * beams if k is None else int(k)
+    return _BEAM_PROBLEM.pack(_dtype_code(logits), batch, beams, k, vocab, si, int(pad_token)), batch, beams, k
+
+
+def beam_select_workspace_size(logits, k: Optional[int] = None) -> int:
+    """Workspace bytes of beam_select on such logits."""
+    n = ctypes.c_size_t(0)
+    _check(load().cas_beam_select_workspace_size(_beam_problem(logits, k, 0)[0], ctypes.byref(n)))
+    return n.value
+
+
+def beam_select(logits, scores, k: Optional[int] = None, finished=None, pad_token: int = 0, outs=None, stream=None, workspace=None):
+    """The k (default 2 * beams) best continuations of every batch entry: logits
+    [batch, beams, vocab] (bf16 or fp32, any row stride), scores [batch, beams] fp32
+    so far, ``finished`` [batch, beams] bool or uint8: beams that only keep their
+    score, with ``pad_token``. Returns (scores fp32, parents int32, tokens int32),
+    [batch, k] each, best first; equal ones by beam, then token. Beams that have
+    nothing to choose from (their score not finite, all logits -inf, a NaN or +inf
+    among them) are at -inf, as are tokens whose logit is -inf; where fewer than k
+    candidates are left, the first of those fill the rest."""
+    import torch
+    packed, batch, beams, k = _beam_problem(logits, k, pad_token)
+    index, device, f32, i32 = logits.get_device(), logits.device, torch.float32, torch.int32
+    _same_kind("scores", scores, (batch, beams), f32, index)
+    if not scores.is_contiguous():
+        raise ValueError("scores must be contiguous")
+    fp = 0
+    if finished is not None:
+        if finished.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"finished must be bool or uint8, is {finished.dtype}")
+        _same_kind("finished", finished, (batch, beams), finished.dtype, index)
+        if not finished.is_contiguous():
+            raise ValueError("finished must be contiguous")
+        fp = finished.data_ptr()
+    _gpu("logits", logits)
+    if outs is None:
+        if k < 1:
+            raise ValueError("k must be >= 1")
+        outs = tuple(_empty(stream, (batch, k), t, device) for t in (f32, i32, i32))
+    else:
+        for name, t, dtype in zip(("scores", "parents", "tokens"), outs, (f32, i32, i32)):
+            _same_kind(f"outs: {name}", t, (batch, k), dtype, index)
+            if not t.is_contiguous():
+                raise ValueError("outs must be contiguous")
+    lib = load()
+    if workspace is None:
+        n = ctypes.c_size_t(0)
+        _check(lib.cas_beam_select_workspace_size(packed, ctypes.byref(n)))
+        workspace = _empty(stream, (max(n.value, 1),), torch.uint8, device)
+    elif workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous and on the tensors' device")
+    s, p, t = outs
+    _on_device(index, stream, lambda handle: lib.cas_beam_select(packed, logits.data_ptr(), scores.data_ptr(), fp, s.data_ptr(),
+                                                                 p.data_ptr(), t.data_ptr(), workspace.data_ptr(),
+                                                                 workspace.nbytes, handle))
+    return s, p, t
+
+
+def _beam_rows(what: str, t) -> Tuple[int, int, int]:
+    """(bytes of a row, batch stride, beam stride) of a [batch, beams, ..] tensor whose rows are contiguous."""
+    shape, st, size = t.shape, t.stride(), t.element_size()
+    n = 1
+    for d, s in zip(reversed(shape[2:]), reversed(st[2:])):
+        if d != 1 and s != n and n:
+            raise ValueError(f"{what}: what a beam has must be contiguous")
+        n *= d
+    return n * size, st[0] * size if shape[0] > 1 else 0, st[1] * size if shape[1] > 1 else 0
+
+
+def beam_reorder(xs: Sequence[object], parents, outs: Optional[Sequence[object]] = None, stream=None) -> List[object]:
+    """States of beams follow their parents: y[b, j] = x[b, parents[b, j]] for 1 to 8
+    tensors [batch, beams, ..] (any dtype; what a beam has is contiguous, as in
+    history[:, :, :used]). parents: int32 [batch, beams'] beams of the same batch
+    entry, as beam_select returns them (contiguous). outs=xs reorders in place."""
+    import torch
+    n = len(xs)
+    if not 1 <= n <= 8:
+        raise ValueError("1 to 8 tensors")
+    outs = [None] * n if outs is None else list(outs)
+    if len(outs) != n:
+        raise ValueError("outs must have an entry per tensor")
+    if parents.dim() != 2 or parents.dtype is not torch.int32 or not parents.is_contiguous():
+        raise ValueError("parents must be a contiguous int32 [batch, beams]")
+    index = _gpu("parents", parents)
+    batch, beams_out = parents.shape
+    packed, beams_in = b"", None
+    for i, x in enumerate(xs):
+        if x.dim() < 2 or x.shape[0] != batch:
+            raise ValueError(f"the tensors must be [{batch}, beams, ..]")
+        if beams_in is None:
+            beams_in = x.shape[1]
+        elif x.shape[1] != beams_in:
+            raise ValueError("the tensors must have the same beams")
+        if x.get_device() != index:
+            raise ValueError(f"a tensor is on {x.device}, not on GPU {index}")
+        row, xb, xi = _beam_rows("x", x)
+        y = outs[i]
+        if y is None:
+            y = outs[i] = _empty(stream, (batch, beams_out, *x.shape[2:]), x.dtype, x.device)
+        if y is x:
+            if beams_out != beams_in:
+                raise ValueError("in place, parents must have a column per beam")
+            yb, yi = xb, xi
+        else:
+            _same_kind("output", y, (batch, beams_out, *x.shape[2:]), x.dtype, index)
+            _, yb, yi = _beam_rows("output", y)
+        packed += _BEAM_STATE.pack(x.data_ptr(), y.data_ptr(), row, xb, xi, yb, yi)
+    if beams_out == 0:
+        return outs
+    _on_device(index, stream, lambda handle: load().cas_beam_reorder(parents.data_ptr(), batch, beams_in, beams_out, packed, n, handle))
+    return outs
 
 
 def plan_rotation(steps: Sequence[int], active: Sequence[bool], budget: int, swap_fraction: float):

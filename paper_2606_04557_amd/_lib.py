@@ -16,6 +16,7 @@ CAS_ERR_NOT_PINNED = 4
 CAS_ERR_WORKSPACE = 5
 CAS_ERR_HIP = 6
 CAS_ERR_IO = 7
+CAS_ERR_PAGES = 8
 
 CAS_DTYPE_BF16 = 0
 CAS_DTYPE_FP32 = 1
@@ -34,6 +35,9 @@ EXPORTS = [
     "cas_paged_append_plan_create", "cas_paged_append_run", "cas_paged_append_plan_matches", "cas_paged_append_plan_destroy",
     "cas_paged_chunk_workspace_size", "cas_paged_chunk_fwd", "cas_paged_chunk_plan_create", "cas_paged_chunk_run",
     "cas_paged_chunk_plan_matches", "cas_paged_chunk_plan_destroy", "cas_paged_chunk_plan_info",
+    "cas_page_table_create", "cas_page_table_destroy", "cas_page_table_info", "cas_page_table_add", "cas_page_table_extend",
+    "cas_page_table_reorder", "cas_page_table_truncate", "cas_page_table_free", "cas_page_table_compact", "cas_page_table_lists",
+    "cas_pages_copy_workspace_size", "cas_pages_copy", "cas_beam_select_workspace_size", "cas_beam_select", "cas_beam_reorder",
 ]
 
 CAS_ROPE_HALF = 0
@@ -108,6 +112,22 @@ class ChunkPlanInfo(ctypes.Structure):
     _fields_ = [("workgroups", ctypes.c_int32), ("items", ctypes.c_int32), ("partials", ctypes.c_int32),
                 ("max_partials", ctypes.c_int32), ("key_tiles", ctypes.c_int64), ("decode_parts", ctypes.c_int32),
                 ("decode_tokens", ctypes.c_int32), ("ws_bytes", ctypes.c_size_t)]
+
+
+class PageTableInfo(ctypes.Structure):
+    _fields_ = [("sequences", ctypes.c_int64), ("pages_used", ctypes.c_int64), ("pages_free", ctypes.c_int64),
+                ("pages_end", ctypes.c_int64)]
+
+
+class BeamProblem(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("beams", ctypes.c_int32), ("k", ctypes.c_int32),
+                ("vocab", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("pad_token", ctypes.c_int32)]
+
+
+class BeamState(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("row_bytes", ctypes.c_int64),
+                ("x_stride_batch", ctypes.c_int64), ("x_stride_beam", ctypes.c_int64),
+                ("y_stride_batch", ctypes.c_int64), ("y_stride_beam", ctypes.c_int64)]
 
 
 class PoolConfig(ctypes.Structure):
@@ -200,6 +220,24 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.cas_paged_chunk_plan_matches.restype = i32
     lib.cas_paged_chunk_plan_destroy.argtypes = [vp]
     lib.cas_paged_chunk_plan_info.argtypes = [vp, P(ChunkPlanInfo), P(i32)]
+    # (Arrays of the page table's and the copies' calls are passed by address.)
+    i64 = ctypes.c_int64
+    lib.cas_page_table_create.argtypes = [i64, i32, P(vp)]
+    lib.cas_page_table_destroy.argtypes = [vp]
+    lib.cas_page_table_info.argtypes = [vp, P(PageTableInfo)]
+    lib.cas_page_table_add.argtypes = [vp, vp, i32, P(i64)]
+    lib.cas_page_table_extend.argtypes = [vp, vp, i32, vp, vp, P(i32)]
+    lib.cas_page_table_reorder.argtypes = [vp, vp, i32, vp]
+    lib.cas_page_table_truncate.argtypes = [vp, i64, i64]
+    lib.cas_page_table_free.argtypes = [vp, vp, i32]
+    lib.cas_page_table_compact.argtypes = [vp, i32, vp, P(i32)]
+    lib.cas_page_table_lists.argtypes = [vp, vp, i32, vp, vp, vp, i64]
+    lib.cas_pages_copy_workspace_size.argtypes = [i32, P(sz)]
+    lib.cas_pages_copy.argtypes = [vp, i32, i64, i32, i64, vp, i32, vp, sz, vp]
+    # (The binding packs cas_beam_problem_t and cas_beam_state_t into bytes.)
+    lib.cas_beam_select_workspace_size.argtypes = [vp, P(sz)]
+    lib.cas_beam_select.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.cas_beam_reorder.argtypes = [vp, i32, i32, i32, vp, i32, vp]
     u8p = P(ctypes.c_uint8)
     lib.cas_pool_plan_rotation.argtypes = [P(i32), u8p, i32, i32, ctypes.c_float, P(i32), P(i32), P(i32)]
     lib.cas_pool_create.argtypes = [P(PoolConfig), P(vp)]
@@ -228,7 +266,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
                  "cas_rope_frequencies", "cas_rope", "cas_paged_append", "cas_paged_append_plan_create", "cas_paged_append_run",
                  "cas_paged_append_plan_destroy", "cas_paged_chunk_workspace_size", "cas_paged_chunk_fwd",
                  "cas_paged_chunk_plan_create", "cas_paged_chunk_run", "cas_paged_chunk_plan_destroy",
-                 "cas_paged_chunk_plan_info"):
+                 "cas_paged_chunk_plan_info", "cas_page_table_create", "cas_page_table_destroy", "cas_page_table_info",
+                 "cas_page_table_add", "cas_page_table_extend", "cas_page_table_reorder", "cas_page_table_truncate",
+                 "cas_page_table_free", "cas_page_table_compact", "cas_page_table_lists", "cas_pages_copy_workspace_size",
+                 "cas_pages_copy", "cas_beam_select_workspace_size", "cas_beam_select", "cas_beam_reorder"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib

@@ -1584,6 +1584,7 @@ const char *cas_status_string(cas_status_t s) {
     case CAS_ERR_WORKSPACE: return "CAS_ERR_WORKSPACE";
     case CAS_ERR_HIP: return "CAS_ERR_HIP";
     case CAS_ERR_IO: return "CAS_ERR_IO";
+    case CAS_ERR_PAGES: return "CAS_ERR_PAGES";
   }
   return "CAS_ERR_UNKNOWN";
 }

@@ -42,6 +42,10 @@ cas_status_t decode_run_part(const cas_decode_plan_t *plan, const void *q, const
 // Key tiles and shared page runs of a plan.
 void decode_plan_counts(const cas_decode_plan_t *plan, int64_t *key_tiles, int32_t *shared_runs);
 
+// Writes launch tables of `bytes` bytes to ws on the stream with fill(): through
+// pinned slots, or as kernel arguments while the stream is being captured.
+cas_status_t upload_call_tables(size_t bytes, void *ws, hipStream_t stream, const std::function<void(char *)> &fill);
+
 // launch(), bracketed by timing events while cas_timing_enable is on.
 hipError_t timed_launch(const char *name, hipStream_t s, const std::function<hipError_t()> &launch);
 

@@ -363,6 +363,53 @@ struct ChunkDirect {
 };
 static_assert(sizeof(ChunkParams) % 8 == 0 && sizeof(ChunkParams) + sizeof(ChunkDirect) <= 4096, "kernel arguments");
 
+// Copies between pages of the cache. Workgroup (x, y) has piece x mod pieces, of
+// `piece` bytes, of copy first + x / pieces in pool y.
+constexpr int kPageCopyArgs = 240;    // copies that travel as kernel arguments
+constexpr int kPageCopyPools = 64;    // pools of a launch
+constexpr int kPagePiece = 16384;
+struct PageCopyParams {
+  char *pools[kPageCopyPools];
+  int64_t page_bytes, row_bytes;
+  const cas_page_copy_t *table;   // the copies, or null: they are in copies[]
+  int32_t pieces, piece, first;
+};
+struct PageCopyList {
+  cas_page_copy_t copies[kPageCopyArgs];
+};
+static_assert(sizeof(PageCopyParams) + sizeof(PageCopyList) <= 4096, "kernel arguments");
+
+// Beam search: choosing the candidates of a step. Row r = batch entry r / beams,
+// beam r % beams.
+struct BeamSelectParams {
+  const void *logits;
+  const float *scores;
+  const uint8_t *finished;    // or null
+  float *out_scores;
+  int32_t *out_parents, *out_tokens;
+  int64_t stride;             // elements between rows
+  int32_t vocab, batch, beams, k, pad;
+  float *list_logit;          // [row][k] a row's best logits, in order
+  int32_t *list_token;        // [row][k]
+  int32_t *list_count;        // [row]
+  double *norm;               // [row][2]: the largest logit m and ln sum exp(x - m)
+};
+
+// Reordering of states kept per beam: tensor z, batch entry y.
+struct DevBeamState {
+  const char *x;
+  char *y;
+  int64_t row_bytes, xb, xi, yb, yi;
+  int32_t unit;               // bytes that a thread moves at a time
+};
+constexpr int kBeamStates = 8;
+constexpr int kMaxBeams = 64;
+struct BeamReorderParams {
+  DevBeamState t[kBeamStates];
+  const int32_t *parents;
+  int32_t batch, beams_in, beams_out;
+};
+
 // Forward shared by cas_prefix_attn_fwd (scratch == nullptr: the caller's
 // workspace, tables through the pinned staging ring) and the no-allocation
 // forward (scratch != nullptr: after validation, scratch() yields the device
@@ -409,6 +456,11 @@ hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_m
 // Copies `bytes` (a multiple of 16) of pinned host memory to device memory; when
 // all n_flags flags (pinned host memory) have the value, the source has been read.
 hipError_t launch_table_flags(void *dst, const void *src, size_t bytes, uint32_t *flags, int n_flags, uint32_t value, hipStream_t s);
+// copies: a list of at most kPageCopyArgs, or null where p.table has them.
+hipError_t launch_page_copy(const PageCopyParams &p, const PageCopyList *copies, int n, int n_pools, hipStream_t s);
+hipError_t launch_beam_rows(const BeamSelectParams &p, DType dt, hipStream_t s);
+hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s);
+hipError_t launch_beam_reorder(const BeamReorderParams &p, int n, hipStream_t s);
 hipError_t launch_append(const AppendParams &p, int D, int units, int head_groups, hipStream_t s);
 
 }  // namespace cas

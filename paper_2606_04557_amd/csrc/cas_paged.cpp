@@ -21,6 +21,7 @@
 #include "../../include/cas.h"
 #include "cas_host.h"
 #include "cas_internal.h"
+#include "cas_spans.h"
 
 using namespace cas;
 
@@ -57,53 +58,6 @@ cas_status_t check_rope(const cas_rope_t *r, int head_dim) {
 
 DevRope dev_rope(const cas_rope_t *r, bool inverse) {
   return DevRope{r->turns, r->rotary_dim, r->scale, r->layout == CAS_ROPE_INTERLEAVED, inverse};
-}
-
-// What a strided [tokens, heads, head_dim] tensor covers, in bytes: rows of
-// `ext` bytes (of one or several heads or tokens), `stride` apart, made of pieces of
-// `width` bytes (a head), `inner` apart (0: one piece).
-struct Footprint {
-  uintptr_t base, end;
-  uint64_t stride, ext, inner, width;
-  bool distinct;   // no two elements share an address
-};
-
-Footprint footprint(const void *x, int64_t tokens, int64_t heads, int64_t st, int64_t sh, int D, int es) {
-  int64_t outer = st, n_outer = tokens, inner = sh, n_inner = heads;
-  if (n_outer == 1 || (n_inner > 1 && inner > outer)) {
-    std::swap(outer, inner);
-    std::swap(n_outer, n_inner);
-  }
-  const int64_t in = n_inner > 1 ? inner : 0, out = n_outer > 1 ? outer : 0;
-  Footprint f;
-  f.base = (uintptr_t)x;
-  f.width = (uint64_t)D * es;
-  f.inner = (uint64_t)in * es;
-  f.ext = (uint64_t)(n_inner - 1) * f.inner + f.width;
-  f.stride = (uint64_t)out * es;
-  f.end = f.base + (uint64_t)(n_outer - 1) * f.stride + f.ext;
-  f.distinct = (n_inner == 1 || in >= D) && (n_outer == 1 || f.stride >= f.ext);
-  return f;
-}
-
-// The footprint of `bytes` bytes in a row.
-Footprint span_of(const void *x, uint64_t bytes) {
-  return Footprint{(uintptr_t)x, (uintptr_t)x + bytes, 0, bytes, 0, bytes, true};
-}
-
-// Two tensors that share a range of addresses are still apart when their rows
-// interleave (slices of one projection's output, [tokens, Hq + 2 Hkv, d]), or their
-// heads do ([tokens, heads, 3, d]): counted modulo a step that divides all their
-// strides, every row (or head) of a tensor lies in the same place.
-bool apart(const Footprint &a, const Footprint &b) {
-  if (a.end <= b.base || b.end <= a.base) return true;
-  auto modulo = [&](uint64_t step, uint64_t wa, uint64_t wb) {
-    if (step == 0) return false;
-    const uint64_t delta = b.base >= a.base ? (b.base - a.base) % step : (step - (a.base - b.base) % step) % step;
-    return delta >= wa && delta + wb <= step;
-  };
-  const uint64_t rows = std::gcd(a.stride, b.stride);
-  return modulo(rows, a.ext, b.ext) || modulo(std::gcd(rows, std::gcd(a.inner, b.inner)), a.width, b.width);
 }
 
 constexpr int64_t kMaxStride = (int64_t)1 << 31;   // (with the limits on tokens and heads, spans fit 64 bits)
@@ -871,6 +825,12 @@ cas_status_t upload_tables(size_t bytes, void *ws, hipStream_t stream, Clock::ti
   return CAS_OK;
 }
 
+bool is_capturing(hipStream_t stream) {
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (stream && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
+  return capture == hipStreamCaptureStatusActive;
+}
+
 cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const void *q, const void *k_pages, const void *v_pages,
                        void *o, float *lse, void *workspace, size_t ws_bytes, hipStream_t stream) {
   if (pl.items.empty() && pl.decode.empty()) return CAS_OK;
@@ -896,9 +856,7 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
     if (!pl.merges.empty()) std::memcpy(h + pl.off_merges, pl.merges.data(), pl.merges.size() * sizeof(DevChunkMerge));
     std::memcpy(h + pl.off_granules, pl.granules.data(), pl.granules.size() * sizeof(uint32_t));
   };
-  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-  if (stream && hipStreamIsCapturing(stream, &capture) != hipSuccess) (void)hipGetLastError();
-  const bool capturing = capture == hipStreamCaptureStatusActive;
+  const bool capturing = is_capturing(stream);
   const Clock::time_point deadline = Clock::now() + kSlotWait;
   const TableUpload upload = [&](size_t bytes, void *dst, hipStream_t st, const std::function<void(char *)> &write) {
     // A graph keeps kernel arguments, but not what the pinned slots hold now.
@@ -948,6 +906,14 @@ cas_status_t run_chunk(const cas_decode_problem_t *p, const ChunkPlan &pl, const
 }
 
 }  // namespace
+
+namespace cas {
+cas_status_t upload_call_tables(size_t bytes, void *ws, hipStream_t stream, const std::function<void(char *)> &fill) {
+  // (A graph keeps kernel arguments, but not what the pinned slots hold now.)
+  if (is_capturing(stream)) return upload_as_arguments(bytes, ws, stream, fill);
+  return upload_tables(bytes, ws, stream, Clock::now() + kSlotWait, fill);
+}
+}  // namespace cas
 
 struct cas_append_plan {
   OwnedProblem own;
