@@ -50,17 +50,22 @@ cas_status_t check_beam(const cas_beam_problem_t *p) {
 }
 
 struct BeamLayout {
-  size_t logit, token, count, norm, bytes;
+  int32_t pieces, chunks, per_wave, waves;
+  size_t parts, bytes;
 };
 
 BeamLayout beam_layout(const cas_beam_problem_t &p) {
-  const size_t rows = (size_t)p.batch * (size_t)p.beams, lists = rows * (size_t)p.k * 4;
+  constexpr int64_t kWaves = 4096;   // 16 for each of 256 compute units
+  const int64_t rows = (int64_t)p.batch * p.beams, piece = p.dtype == CAS_DTYPE_BF16 ? 8 : 4;
+  // (A row that begins inside a 16-byte piece reaches up to a piece further.)
+  auto chunks = [&](int64_t j) { return (p.vocab + piece - 1 + 64 * j * piece - 1) / (64 * j * piece); };
   BeamLayout l;
-  l.norm = 0;
-  l.count = align_up(rows * 16, 256);
-  l.logit = align_up(l.count + rows * 4, 256);
-  l.token = align_up(l.logit + lists, 256);
-  l.bytes = rows ? align_up(l.token + lists, 256) : 0;
+  l.pieces = rows * chunks(8) >= kWaves / 2 ? 8 : 2;
+  l.chunks = (int32_t)chunks(l.pieces);
+  l.per_wave = (int32_t)std::max<int64_t>(1, rows * l.chunks / kWaves);
+  l.waves = (l.chunks + l.per_wave - 1) / l.per_wave;
+  l.parts = (size_t)rows * (size_t)l.chunks * 256;
+  l.bytes = l.parts + align_up((size_t)rows * (size_t)l.waves * sizeof(DevBeamPart), 256);
   return l;
 }
 
@@ -102,13 +107,15 @@ cas_status_t select(const cas_beam_problem_t *p, const void *logits, const float
   a.beams = p->beams;
   a.k = p->k;
   a.pad = p->pad_token;
-  a.norm = (double *)(ws + l.norm);
-  a.list_count = (int32_t *)(ws + l.count);
-  a.list_logit = (float *)(ws + l.logit);
-  a.list_token = (int32_t *)(ws + l.token);
+  a.chunks = l.chunks;
+  a.per_wave = l.per_wave;
+  a.waves = l.waves;
+  a.pieces = l.pieces;
+  a.group_max = (float *)ws;
+  a.parts = (DevBeamPart *)(ws + l.parts);
   const DType dt = p->dtype == CAS_DTYPE_BF16 ? kBF16 : kFP32;
-  hipError_t e = timed_launch("beam_rows", stream, [&] { return launch_beam_rows(a, dt, stream); });
-  if (e != hipSuccess) return set_hip_error("beam_rows launch", e);
+  hipError_t e = timed_launch("beam_scan", stream, [&] { return launch_beam_scan(a, dt, stream); });
+  if (e != hipSuccess) return set_hip_error("beam_scan launch", e);
   e = timed_launch("beam_pick", stream, [&] { return launch_beam_pick(a, dt, stream); });
   return e == hipSuccess ? CAS_OK : set_hip_error("beam_pick launch", e);
 }

@@ -380,7 +380,14 @@ struct PageCopyList {
 static_assert(sizeof(PageCopyParams) + sizeof(PageCopyList) <= 4096, "kernel arguments");
 
 // Beam search: choosing the candidates of a step. Row r = batch entry r / beams,
-// beam r % beams.
+// beam r % beams. A row is cut into 16-byte pieces at aligned addresses (the first
+// and the last may be partial); piece 64 (J c + j) + lane of it is the j-th of lane
+// `lane` in chunk c. A group is what one lane has of one chunk: J pieces.
+struct DevBeamPart {
+  double sum;   // of exp(x - ref) over a wave's chunks
+  float ref;
+  float pad_;
+};
 struct BeamSelectParams {
   const void *logits;
   const float *scores;
@@ -389,10 +396,12 @@ struct BeamSelectParams {
   int32_t *out_parents, *out_tokens;
   int64_t stride;             // elements between rows
   int32_t vocab, batch, beams, k, pad;
-  float *list_logit;          // [row][k] a row's best logits, in order
-  int32_t *list_token;        // [row][k]
-  int32_t *list_count;        // [row]
-  double *norm;               // [row][2]: the largest logit m and ln sum exp(x - m)
+  int32_t chunks;             // of a row
+  int32_t per_wave;           // chunks of a wave
+  int32_t waves;              // of a row
+  int32_t pieces;             // J, 8 or 2
+  float *group_max;           // [row][chunk][64] the largest logit of every group
+  DevBeamPart *parts;         // [row][wave]
 };
 
 // Reordering of states kept per beam: tensor z, batch entry y.
@@ -458,7 +467,7 @@ hipError_t launch_chunk_merge_bf16(const ChunkParams &p, int D, int few, int n_m
 hipError_t launch_table_flags(void *dst, const void *src, size_t bytes, uint32_t *flags, int n_flags, uint32_t value, hipStream_t s);
 // copies: a list of at most kPageCopyArgs, or null where p.table has them.
 hipError_t launch_page_copy(const PageCopyParams &p, const PageCopyList *copies, int n, int n_pools, hipStream_t s);
-hipError_t launch_beam_rows(const BeamSelectParams &p, DType dt, hipStream_t s);
+hipError_t launch_beam_scan(const BeamSelectParams &p, DType dt, hipStream_t s);
 hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s);
 hipError_t launch_beam_reorder(const BeamReorderParams &p, int n, hipStream_t s);
 hipError_t launch_append(const AppendParams &p, int D, int units, int head_groups, hipStream_t s);
