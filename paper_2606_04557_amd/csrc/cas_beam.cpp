@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <exception>
 #include <string>
 #include <vector>
@@ -111,6 +112,7 @@ cas_status_t select(const cas_beam_problem_t *p, const void *logits, const float
   a.per_wave = l.per_wave;
   a.waves = l.waves;
   a.pieces = l.pieces;
+  a.ln_vocab = std::log((double)p->vocab);
   a.group_max = (float *)ws;
   a.parts = (DevBeamPart *)(ws + l.parts);
   const DType dt = p->dtype == CAS_DTYPE_BF16 ? kBF16 : kFP32;

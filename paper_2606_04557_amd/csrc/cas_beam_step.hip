@@ -14,7 +14,9 @@ namespace cas {
 namespace {
 
 constexpr int kScanThreads = 256;
+constexpr int kPickThreads = 512;
 constexpr int kListCap = 128;    // groups that a wave has found and not looked at yet
+constexpr int kLook = 3;         // pieces of such groups that a lane takes at a time
 
 // Whether beam `row` has nothing to choose from by its own state.
 __device__ __forceinline__ bool out_of_search(const BeamSelectParams &p, int row) {
@@ -27,20 +29,38 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 
+// x of another lane of the wave: lane l +- 1, +- 2 (quad permutations), the mirror of
+// 8 and of 16 lanes, and lanes 15 and 31 of the rows before. Rows outside MASK get `old`.
+template <int CTRL, int MASK = 0xf>
+__device__ __forceinline__ int lane_move(int old, int x) {
+  return __builtin_amdgcn_update_dpp(old, x, CTRL, MASK, 0xf, false);
+}
+constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kMirror8 = 0x141, kMirror16 = 0x140, kFrom15 = 0x142, kFrom31 = 0x143;
+
+template <int CTRL, int MASK = 0xf>
+__device__ __forceinline__ float max_with(float x) {
+  return fmaxf(x, __int_as_float(lane_move<CTRL, MASK>(__float_as_int(x), __float_as_int(x))));
+}
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-  return x;
+  x = max_with<kMirror16>(max_with<kMirror8>(max_with<kSwap2>(max_with<kSwap1>(x))));
+  x = max_with<kFrom31, 0xc>(max_with<kFrom15, 0xa>(x));
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
+template <int CTRL, int MASK = 0xf>
+__device__ __forceinline__ double plus(double x) {
+  const int64_t u = __double_as_longlong(x);
+  const uint32_t lo = (uint32_t)lane_move<CTRL, MASK>(0, (int)u), hi = (uint32_t)lane_move<CTRL, MASK>(0, (int)(u >> 32));
+  return x + __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+__device__ __forceinline__ uint64_t lane_value(uint64_t x, int lane) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)x, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane);
+  return (uint64_t)hi << 32 | lo;
+}
 __device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-  return x;
-}
-
-__device__ __forceinline__ float lane_value(float x, int lane) {
-  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+  x = plus<kMirror16>(plus<kMirror8>(plus<kSwap2>(plus<kSwap1>(x))));
+  x = plus<kFrom31, 0xc>(plus<kFrom15, 0xa>(x));
+  return __longlong_as_double((int64_t)lane_value((uint64_t)__double_as_longlong(x), 63));
 }
 
 // What the wave's lanes wrote to LDS before is what they read after.
@@ -84,10 +104,13 @@ struct Row {
     end = begin + p.vocab;
     base = x - begin;
   }
+  __device__ __forceinline__ bool whole(int piece) const {
+    return piece * Piece<T>::N >= begin && (piece + 1) * Piece<T>::N <= end;
+  }
   __device__ __forceinline__ void load(int piece, float *x) const {
     constexpr int N = Piece<T>::N;
     const int at = piece * N;
-    if (at >= begin && at + N <= end) {
+    if (whole(piece)) {
       Piece<T>::unpack(*reinterpret_cast<const u32x4 *>(base + at), x);
     } else {
 #pragma unroll
@@ -143,9 +166,6 @@ __global__ __launch_bounds__(kScanThreads) void beam_scan_kernel(BeamSelectParam
   if (lane == 0) p.parts[(int64_t)row * p.waves + w] = DevBeamPart{sum, ref, 0.0f};
 }
 
-// Before b in a beam's order.
-__device__ __forceinline__ bool ahead(float xa, int ta, float xb, int tb) { return xa > xb || (xa == xb && ta < tb); }
-
 // 32-bit keys in the order of the floats.
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);   // (-0 and 0 are alike)
@@ -153,7 +173,12 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
-// The k-th largest of the lanes' values.
+// A beam's candidate, the higher the better: equal logits are in the order of their tokens. 0 is none.
+__device__ __forceinline__ uint64_t candidate(float x, int token) { return (uint64_t)order_key(x) << 32 | (uint32_t)~token; }
+__device__ __forceinline__ float candidate_logit(uint64_t c) { return key_value((uint32_t)(c >> 32)); }
+__device__ __forceinline__ int candidate_token(uint64_t c) { return (int)~(uint32_t)c; }
+
+// The k-th largest of the lanes' values, or a value below it that no fewer than k lanes reach; finite.
 __device__ __forceinline__ float kth_of_lanes(float x, int k) {
   const uint32_t key = order_key(x);
   uint32_t t = 0;
@@ -163,151 +188,244 @@ __device__ __forceinline__ float kth_of_lanes(float x, int k) {
     if (n >= k) t = trial;
     if (n == k) break;
   }
-  return key_value(t > 0x7fffffu ? t : 0x7fffffu);   // (-inf; keys below are those of NaNs)
+  return t > order_key(-FLT_MAX) ? key_value(t) : -FLT_MAX;
 }
 
-// A beam's best logits so far, one in a lane, in order; (-inf, INT_MAX) where there is none.
+// The best logits of a row that a wave has found: `count` (at most k) of them in its
+// first lanes, in order, and n more in LDS that have not been compared yet.
 struct BeamList {
-  float x;
-  int token;
-  __device__ __forceinline__ void insert(int lane, int k, float nx, int nt) {
-    const int at = __popcll(__ballot(ahead(x, token, nx, nt)));
-    if (at >= k) return;
-    // (From the lane before.)
-    const float ux = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x138, 0xf, 0xf, true));
-    const int ut = __builtin_amdgcn_update_dpp(0, token, 0x138, 0xf, 0xf, true);
-    if (lane > at) {
-      x = ux;
-      token = ut;
+  uint64_t best;
+  uint64_t *found;   // [64]
+  int count, n, k;
+  float least;       // what is below is not wanted
+
+  // A candidate's place is the number of those ahead of it.
+  __device__ __forceinline__ void sort(int lane) {
+    wave_lds_fence();
+    const uint64_t mine = lane < n ? found[lane] : 0;
+    wave_lds_fence();
+    int at = lane, at_found = 0;
+    for (int i = 0; i < n; ++i) {
+      const uint64_t c = lane_value(mine, i);
+      at += c > best;
+      at_found += c > mine;
     }
-    if (lane == at) {
-      x = nx;
-      token = nt;
-    }
+    for (int i = 0; i < count; ++i) at_found += lane_value(best, i) > mine;
+    if (lane < count && at < k) found[at] = best;
+    if (lane < n && at_found < k) found[at_found] = mine;
+    count = min(count + n, k);
+    n = 0;
+    wave_lds_fence();
+    best = lane < count ? found[lane] : 0;
+    wave_lds_fence();
+    if (count == k) least = fmaxf(least, candidate_logit(lane_value(best, k - 1)));
   }
 };
 
-// Looks at n listed groups of a row for logits that belong to its k best.
-template <typename T, int J>
-__device__ __forceinline__ void look_at(const Row<T> &r, const int *groups, int n, int lane, int k, float &least, BeamList &best) {
-  constexpr int N = Piece<T>::N, G = 64 / J;   // groups that the wave takes at a time
-  for (int g0 = 0; g0 < n; g0 += G) {
-    const int g = g0 + lane / J, group = g < n ? groups[g] : 0;
-    const int piece = (group >> 6) * 64 * J + lane % J * 64 + (group & 63);
-    float x[N];
-    r.load(piece, x);
+// The largest logits of the row's groups, kTile chunks at a time (the first ones stay in registers).
+constexpr int kTile = 40;
+struct GroupTile {
+  float g[kTile];
+  __device__ __forceinline__ void load(const float *at, int chunks) {
+    // (By eights, whose last ones repeat the row's last chunk: a branch for each would wait for what it loaded.)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int token = piece * N + i - r.begin;
-      uint64_t hit = __ballot(g < n && x[i] >= least && x[i] > -INFINITY);
-      while (hit) {
-        const int l = __builtin_ctzll(hit);
-        hit &= hit - 1;
-        best.insert(lane, k, lane_value(x[i], l), __builtin_amdgcn_readlane(token, l));
+    for (int c = 0; c < kTile; c += 8) {
+      if (c < chunks) {
+#pragma unroll
+        for (int i = c; i < c + 8; ++i) g[i] = at[min(i, chunks - 1) * 64];
+      } else {
+#pragma unroll
+        for (int i = c; i < c + 8; ++i) g[i] = -INFINITY;
       }
     }
-    least = fmaxf(least, lane_value(best.x, k - 1));
   }
+  __device__ __forceinline__ float largest() const {
+    float m = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < kTile; ++c) m = fmaxf(m, g[c]);
+    return m;
+  }
+};
+
+// The largest of each lane's groups of a row, of which the tile has the first ones.
+__device__ __forceinline__ float largest_of_lane(const float *at, int chunks, const GroupTile &tile) {
+  float m = tile.largest();
+  for (int c = kTile; c < chunks; c += 8) {
+    float g[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[i] = at[min(c + i, chunks - 1) * 64];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, g[i]);
+  }
+  return m;
 }
 
-// The k best logits above -inf of a row. A group with one of them has a maximum
-// that is at least the k-th largest of any k groups' maxima; only such groups are
-// read again.
+// The logits of a row that are at least list.least, the k best of them. They are in
+// groups whose maximum is at least that, and only such groups are read again, J lanes
+// to a group, kLook pieces to a lane at a time. (The kernel runs through its code
+// once, so that fetching it counts: each part is there once, and what is seldom
+// needed is out of the way.)
 template <typename T, int J>
-__device__ __forceinline__ BeamList best_of_row(const BeamSelectParams &p, int row, int lane, int *groups) {
+__device__ __forceinline__ void best_of_row(const BeamSelectParams &p, int row, int lane, int *groups, GroupTile &tile, BeamList &list) {
+  constexpr int N = Piece<T>::N, G = 64 / J, E = kLook * N;
   const Row<T> r(p, row);
   const float *gm = p.group_max + (int64_t)row * p.chunks * 64 + lane;
-  float m = -INFINITY;
-#pragma unroll 8
-  for (int c = 0; c < p.chunks; ++c) m = fmaxf(m, gm[c * 64]);
-  float least = kth_of_lanes(m, p.k);
-  BeamList best{-INFINITY, INT32_MAX};
-  int n = 0;
-  for (int c = 0; c < p.chunks; ++c) {
-    const float g = gm[c * 64];
-    const bool mine = g >= least && g > -INFINITY;
-    const uint64_t hit = __ballot(mine);
-    if (!hit) continue;
-    if (mine) groups[n + __popcll(hit & ((1ull << lane) - 1))] = c * 64 + lane;
-    n += __popcll(hit);
-    if (n > kListCap - 64) {
+  for (int c0 = 0;; c0 += kTile) {
+    const bool last = c0 + kTile >= p.chunks;
+    if (c0) tile.load(gm + c0 * 64, p.chunks - c0);
+    uint64_t mine = 0;   // the lane's groups in the tile that may have something
+#pragma unroll
+    for (int c = 0; c < kTile; ++c) mine |= (uint64_t)(tile.g[c] >= list.least) << c;
+    if (last) mine &= ~0ull >> (64 - (p.chunks - c0));
+    for (bool more = true; more;) {
+      int n = 0;   // groups listed
+      uint64_t hit;
+      while (n <= kListCap - 64 && (hit = __ballot(mine != 0))) {
+        if (mine) groups[n + __popcll(hit & ((1ull << lane) - 1))] = (c0 + __builtin_ctzll(mine)) * 64 + lane;
+        n += __popcll(hit);
+        mine &= mine - 1;
+      }
       wave_lds_fence();
-      look_at<T, J>(r, groups, n, lane, p.k, least, best);
+      more = n > kListCap - 64;
+      for (int g0 = 0;; g0 += G * kLook) {
+        float x[E];
+        int piece[kLook];
+        uint32_t hits = 0;   // the lane's elements that may be among the best
+        if (g0 < n) {
+          bool partial = false;
+#pragma unroll
+          for (int u = 0; u < kLook; ++u) {
+            const int g = g0 + u * G + lane / J, group = groups[g < n ? g : 0];
+            piece[u] = (group >> 6) * 64 * J + lane % J * 64 + (group & 63);
+            const bool whole = r.whole(piece[u]);
+            partial |= g < n && !whole;
+            u32x4 v{};
+            if (g < n && whole) v = *reinterpret_cast<const u32x4 *>(r.base + piece[u] * N);
+            Piece<T>::unpack(v, x + u * N);
+            hits |= (g < n && whole ? (1u << N) - 1 : 0) << u * N;
+          }
+          if (__builtin_expect(__any(partial), 0)) {
+#pragma unroll
+            for (int u = 0; u < kLook; ++u)
+              if (g0 + u * G + lane / J < n && !r.whole(piece[u])) {
+                r.load(piece[u], x + u * N);
+                hits |= ((1u << N) - 1) << u * N;
+              }
+          }
+          uint32_t high = 0;
+#pragma unroll
+          for (int e = 0; e < E; ++e) high |= (uint32_t)(x[e] >= list.least) << e;
+          hits &= high;
+        }
+        const bool end = last && !more && g0 + G * kLook >= n;
+        for (;;) {
+          // The lane's first one that is left.
+          const int e = __builtin_ctz(hits | 1u << 31);
+          float y = x[0];
+          int at = piece[0];
+#pragma unroll
+          for (int i = 1; i < E; ++i) y = e == i ? x[i] : y;
+#pragma unroll
+          for (int u = 1; u < kLook; ++u) at = e / N == u ? piece[u] : at;
+          const uint64_t any = __ballot(hits != 0);
+          if (!any && !end) break;
+          if (!any || list.n + __popcll(any) > 64) {
+            list.sort(lane);
+            if (!any) return;
+            uint32_t high = 0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) high |= (uint32_t)(x[i] >= list.least) << i;
+            hits &= high;
+            continue;
+          }
+          if (hits) list.found[list.n + __popcll(any & ((1ull << lane) - 1))] = candidate(y, at * N + e % N - r.begin);
+          list.n += __popcll(any);
+          hits &= hits - 1;
+        }
+        if (g0 + G * kLook >= n) break;
+      }
       wave_lds_fence();
-      n = 0;
     }
   }
-  wave_lds_fence();
-  look_at<T, J>(r, groups, n, lane, p.k, least, best);
-  wave_lds_fence();
-  return best;
 }
 
 // The exact logarithm's share of a beam's score: how far ln sum may be off by what
 // the scan rounds. Relative to its value each term is off by its argument d's two
-// roundings (2 |d| 2^-24, and 1 % for log2 e's own), the exponential's unit
+// roundings (2 |d| 2^-24, and a tenth for that of log2 e), the exponential's unit
 // (2 x 2^-24) and six additions; the sum's terms, weighted by it, have at most
 // ln V - ln sum + 2 for |d| (the entropy of V tokens is at most ln V, and d is at most 1).
-__device__ __forceinline__ double sum_error(int vocab, double ln_sum) {
-  return (2.2 * (log((double)vocab) - ln_sum + 2.0) + 9.0) * 0x1p-24;
+__device__ __forceinline__ double sum_error(double ln_vocab, double ln_sum) {
+  return (2.2 * (ln_vocab - ln_sum + 2.0) + 9.0) * 0x1p-24;
 }
 
-// One batch entry: the best tokens of each beam (a wave to a beam), and then the
-// best of all. A candidate's place is the number of candidates ahead of it; those
-// of another beam are sorted, too, so counting stops at the first one behind it.
-// Where two beams' candidates are closer than their sums are exact, those sums are
-// made again in fp64 and the places counted again.
+// One batch entry, a wave to a beam. The largest score of any group with index l mod
+// 64 is the l-th of 64 values; as many groups as there are values above it reach the
+// k-th largest of these, and only logits that reach it are looked for: hardly more
+// than k of all beams together. Then a candidate's place is the number of candidates
+// ahead of it; those of another beam are sorted, too. Where two beams' candidates
+// are closer than their sums are exact, those sums are made again in fp64 and the
+// places counted again.
 template <typename T, int J>
-__global__ __launch_bounds__(1024) void beam_pick_kernel(BeamSelectParams p) {
+__global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParams p) {
+  constexpr int W = kPickThreads / 64;
   extern __shared__ char smem[];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_waves = blockDim.x >> 6;
-  const int n_beams = p.beams, k = p.k, total = n_beams * k;
-  double *own = (double *)smem;                   // [beams] the score so far
-  double *ref = own + n_beams;                    // [beams]
-  double *ln = ref + n_beams;                     // [beams] ln sum exp(x - ref)
-  double *error = ln + n_beams;                   // [beams] of the latter
-  double *partial = error + n_beams;              // [waves]
-  float *logit = (float *)(partial + n_waves);    // [beams][k]
-  int *token = (int *)(logit + total);            // [beams][k]
-  int *count = token + total;                     // [beams]
-  int *again = count + n_beams;                   // [beams] to be summed again
-  int *order = again + n_beams;                   // [k + 1] candidate of each place, or -1
-  int *groups = order + k + 1 + wave * kListCap;  // [waves][kListCap]
-  auto score = [&](int c, int i) { return own[i] + ((double)logit[c] - ref[i]) - ln[i]; };
-  for (int i = wave; i < n_beams; i += n_waves) {
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_beams = p.beams, k = p.k;
+  double *score = (double *)smem;                    // [beams][64] of a beam's candidates
+  double *own = score + n_beams * 64;                // [beams] the score so far
+  double *ref = own + n_beams;                       // [beams]
+  double *ln = ref + n_beams;                        // [beams] ln sum exp(x - ref)
+  double *error = ln + n_beams;                      // [beams] of the latter
+  double *partial = error + n_beams;                 // [W]
+  uint64_t *found = (uint64_t *)(partial + W) + wave * 64;   // [W][64]
+  int *token = (int *)((uint64_t *)(partial + W) + W * 64);  // [beams][64]
+  int *count = token + n_beams * 64;                 // [beams] -1: candidates of it are looked for
+  int *again = count + n_beams;                      // [beams] to be summed again
+  int *order = again + n_beams;                      // [k + 1] candidate of each place, or -1
+  float *best = (float *)(order + k + 1);            // [W][64]
+  int *groups = (int *)(best + W * 64) + wave * kListCap;    // [W][kListCap]
+  GroupTile tile;
+  float most_of_lane = -INFINITY;
+  for (int i = wave; i < n_beams; i += W) {
     const int row = b * n_beams + i;
+    // (All that is needed is loaded at once; for a row out of the search it is not used.)
+    const DevBeamPart *parts = p.parts + (int64_t)row * p.waves;
+    const float *gm = p.group_max + (int64_t)row * p.chunks * 64 + lane;
+    const DevBeamPart first = parts[min(lane, p.waves - 1)];
     const float so_far = p.scores[row];
     const bool done = p.finished && p.finished[row];
+    tile.load(gm, p.chunks);
     int n = 0;
-    if (done && fabsf(so_far) < INFINITY) {
-      n = 1;
-      if (lane == 0) {
-        logit[i * k] = 0.0f;
-        token[i * k] = p.pad;
-        own[i] = so_far;
-        ref[i] = ln[i] = error[i] = 0.0;
-      }
-    } else if (!out_of_search(p, row)) {
-      const DevBeamPart *parts = p.parts + (int64_t)row * p.waves;
-      float most = -FLT_MAX;
-      for (int w = lane; w < p.waves; w += 64) most = fmaxf(most, parts[w].ref);
-      most = wave_max(most);
-      double sum = 0.0;
-      for (int w = lane; w < p.waves; w += 64) sum += parts[w].sum * exp((double)parts[w].ref - (double)most);
-      sum = wave_sum(sum);
-      if (sum > 0.0 && sum < INFINITY) {   // (a NaN or +inf among the logits is in the sum)
-        const BeamList best = best_of_row<T, J>(p, row, lane, groups);
-        n = __popcll(__ballot(lane < k && best.x > -INFINITY));
-        if (lane < n) {
-          logit[i * k + lane] = best.x;
-          token[i * k + lane] = best.token;
-        }
+    if (fabsf(so_far) < INFINITY) {
+      double most = 0.0, ln_sum = 0.0, off = 0.0;
+      if (done) {
+        n = 1;
         if (lane == 0) {
-          own[i] = so_far;
-          ref[i] = most;
-          ln[i] = log(sum);
-          error[i] = sum_error(p.vocab, ln[i]);
+          score[i * 64] = so_far;
+          token[i * 64] = p.pad;
+          most_of_lane = fmaxf(most_of_lane, so_far);
         }
+      } else {
+        float x = first.ref;
+        for (int w = lane + 64; w < p.waves; w += 64) x = fmaxf(x, parts[w].ref);
+        most = wave_max(x);
+        double sum = 0.0;
+        for (int w = lane; w < p.waves; w += 64) {
+          const DevBeamPart part = w < 64 ? first : parts[w];
+          sum += part.sum * exp((double)part.ref - most);
+        }
+        sum = wave_sum(sum);
+        if (sum > 0.0 && sum < INFINITY) {   // (a NaN or +inf among the logits is in the sum)
+          n = -1;
+          ln_sum = log(sum);
+          off = sum_error(p.ln_vocab, ln_sum);
+          most_of_lane = fmaxf(most_of_lane, (float)(so_far + ((double)largest_of_lane(gm, p.chunks, tile) - most) - ln_sum));
+        }
+      }
+      if (lane == 0) {
+        own[i] = so_far;
+        ref[i] = most;
+        ln[i] = ln_sum;
+        error[i] = off;
       }
     }
     if (lane == 0) {
@@ -315,31 +433,62 @@ __global__ __launch_bounds__(1024) void beam_pick_kernel(BeamSelectParams p) {
       again[i] = 0;
     }
   }
+  best[wave * 64 + lane] = most_of_lane;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < W; ++w) most_of_lane = fmaxf(most_of_lane, best[w * 64 + lane]);
+  const double reached = kth_of_lanes(most_of_lane, k);
+  for (int i = wave; i < n_beams; i += W) {
+    if (count[i] >= 0) continue;
+    const int row = b * n_beams + i;
+    if (n_beams > W) tile.load(p.group_max + (int64_t)row * p.chunks * 64 + lane, p.chunks);
+    // (Lower by what the scores and their rounding to fp32 may be off, and by a step of fp32 for the rounding here.)
+    const double bound = reached - own[i] + ref[i] + ln[i], slack = 2.0 * error[i] + 1e-5 + 0x1p-22 * (fabs(reached) + fabs(bound));
+    // (Without k values to go by, whatever a beam has may be wanted.)
+    const float least = reached > -FLT_MAX ? fmaxf((float)(bound - slack), -FLT_MAX) : -FLT_MAX;
+    BeamList list{0, found, 0, 0, k, least};
+    best_of_row<T, J>(p, row, lane, groups, tile, list);
+    if (lane < list.count) {
+      score[i * 64 + lane] = own[i] + ((double)candidate_logit(list.best) - ref[i]) - ln[i];
+      token[i * 64 + lane] = candidate_token(list.best);
+    }
+    if (lane == 0) count[i] = list.count;
+  }
+  // Up to four threads share a candidate, each with every fourth beam.
+  const int log_k = 32 - __builtin_clz(k - 1 | 1), total = n_beams << log_k;
+  const int share = total <= kPickThreads / 4 ? 2 : total <= kPickThreads / 2 ? 1 : 0;
   for (int round = 0;; ++round) {
-    for (int i = tid; i <= k; i += blockDim.x) order[i] = -1;
+    for (int i = tid; i <= k; i += kPickThreads) order[i] = -1;
     __syncthreads();
-    for (int c = tid; c < total; c += blockDim.x) {
-      const int i = c / k;
-      int place = c - i * k;
-      if (place >= count[i]) continue;
-      const double mine = score(c, i);
-      for (int j = 0; j < n_beams && place <= k; ++j) {
+    for (int q = tid >> share; q < total; q += kPickThreads >> share) {
+      const int i = q >> log_k, at = q & ((1 << log_k) - 1), c = i * 64 + at;
+      if (at >= count[i]) continue;
+      const double mine = score[c];
+      int place = 0;
+      for (int j = tid & ((1 << share) - 1); j < n_beams && place <= k; j += 1 << share) {
         if (j == i) continue;
-        for (int e = j * k; e < j * k + count[j] && place <= k; ++e, ++place) {
-          const double other = score(e, j);
-          if (!(other > mine || (other == mine && j < i))) break;
-        }
+        // lo of its candidates are ahead: found by doubling steps, then halving them.
+        const double *s = score + j * 64;
+        auto ahead = [&](int e) { return s[e] > mine || (s[e] == mine && j < i); };
+        int lo = 0, hi = count[j];
+        for (int step = 1; lo + step <= hi && ahead(lo + step - 1); step *= 2) lo += step;
+        for (int step = 32; step; step /= 2)
+          if (lo + step <= hi && ahead(lo + step - 1)) lo += step;
+        place += lo;
       }
+      if (share > 0) place += lane_move<kSwap1>(0, place);
+      if (share > 1) place += lane_move<kSwap2>(0, place);
+      place += at;
       if (place <= k) order[place] = c;
     }
     __syncthreads();
     if (round == 1) break;
     bool near = false;
-    for (int i = tid; i < k; i += blockDim.x) {
+    for (int i = tid; i < k; i += kPickThreads) {
       const int c0 = order[i], c1 = order[i + 1];
       if (c0 < 0 || c1 < 0) continue;
-      const int i0 = c0 / k, i1 = c1 / k;
-      if (i0 == i1 || score(c0, i0) - score(c1, i1) >= error[i0] + error[i1]) continue;
+      const int i0 = c0 >> 6, i1 = c1 >> 6;
+      if (i0 == i1 || score[c0] - score[c1] >= error[i0] + error[i1]) continue;
       near = true;
       if (error[i0] > 0.0) again[i0] = 1;
       if (error[i1] > 0.0) again[i1] = 1;
@@ -352,24 +501,25 @@ __global__ __launch_bounds__(1024) void beam_pick_kernel(BeamSelectParams p) {
       const double most = ref[i];
       double sum = 0.0;
 #pragma unroll 4
-      for (int v = tid; v < p.vocab; v += blockDim.x) sum += exp((double)(float)x[v] - most);
+      for (int v = tid; v < p.vocab; v += kPickThreads) sum += exp((double)(float)x[v] - most);
       sum = wave_sum(sum);
       if (lane == 0) partial[wave] = sum;
       __syncthreads();
       sum = 0.0;
-      for (int w = 0; w < n_waves; ++w) sum += partial[w];
-      if (tid == 0) ln[i] = log(sum);
+      for (int w = 0; w < W; ++w) sum += partial[w];
+      if (tid < count[i]) score[i * 64 + tid] = own[i] + ((double)(float)x[token[i * 64 + tid]] - most) - log(sum);
       __syncthreads();
     }
   }
   int n = 0;
-  while (n < k && order[n] >= 0) ++n;
-  for (int i = tid; i < k; i += blockDim.x) {
+  for (int i = 0; i < n_beams; ++i) n += count[i];
+  n = min(n, k);
+  for (int i = tid; i < k; i += kPickThreads) {
     const int64_t at = (int64_t)b * k + i;
     if (i < n) {
       const int c = order[i];
-      p.out_scores[at] = (float)score(c, c / k);
-      p.out_parents[at] = c / k;
+      p.out_scores[at] = (float)score[c];
+      p.out_parents[at] = c >> 6;
       p.out_tokens[at] = token[c];
       continue;
     }
@@ -378,7 +528,7 @@ __global__ __launch_bounds__(1024) void beam_pick_kernel(BeamSelectParams p) {
     for (int64_t g = -1; g != f;) {
       g = f;
       f = i - n;
-      for (int e = 0; e < n; ++e) f += (int64_t)(order[e] / k) * p.vocab + token[order[e]] <= g;
+      for (int e = 0; e < n; ++e) f += (int64_t)(order[e] >> 6) * p.vocab + token[order[e]] <= g;
     }
     p.out_scores[at] = -INFINITY;
     p.out_parents[at] = (int)(f / p.vocab);
@@ -431,9 +581,9 @@ hipError_t launch_beam_scan(const BeamSelectParams &p, DType dt, hipStream_t s) 
 }
 
 hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s) {
-  const int waves = p.beams > 8 ? 16 : 8, total = p.beams * p.k;
-  const size_t lds = (size_t)total * 8 + (size_t)p.beams * 40 + (size_t)waves * (8 + 4 * kListCap) + ((size_t)p.k + 1) * 4;
-  const dim3 grid((unsigned)p.batch), threads((unsigned)waves * 64);
+  constexpr int waves = kPickThreads / 64;
+  const size_t lds = (size_t)p.beams * (64 * 12 + 40) + (size_t)waves * (8 + 64 * 8 + 64 * 4 + 4 * kListCap) + ((size_t)p.k + 1) * 4;
+  const dim3 grid((unsigned)p.batch), threads(kPickThreads);
   if (dt == kBF16 && p.pieces == 8) hipLaunchKernelGGL((beam_pick_kernel<__bf16, 8>), grid, threads, lds, s, p);
   else if (dt == kBF16) hipLaunchKernelGGL((beam_pick_kernel<__bf16, 2>), grid, threads, lds, s, p);
   else if (p.pieces == 8) hipLaunchKernelGGL((beam_pick_kernel<float, 8>), grid, threads, lds, s, p);

@@ -400,6 +400,7 @@ struct BeamSelectParams {
   int32_t per_wave;           // chunks of a wave
   int32_t waves;              // of a row
   int32_t pieces;             // J, 8 or 2
+  double ln_vocab;
   float *group_max;           // [row][chunk][64] the largest logit of every group
   DevBeamPart *parts;         // [row][wave]
 };
