@@ -384,9 +384,8 @@ static_assert(sizeof(PageCopyParams) + sizeof(PageCopyList) <= 4096, "kernel arg
 // and the last may be partial); piece 64 (J c + j) + lane of it is the j-th of lane
 // `lane` in chunk c. A group is what one lane has of one chunk: J pieces.
 struct DevBeamPart {
-  double sum;   // of exp(x - ref) over a wave's chunks
-  float ref;
-  float pad_;
+  double sum;   // of exp(x - base) over a wave's chunks
+  double base;
 };
 struct BeamSelectParams {
   const void *logits;
