@@ -51,18 +51,17 @@ cas_status_t check_beam(const cas_beam_problem_t *p) {
 }
 
 struct BeamLayout {
-  int32_t pieces, chunks, per_wave, waves;
+  int32_t chunks, per_wave, waves;
   size_t parts, bytes;
 };
 
 BeamLayout beam_layout(const cas_beam_problem_t &p) {
-  constexpr int64_t kWaves = 4096;   // 16 for each of 256 compute units
-  const int64_t rows = (int64_t)p.batch * p.beams, piece = p.dtype == CAS_DTYPE_BF16 ? 8 : 4;
-  // (A row that begins inside a 16-byte piece reaches up to a piece further.)
-  auto chunks = [&](int64_t j) { return (p.vocab + piece - 1 + 64 * j * piece - 1) / (64 * j * piece); };
+  // Chunks of a wave: as many as leave 8,192 waves, twice what is on the GPU at a time (64 x 8 rows of 131,072
+  // bf16: 30 us, with half or a quarter as many waves 33).
+  constexpr int64_t kWaves = 8192;
+  const int64_t rows = (int64_t)p.batch * p.beams, piece = p.dtype == CAS_DTYPE_BF16 ? 8 : 4, chunk = 64 * kBeamPieces * piece;
   BeamLayout l;
-  l.pieces = rows * chunks(8) >= kWaves / 2 ? 8 : 2;
-  l.chunks = (int32_t)chunks(l.pieces);
+  l.chunks = (int32_t)((p.vocab + piece - 1 + chunk - 1) / chunk);   // (a row that begins inside a piece reaches further)
   l.per_wave = (int32_t)std::max<int64_t>(1, rows * l.chunks / kWaves);
   l.waves = (l.chunks + l.per_wave - 1) / l.per_wave;
   l.parts = (size_t)rows * (size_t)l.chunks * 256;
@@ -111,7 +110,6 @@ cas_status_t select(const cas_beam_problem_t *p, const void *logits, const float
   a.chunks = l.chunks;
   a.per_wave = l.per_wave;
   a.waves = l.waves;
-  a.pieces = l.pieces;
   a.ln_vocab = std::log((double)p->vocab);
   a.group_max = (float *)ws;
   a.parts = (DevBeamPart *)(ws + l.parts);

@@ -128,9 +128,9 @@ struct Row {
       if (piece * N + i >= begin && piece * N + i < end) Piece<T>::put(v, i, base[piece * N + i]);
     return v;
   }
-  // The J pieces of a lane in chunk c.
-  template <int J>
+  // A lane's pieces of chunk c.
   __device__ __forceinline__ void load_chunk(int c, int lane, u32x4 *v) const {
+    constexpr int J = kBeamPieces;
     const int first = c * 64 * J;
     if (whole(first) && whole(first + 64 * J - 1)) {
 #pragma unroll
@@ -155,9 +155,9 @@ struct Row {
 //
 // Bound by HBM and by the exponentials together: an element is 7.5 operations of
 // full rate, four of them its exponential's.
-template <typename T, int J>
+template <typename T>
 __global__ __launch_bounds__(kScanThreads, 4) void beam_scan_kernel(BeamSelectParams p) {
-  constexpr int N = Piece<T>::N;
+  constexpr int N = Piece<T>::N, J = kBeamPieces;
   const int lane = threadIdx.x & 63;
   const int64_t id = (int64_t)blockIdx.x * (kScanThreads / 64) + (threadIdx.x >> 6);
   const int row = (int)(id / p.waves), w = (int)(id - (int64_t)row * p.waves);
@@ -170,7 +170,7 @@ __global__ __launch_bounds__(kScanThreads, 4) void beam_scan_kernel(BeamSelectPa
   bool fresh = true;
   for (int c = c0; c < c1; ++c) {
     u32x4 v[J];
-    r.template load_chunk<J>(c, lane, v);
+    r.load_chunk(c, lane, v);
     float m = -INFINITY, part;
     for (;;) {
       if (fresh) {   // (by the first piece; by all of them where that was not enough)
@@ -231,16 +231,21 @@ __device__ __forceinline__ uint64_t candidate(float x, int token) { return (uint
 __device__ __forceinline__ float candidate_logit(uint64_t c) { return key_value((uint32_t)(c >> 32)); }
 __device__ __forceinline__ int candidate_token(uint64_t c) { return (int)~(uint32_t)c; }
 
-// The k-th largest of the lanes' values, or a value below it that no fewer than k lanes reach; finite.
-__device__ __forceinline__ float kth_of_lanes(float x, int k) {
-  const uint32_t key = order_key(x);
-  uint32_t t = 0;
-  for (int b = 31; b >= 0; --b) {
-    const uint32_t trial = t | 1u << b;
-    const int n = __popcll(__ballot(key >= trial));
-    if (n >= k) t = trial;
-    if (n == k) break;
+// A value that k lanes reach, the k-th largest of theirs less 2^-17 of it at most;
+// finite. A lane's place by comparing it with all 64, by way of LDS (keys: [64], the
+// wave's own): bit by bit it took twice as long.
+__device__ __forceinline__ float kth_of_lanes(float x, int lane, int k, uint32_t *keys) {
+  const uint32_t key = (order_key(x) & ~63u) | (63 - lane);   // (all different)
+  keys[lane] = key;
+  wave_lds_fence();
+  int place = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const u32x4 o = reinterpret_cast<const u32x4 *>(keys)[i];
+    place += (o[0] > key) + (o[1] > key) + (o[2] > key) + (o[3] > key);
   }
+  wave_lds_fence();
+  const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)key, __builtin_ctzll(__ballot(place == k - 1))) & ~63u;
   return t > order_key(-FLT_MAX) ? key_value(t) : -FLT_MAX;
 }
 
@@ -318,17 +323,18 @@ __device__ __forceinline__ float largest_of_lane(const float *at, int chunks, co
 // to a group, kLook pieces to a lane at a time. (The kernel runs through its code
 // once, so that fetching it counts: each part is there once, and what is seldom
 // needed is out of the way.)
-template <typename T, int J>
+template <typename T>
 __device__ __forceinline__ void best_of_row(const BeamSelectParams &p, int row, int lane, int *groups, GroupTile &tile, BeamList &list) {
-  constexpr int N = Piece<T>::N, G = 64 / J, E = kLook * N;
+  constexpr int N = Piece<T>::N, J = kBeamPieces, G = 64 / J, E = kLook * N;
   const Row<T> r(p, row);
   const float *gm = p.group_max + (int64_t)row * p.chunks * 64 + lane;
   for (int c0 = 0;; c0 += kTile) {
     const bool last = c0 + kTile >= p.chunks;
     if (c0) tile.load(gm + c0 * 64, p.chunks - c0);
-    uint64_t mine = 0;   // the lane's groups in the tile that may have something
+    uint32_t of[2] = {0, 0};
 #pragma unroll
-    for (int c = 0; c < kTile; ++c) mine |= (uint64_t)(tile.g[c] >= list.least) << c;
+    for (int c = 0; c < kTile; ++c) of[c / 32] |= tile.g[c] >= list.least ? 1u << c % 32 : 0u;
+    uint64_t mine = (uint64_t)of[1] << 32 | of[0];   // the lane's groups in the tile that may have something
     if (last) mine &= ~0ull >> (64 - (p.chunks - c0));
     for (bool more = true; more;) {
       int n = 0;   // groups listed
@@ -416,11 +422,10 @@ __device__ __forceinline__ double sum_error(double ln_vocab, double ln_sum, doub
 // One batch entry, a wave to a beam. The largest score of any group with index l mod
 // 64 is the l-th of 64 values; as many groups as there are values above it reach the
 // k-th largest of these, and only logits that reach it are looked for: hardly more
-// than k of all beams together. Then a candidate's place is the number of candidates
-// ahead of it; those of another beam are sorted, too. Where two beams' candidates
-// are closer than their sums are exact, those sums are made again in fp64 and the
-// places counted again.
-template <typename T, int J>
+// than k of all beams together. Then a candidate's place is the number of those
+// ahead of it. Where two beams' candidates are closer than their sums are exact,
+// those sums are made again in fp64 and the places counted again.
+template <typename T>
 __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParams p) {
   constexpr int W = kPickThreads / 64;
   extern __shared__ char smem[];
@@ -437,8 +442,16 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
   int *again = count + n_beams;                      // [beams] to be summed again
   int *inside = again + n_beams;                     // [beams] candidates among the k
   int *order = inside + n_beams;                     // [k] candidate of each place, or -1
-  float *best = (float *)(order + k);                // [W][64]
+  int *pool_size = order + k;
+  int *pool = pool_size + 1;                         // [kPickThreads] the candidates of all beams, if there are so few
+  float *best = (float *)(pool + kPickThreads);      // [W][64]
   int *groups = (int *)(best + W * 64) + wave * kListCap;    // [W][kListCap]
+  if (tid == 0) *pool_size = 0;
+  auto put = [&](int i, int n) {   // candidates 0 .. n - 1 of beam i into the pool
+    int at = lane == 0 ? atomicAdd(pool_size, n) : 0;
+    at = __builtin_amdgcn_readfirstlane(at);
+    if (lane < n && at + lane < kPickThreads) pool[at + lane] = i * 64 + lane;
+  };
   GroupTile tile;
   float most_of_lane = -INFINITY;
   for (int i = wave; i < n_beams; i += W) {
@@ -494,11 +507,20 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
   }
   best[wave * 64 + lane] = most_of_lane;
   __syncthreads();
+  // (One wave for all: with eight at it the LDS is what they wait for, 1.3 us instead of 0.6.)
+  if (wave == 0) {
 #pragma unroll
-  for (int w = 0; w < W; ++w) most_of_lane = fmaxf(most_of_lane, best[w * 64 + lane]);
-  const double reached = kth_of_lanes(most_of_lane, k);
+    for (int w = 0; w < W; ++w) most_of_lane = fmaxf(most_of_lane, best[w * 64 + lane]);
+    const float t = kth_of_lanes(most_of_lane, lane, k, (uint32_t *)found);
+    if (lane == 0) best[0] = t;
+  }
+  __syncthreads();
+  const double reached = best[0];
   for (int i = wave; i < n_beams; i += W) {
-    if (count[i] >= 0) continue;
+    if (count[i] >= 0) {
+      put(i, count[i]);
+      continue;
+    }
     const int row = b * n_beams + i;
     if (n_beams > W) tile.load(p.group_max + (int64_t)row * p.chunks * 64 + lane, p.chunks);
     // (Lower by what the scores and their rounding to fp32 may be off, and by a step of fp32 for the rounding here.)
@@ -506,63 +528,87 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
     // (Without k values to go by, whatever a beam has may be wanted.)
     const float least = reached > -FLT_MAX ? fmaxf((float)(bound - slack), -FLT_MAX) : -FLT_MAX;
     BeamList list{0, found, 0, 0, k, least};
-    best_of_row<T, J>(p, row, lane, groups, tile, list);
+    best_of_row<T>(p, row, lane, groups, tile, list);
     if (lane < list.count) {
       score[i * 64 + lane] = own[i] + ((double)candidate_logit(list.best) - ref[i]) - ln[i];
       token[i * 64 + lane] = candidate_token(list.best);
     }
     if (lane == 0) count[i] = list.count;
+    put(i, list.count);
   }
-  // Up to four threads share a candidate, each with every fourth beam.
-  const int log_k = 32 - __builtin_clz(k - 1 | 1), total = n_beams << log_k;
-  const int share = total <= kPickThreads / 4 ? 2 : total <= kPickThreads / 2 ? 1 : 0;
-  double unsure = lane < n_beams ? error[lane] : 0.0;   // (twice the largest error of any beam's sum)
+  // The places. Beams are told apart by sums that are made again where a candidate that may be among the k is closer
+  // to another beam's than unsure, twice what a sum may be off.
+  double unsure = lane < n_beams ? error[lane] : 0.0;
   unsure = -2.0 * wave_min(-unsure);
+  __syncthreads();
+  const int total = *pool_size, n = min(total, k);
   for (int round = 0;; ++round) {
-    for (int i = tid; i < k; i += kPickThreads) order[i] = -1;
-    for (int i = tid; i < n_beams; i += kPickThreads) inside[i] = 0;
-    __syncthreads();
-    for (int q = tid >> share; q < total; q += kPickThreads >> share) {
-      const int i = q >> log_k, at = q & ((1 << log_k) - 1), c = i * 64 + at;
-      if (at >= count[i]) continue;
-      const double mine = score[c];
-      int place = 0;
-      for (int j = tid & ((1 << share) - 1); j < n_beams && place < k; j += 1 << share) {
-        if (j == i) continue;
-        // lo of its candidates are ahead: found by doubling steps, then halving them.
-        const double *s = score + j * 64;
-        auto ahead = [&](int e) { return s[e] > mine || (s[e] == mine && j < i); };
-        int lo = 0, hi = count[j];
-        for (int step = 1; lo + step <= hi && ahead(lo + step - 1); step *= 2) lo += step;
-        for (int step = 32; step; step /= 2)
-          if (lo + step <= hi && ahead(lo + step - 1)) lo += step;
-        place += lo;
-      }
-      if (share > 0) place += lane_move<kSwap1>(0, place);
-      if (share > 1) place += lane_move<kSwap2>(0, place);
-      place += at;
-      if (place < k) {
-        order[place] = c;
-        if (round == 0 && (tid & ((1 << share) - 1)) == 0) atomicAdd(&inside[i], 1);
-      }
-    }
-    __syncthreads();
-    if (round == 1) break;
-    // Beams whose order is not certain: neighbours among the k that are closer than unsure, and any of the k and
-    // the best of another beam's others. Whatever else is as close is so by way of such pairs.
     bool near = false;
-    auto tell_apart = [&](int c0, int c1) {
-      if (c0 < 0 || c1 < 0 || c0 >> 6 == c1 >> 6 || score[c0] - score[c1] >= unsure) return;
-      near = true;
-      again[c0 >> 6] = again[c1 >> 6] = 1;
-    };
-    for (int q = tid; q < total; q += kPickThreads) {
-      const int j = q >> log_k, at = q & ((1 << log_k) - 1);
-      if (at >= k) continue;
-      if (inside[j] < count[j]) tell_apart(order[at], j * 64 + inside[j]);
-      if (j == 0 && at + 1 < k) tell_apart(order[at], order[at + 1]);
+    if (total <= kPickThreads) {   // (each with every other; four threads to a candidate where there are enough)
+      const int share = total <= kPickThreads / 4 ? 2 : 0, q = tid >> share;
+      int c = 0;
+      double mine = 0.0;
+      bool touched = false;
+      if (q < total) {
+        c = pool[q];
+        mine = score[c];
+        int place = 0;
+#pragma unroll 4
+        for (int e = tid & ((1 << share) - 1); e < total; e += 1 << share) {
+          const int o = pool[e];
+          const double gap = score[o] - mine;
+          place += gap > 0.0 || (gap == 0.0 && o < c);
+          touched |= fabs(gap) < unsure && (o ^ c) >= 64;
+        }
+        if (share) place += lane_move<kSwap1>(0, place);
+        if (share) place += lane_move<kSwap2>(0, place);
+        if (place < k) order[place] = c;
+      }
+      __syncthreads();
+      near = touched && mine > score[order[n - 1]] - unsure;
+      if (near) again[c >> 6] = 1;
+    } else {
+      // Masses of equal candidates. Those of another beam are sorted: how many are ahead is found by doubling steps,
+      // then halving them.
+      const int log_k = 32 - __builtin_clz(k - 1 | 1), slots = n_beams << log_k;
+      for (int i = tid; i < n_beams; i += kPickThreads) inside[i] = 0;
+      __syncthreads();
+      for (int q = tid; q < slots; q += kPickThreads) {
+        const int i = q >> log_k, c = i * 64 + (q & ((1 << log_k) - 1));
+        if (c - i * 64 >= count[i]) continue;
+        const double mine = score[c];
+        int place = c - i * 64;
+        for (int j = 0; j < n_beams && place < k; ++j) {
+          if (j == i) continue;
+          const double *s = score + j * 64;
+          auto ahead = [&](int e) { return s[e] > mine || (s[e] == mine && j < i); };
+          int lo = 0, hi = count[j];
+          for (int step = 1; lo + step <= hi && ahead(lo + step - 1); step *= 2) lo += step;
+          for (int step = 32; step; step /= 2)
+            if (lo + step <= hi && ahead(lo + step - 1)) lo += step;
+          place += lo;
+        }
+        if (place < k) {
+          order[place] = c;
+          atomicAdd(&inside[i], 1);
+        }
+      }
+      __syncthreads();
+      // Neighbours among the k, and any of the k and the best of another beam's others: whatever else is as close is so
+      // by way of such pairs.
+      auto tell_apart = [&](int c0, int c1) {
+        if (c0 >> 6 == c1 >> 6 || score[c0] - score[c1] >= unsure) return;
+        near = true;
+        again[c0 >> 6] = again[c1 >> 6] = 1;
+      };
+      for (int q = tid; q < slots; q += kPickThreads) {
+        const int j = q >> log_k, at = q & ((1 << log_k) - 1);
+        if (at >= n) continue;
+        if (inside[j] < count[j]) tell_apart(order[at], j * 64 + inside[j]);
+        if (j == 0 && at + 1 < n) tell_apart(order[at], order[at + 1]);
+      }
     }
-    if (!__syncthreads_or(near)) break;
+    if (round == 1 || !__syncthreads_or(near)) break;
     // exp(d) = 2^n 2^(j/32) exp(r), |r| <= ln 2 / 64: a table and a polynomial of degree 4 (2e-12 off), 16
     // instructions an element. In the order of the tokens, wherever a row begins: rows alike have equal sums.
     double *table = (double *)found - wave * 64;
@@ -592,9 +638,6 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
       __syncthreads();
     }
   }
-  int n = 0;
-  for (int i = 0; i < n_beams; ++i) n += count[i];
-  n = min(n, k);
   for (int i = tid; i < k; i += kPickThreads) {
     const int64_t at = (int64_t)b * k + i;
     if (i < n) {
@@ -654,21 +697,17 @@ __global__ __launch_bounds__(256) void beam_reorder_kernel(BeamReorderParams p) 
 hipError_t launch_beam_scan(const BeamSelectParams &p, DType dt, hipStream_t s) {
   const int64_t waves = (int64_t)p.batch * p.beams * p.waves, per_wg = kScanThreads / 64;
   const dim3 grid((unsigned)((waves + per_wg - 1) / per_wg)), threads(kScanThreads);
-  if (dt == kBF16 && p.pieces == 8) hipLaunchKernelGGL((beam_scan_kernel<__bf16, 8>), grid, threads, 0, s, p);
-  else if (dt == kBF16) hipLaunchKernelGGL((beam_scan_kernel<__bf16, 2>), grid, threads, 0, s, p);
-  else if (p.pieces == 8) hipLaunchKernelGGL((beam_scan_kernel<float, 8>), grid, threads, 0, s, p);
-  else hipLaunchKernelGGL((beam_scan_kernel<float, 2>), grid, threads, 0, s, p);
+  if (dt == kBF16) hipLaunchKernelGGL(beam_scan_kernel<__bf16>, grid, threads, 0, s, p);
+  else hipLaunchKernelGGL(beam_scan_kernel<float>, grid, threads, 0, s, p);
   return hipGetLastError();
 }
 
 hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s) {
   constexpr int waves = kPickThreads / 64;
-  const size_t lds = (size_t)p.beams * (64 * 12 + 44) + (size_t)waves * (8 + 64 * 8 + 64 * 4 + 4 * kListCap) + (size_t)p.k * 4;
+  const size_t lds = (size_t)p.beams * (64 * 12 + 44) + (size_t)waves * (8 + 64 * 8 + 64 * 4 + 4 * kListCap) + ((size_t)p.k + 1 + kPickThreads) * 4;
   const dim3 grid((unsigned)p.batch), threads(kPickThreads);
-  if (dt == kBF16 && p.pieces == 8) hipLaunchKernelGGL((beam_pick_kernel<__bf16, 8>), grid, threads, lds, s, p);
-  else if (dt == kBF16) hipLaunchKernelGGL((beam_pick_kernel<__bf16, 2>), grid, threads, lds, s, p);
-  else if (p.pieces == 8) hipLaunchKernelGGL((beam_pick_kernel<float, 8>), grid, threads, lds, s, p);
-  else hipLaunchKernelGGL((beam_pick_kernel<float, 2>), grid, threads, lds, s, p);
+  if (dt == kBF16) hipLaunchKernelGGL(beam_pick_kernel<__bf16>, grid, threads, lds, s, p);
+  else hipLaunchKernelGGL(beam_pick_kernel<float>, grid, threads, lds, s, p);
   return hipGetLastError();
 }
 

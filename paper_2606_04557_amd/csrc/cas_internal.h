@@ -381,8 +381,9 @@ static_assert(sizeof(PageCopyParams) + sizeof(PageCopyList) <= 4096, "kernel arg
 
 // Beam search: choosing the candidates of a step. Row r = batch entry r / beams,
 // beam r % beams. A row is cut into 16-byte pieces at aligned addresses (the first
-// and the last may be partial); piece 64 (J c + j) + lane of it is the j-th of lane
-// `lane` in chunk c. A group is what one lane has of one chunk: J pieces.
+// and the last may be partial); piece 64 (8 c + j) + lane of it is the j-th of lane
+// `lane` in chunk c. A group is what one lane has of one chunk: 8 pieces.
+constexpr int kBeamPieces = 8;
 struct DevBeamPart {
   double sum;   // of exp(x - base) over a wave's chunks
   double base;
@@ -398,7 +399,6 @@ struct BeamSelectParams {
   int32_t chunks;             // of a row
   int32_t per_wave;           // chunks of a wave
   int32_t waves;              // of a row
-  int32_t pieces;             // J, 8 or 2
   double ln_vocab;
   float *group_max;           // [row][chunk][64] the largest logit of every group
   DevBeamPart *parts;         // [row][wave]
