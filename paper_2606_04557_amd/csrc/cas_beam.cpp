@@ -120,11 +120,11 @@ cas_status_t select(const cas_beam_problem_t *p, const void *logits, const float
   return e == hipSuccess ? CAS_OK : set_hip_error("beam_pick launch", e);
 }
 
-// The widest moves that addresses and strides allow.
-int32_t widest(const cas_beam_state_t &t) {
+// The widest moves that addresses and strides allow: 16, 4 or 1 bytes (their logarithm).
+int32_t log_unit(const cas_beam_state_t &t) {
   const uintptr_t all = (uintptr_t)t.x | (uintptr_t)t.y | (uintptr_t)t.x_stride_batch | (uintptr_t)t.x_stride_beam |
-                        (uintptr_t)t.y_stride_batch | (uintptr_t)t.y_stride_beam | 16u;
-  return (int32_t)(all & (~all + 1));
+                        (uintptr_t)t.y_stride_batch | (uintptr_t)t.y_stride_beam;
+  return all % 16 == 0 ? 4 : all % 4 == 0 ? 2 : 0;
 }
 
 cas_status_t reorder(const int32_t *parents, int32_t batch, int32_t beams_in, int32_t beams_out, const cas_beam_state_t *ts,
@@ -162,7 +162,7 @@ cas_status_t reorder(const int32_t *parents, int32_t batch, int32_t beams_in, in
       return refuse(CAS_ERR_INVALID_ARGUMENT, "in place, x and y must have equal beams and strides");
     which[m] = i;
     p.t[m++] = DevBeamState{(const char *)t.x, (char *)t.y, t.row_bytes, t.x_stride_batch, t.x_stride_beam, t.y_stride_batch,
-                            t.y_stride_beam, widest(t)};
+                            t.y_stride_beam, log_unit(t)};
   }
   if (m == 0) return CAS_OK;
   for (int i = 0; i < m; ++i) {

@@ -7,6 +7,8 @@
 // among those of its beams. Equal scores go by beam, then token.
 #include <float.h>
 
+#include <algorithm>
+
 #include "cas_device.h"
 
 namespace cas {
@@ -16,6 +18,7 @@ namespace {
 constexpr int kScanThreads = 256;
 constexpr float kFarLogit = 64.0f;
 constexpr int kPickThreads = 512;
+constexpr int kReorderThreads = 256;
 constexpr int kListCap = 128;    // groups that a wave has found and not looked at yet
 constexpr int kLook = 3;         // pieces of such groups that a lane takes at a time
 
@@ -660,35 +663,51 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
   }
 }
 
-// A thread has the bytes at one place of every row of a batch entry: it loads them
-// all before it stores the first, so that a reordering in place needs no copy.
+// Reordering. A thread has the bytes at one place of every row of a batch entry: it
+// loads them all before it stores the first, so that a reordering in place needs no
+// copy. Bound by HBM: every row that is a parent is read once (its further children
+// find it in the cache), every other one written.
 template <typename U, int N>
-__device__ __forceinline__ void move(const DevBeamState &t, const int *parents, int n, int n_in, int64_t at, const char *x, char *y) {
+__device__ __forceinline__ void move(const char *x, int64_t xi, char *y, int64_t yi, int parent_of_lane, int n, int n_in, uint32_t at) {
   U v[N];
+  const char *row = x;   // (of the last parent that was in range: what has no row of its own loads that, without a branch)
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (j < n && (unsigned)parents[j] < (unsigned)n_in) v[j] = *reinterpret_cast<const U *>(x + parents[j] * t.xi + at);
+  for (int j = 0; j < N; ++j) {
+    const int parent = __builtin_amdgcn_readlane(parent_of_lane, j);
+    row = j < n && (unsigned)parent < (unsigned)n_in ? x + parent * xi : row;
+    v[j] = *reinterpret_cast<const U *>(row + at);
+  }
 #pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (j < n && (unsigned)parents[j] < (unsigned)n_in) *reinterpret_cast<U *>(y + j * t.yi + at) = v[j];
+  for (int j = 0; j < N; ++j) {
+    const int parent = __builtin_amdgcn_readlane(parent_of_lane, j);
+    if (j < n && (unsigned)parent < (unsigned)n_in && !(x == y && parent == j)) *reinterpret_cast<U *>(y + j * yi + at) = v[j];
+  }
 }
 
 template <int N>
-__global__ __launch_bounds__(256) void beam_reorder_kernel(BeamReorderParams p) {
+__global__ __launch_bounds__(kReorderThreads) void beam_reorder_kernel(BeamReorderParams p) {
   const DevBeamState t = p.t[blockIdx.z];
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, whole = t.row_bytes / t.unit, rest = t.row_bytes - whole * t.unit;
-  if (i >= whole + rest) return;
+  const int n = p.beams_out, n_in = p.beams_in, lane = threadIdx.x & 63, log_unit = t.log_unit;
+  // Whole units, then (from the next wave on) the bytes behind them.
+  const int64_t whole = t.row_bytes >> log_unit, rest0 = (whole + 63) & ~(int64_t)63, rest = t.row_bytes - (whole << log_unit);
+#pragma unroll 1
   for (int b = blockIdx.y; b < p.batch; b += gridDim.y) {
-    const int *parents = p.parents + (int64_t)b * p.beams_out;
-    const char *x = t.x + b * t.xb;
-    char *y = t.y + b * t.yb;
-    const int n = p.beams_out, n_in = p.beams_in;
-    if (i >= whole) move<uint8_t, N>(t, parents, n, n_in, whole * t.unit + i - whole, x, y);
-    else if (t.unit == 16) move<u32x4, N>(t, parents, n, n_in, i * 16, x, y);
-    else if (t.unit == 8) move<uint64_t, N>(t, parents, n, n_in, i * 8, x, y);
-    else if (t.unit == 4) move<uint32_t, N>(t, parents, n, n_in, i * 4, x, y);
-    else if (t.unit == 2) move<uint16_t, N>(t, parents, n, n_in, i * 2, x, y);
-    else move<uint8_t, N>(t, parents, n, n_in, i, x, y);
+    const int parent = p.parents[(int64_t)b * n + min(lane, n - 1)];
+#pragma unroll 1
+    for (int64_t i0 = (int64_t)blockIdx.x * kReorderThreads; i0 < rest0 + rest; i0 += (int64_t)gridDim.x * kReorderThreads) {
+      const char *x = t.x + b * t.xb + (i0 << log_unit);
+      char *y = t.y + b * t.yb + (i0 << log_unit);
+      const int64_t i = i0 + threadIdx.x;
+      if (i < whole) {
+        const uint32_t at = threadIdx.x << log_unit;
+        if (log_unit == 4) move<u32x4, N>(x, t.xi, y, t.yi, parent, n, n_in, at);
+        else if (log_unit == 2) move<uint32_t, N>(x, t.xi, y, t.yi, parent, n, n_in, at);
+        else move<uint8_t, N>(x, t.xi, y, t.yi, parent, n, n_in, at);
+      } else if (i >= rest0 && i < rest0 + rest) {
+        const int64_t back = (whole << log_unit) - (i0 << log_unit);   // (may be before this workgroup's first unit)
+        move<uint8_t, N>(x + back, t.xi, y + back, t.yi, parent, n, n_in, (uint32_t)(i - rest0));
+      }
+    }
   }
 }
 
@@ -714,11 +733,11 @@ hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s) 
 hipError_t launch_beam_reorder(const BeamReorderParams &p, int n, hipStream_t s) {
   int64_t most = 0;
   for (int i = 0; i < n; ++i) {
-    const int64_t whole = p.t[i].row_bytes / p.t[i].unit;
-    most = whole + (p.t[i].row_bytes - whole * p.t[i].unit) > most ? whole + (p.t[i].row_bytes - whole * p.t[i].unit) : most;
+    const int64_t whole = p.t[i].row_bytes >> p.t[i].log_unit, rest = p.t[i].row_bytes - (whole << p.t[i].log_unit);
+    most = std::max(most, ((whole + 63) & ~(int64_t)63) + rest);
   }
-  const int64_t blocks = (most + 255) / 256;
-  const dim3 grid((unsigned)blocks, (unsigned)(p.batch < 65535 ? p.batch : 65535), (unsigned)n), threads(256);
+  const int64_t blocks = std::min<int64_t>((most + kReorderThreads - 1) / kReorderThreads, 1 << 20);
+  const dim3 grid((unsigned)blocks, (unsigned)std::min(p.batch, 65535), (unsigned)n), threads(kReorderThreads);
   if (p.beams_out <= 4) hipLaunchKernelGGL(beam_reorder_kernel<4>, grid, threads, 0, s, p);
   else if (p.beams_out <= 8) hipLaunchKernelGGL(beam_reorder_kernel<8>, grid, threads, 0, s, p);
   else if (p.beams_out <= 16) hipLaunchKernelGGL(beam_reorder_kernel<16>, grid, threads, 0, s, p);

@@ -409,7 +409,7 @@ struct DevBeamState {
   const char *x;
   char *y;
   int64_t row_bytes, xb, xi, yb, yi;
-  int32_t unit;               // bytes that a thread moves at a time
+  int32_t log_unit;           // of the bytes that a thread moves at a time: 4, 2 or 0
 };
 constexpr int kBeamStates = 8;
 constexpr int kMaxBeams = 64;
