@@ -367,7 +367,7 @@ static_assert(sizeof(ChunkParams) % 8 == 0 && sizeof(ChunkParams) + sizeof(Chunk
 // `piece` bytes, of copy first + x / pieces in pool y.
 constexpr int kPageCopyArgs = 240;    // copies that travel as kernel arguments
 constexpr int kPageCopyPools = 64;    // pools of a launch
-constexpr int kPagePiece = 16384;
+constexpr int kPagePiece = 8192;      // a piece is one, two or four of these
 struct PageCopyParams {
   char *pools[kPageCopyPools];
   int64_t page_bytes, row_bytes;
