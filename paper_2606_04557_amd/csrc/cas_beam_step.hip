@@ -489,7 +489,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
         sum = wave_sum(sum);
         if (sum > 0.0 && sum < INFINITY) {
           n = -1;
-          ln_sum = log(sum);
+          ln_sum = fmax(log(sum), 0.0);   // (of a sum that has the term 1: no token is likelier than certain)
           lowest = wave_min(lowest);
           off = sum_error(p.ln_vocab, ln_sum, fmax(most - lowest, 0.0), most, most > kFarLogit - 1 || lowest < 1 - kFarLogit);
           most_of_lane = fmaxf(most_of_lane, (float)(so_far + ((double)x - most) - ln_sum));
