@@ -8,6 +8,7 @@
 #include <float.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cas_device.h"
 
@@ -17,10 +18,16 @@ namespace {
 
 constexpr int kScanThreads = 256;
 constexpr float kFarLogit = 64.0f;
-constexpr int kPickThreads = 512;
 constexpr int kReorderThreads = 256;
 constexpr int kListCap = 128;    // groups that a wave has found and not looked at yet
-constexpr int kLook = 3;         // pieces of such groups that a lane takes at a time
+
+// The pick's waves, and what their registers hold: the first kTile chunks' group maxima, and kLook pieces of groups
+// that are looked at. More than 8 beams have 16 waves: 9 of 32,000 bf16 13.3 us instead of 16.2, 64 of them 33.8
+// instead of 45.6.
+template <int W>
+struct PickShape {
+  static constexpr int kThreads = 64 * W, kTile = W == 8 ? 40 : 24, kLook = W == 8 ? 3 : 2;
+};
 
 // Whether beam `row` has nothing to choose from by its own state.
 __device__ __forceinline__ bool out_of_search(const BeamSelectParams &p, int row) {
@@ -234,22 +241,27 @@ __device__ __forceinline__ uint64_t candidate(float x, int token) { return (uint
 __device__ __forceinline__ float candidate_logit(uint64_t c) { return key_value((uint32_t)(c >> 32)); }
 __device__ __forceinline__ int candidate_token(uint64_t c) { return (int)~(uint32_t)c; }
 
-// A value that k lanes reach, the k-th largest of theirs less 2^-17 of it at most;
-// finite. A lane's place by comparing it with all 64, by way of LDS (keys: [64], the
-// wave's own): bit by bit it took twice as long.
-__device__ __forceinline__ float kth_of_lanes(float x, int lane, int k, uint32_t *keys) {
-  const uint32_t key = (order_key(x) & ~63u) | (63 - lane);   // (all different)
-  keys[lane] = key;
-  wave_lds_fence();
-  int place = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
+// The k-th largest of N values: each has a key of its own, whose low bits are its index, and counts the keys that are
+// larger (in LDS; bit by bit, with ballots, it took twice as long).
+template <int N>
+__device__ __forceinline__ uint32_t distinct_key(float x, int i) {
+  return (order_key(x) & ~(uint32_t)(N - 1)) | (N - 1 - i);
+}
+template <int N>
+__device__ __forceinline__ int ahead_of(uint32_t key, const uint32_t *keys) {
+  int n = 0;
+#pragma unroll 16
+  for (int i = 0; i < N / 4; ++i) {
     const u32x4 o = reinterpret_cast<const u32x4 *>(keys)[i];
-    place += (o[0] > key) + (o[1] > key) + (o[2] > key) + (o[3] > key);
+    n += (o[0] > key) + (o[1] > key) + (o[2] > key) + (o[3] > key);
   }
-  wave_lds_fence();
-  const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)key, __builtin_ctzll(__ballot(place == k - 1))) & ~63u;
-  return t > order_key(-FLT_MAX) ? key_value(t) : -FLT_MAX;
+  return n;
+}
+// The value, or up to 2^-15 of it less; finite.
+template <int N>
+__device__ __forceinline__ float finite_value(uint32_t key) {
+  key &= ~(uint32_t)(N - 1);
+  return key > order_key(-FLT_MAX) ? key_value(key) : -FLT_MAX;
 }
 
 // The best logits of a row that a wave has found: `count` (at most k) of them in its
@@ -284,41 +296,37 @@ struct BeamList {
 };
 
 // The largest logits of the row's groups, kTile chunks at a time (the first ones stay in registers).
-constexpr int kTile = 40;
+template <int kTile>
 struct GroupTile {
   float g[kTile];
   __device__ __forceinline__ void load(const float *at, int chunks) {
-    // (By eights, whose last ones repeat the row's last chunk: a branch for each would wait for what it loaded.)
+    // (By eights, with chunks from the front again behind the row's last: a branch for each would wait for what it loaded.)
 #pragma unroll
     for (int c = 0; c < kTile; c += 8) {
       if (c < chunks) {
 #pragma unroll
-        for (int i = c; i < c + 8; ++i) g[i] = at[min(i, chunks - 1) * 64];
+        for (int i = c; i < c + 8; ++i) g[i] = at[(i < chunks ? i : min(i & 3, chunks - 1)) * 64];
       } else {
 #pragma unroll
         for (int i = c; i < c + 8; ++i) g[i] = -INFINITY;
       }
     }
   }
-  __device__ __forceinline__ float largest() const {
-    float m = -INFINITY;
-#pragma unroll
-    for (int c = 0; c < kTile; ++c) m = fmaxf(m, g[c]);
-    return m;
-  }
 };
 
-// The largest of each lane's groups of a row, of which the tile has the first ones.
-__device__ __forceinline__ float largest_of_lane(const float *at, int chunks, const GroupTile &tile) {
-  float m = tile.largest();
+// The largest of each lane's groups of a row, of which the tile has the first ones, of its chunks i mod 4 (the first
+// of them stand in for chunks that the row does not have).
+template <int kTile>
+__device__ __forceinline__ void largest_of_lane(const float *at, int chunks, const GroupTile<kTile> &tile, float (&m)[4]) {
+#pragma unroll
+  for (int c = 0; c < kTile; ++c) m[c % 4] = fmaxf(c < 4 ? -INFINITY : m[c % 4], tile.g[c]);
   for (int c = kTile; c < chunks; c += 8) {
     float g[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) g[i] = at[min(c + i, chunks - 1) * 64];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = fmaxf(m, g[i]);
+    for (int i = 0; i < 8; ++i) m[i % 4] = fmaxf(m[i % 4], c + i < chunks ? g[i] : -INFINITY);
   }
-  return m;
 }
 
 // The logits of a row that are at least list.least, the k best of them. They are in
@@ -326,8 +334,9 @@ __device__ __forceinline__ float largest_of_lane(const float *at, int chunks, co
 // to a group, kLook pieces to a lane at a time. (The kernel runs through its code
 // once, so that fetching it counts: each part is there once, and what is seldom
 // needed is out of the way.)
-template <typename T>
-__device__ __forceinline__ void best_of_row(const BeamSelectParams &p, int row, int lane, int *groups, GroupTile &tile, BeamList &list) {
+template <typename T, int kTile, int kLook>
+__device__ __forceinline__ void best_of_row(const BeamSelectParams &p, int row, int lane, int *groups, GroupTile<kTile> &tile,
+                                            BeamList &list) {
   constexpr int N = Piece<T>::N, J = kBeamPieces, G = 64 / J, E = kLook * N;
   const Row<T> r(p, row);
   const float *gm = p.group_max + (int64_t)row * p.chunks * 64 + lane;
@@ -423,14 +432,14 @@ __device__ __forceinline__ double sum_error(double ln_vocab, double ln_sum, doub
 }
 
 // One batch entry, a wave to a beam. The largest score of any group with index l mod
-// 64 is the l-th of 64 values; as many groups as there are values above it reach the
-// k-th largest of these, and only logits that reach it are looked for: hardly more
-// than k of all beams together. Then a candidate's place is the number of those
+// 64 (or 256) is the l-th of 64 (256) values: k groups reach the k-th largest of these,
+// and only logits that reach it are looked for. Of k random ones among 64 values that
+// is hardly more than k in all while k is small, 44 for 32, but 300 for 64; among 256, 74. Then a candidate's place is the number of those
 // ahead of it. Where two beams' candidates are closer than their sums are exact,
 // those sums are made again in fp64 and the places counted again.
-template <typename T>
-__global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParams p) {
-  constexpr int W = kPickThreads / 64;
+template <typename T, int W>
+__global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamSelectParams p) {
+  constexpr int kPickThreads = PickShape<W>::kThreads;
   extern __shared__ char smem[];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_beams = p.beams, k = p.k;
   double *score = (double *)smem;                    // [beams][64] of a beam's candidates
@@ -439,24 +448,26 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
   double *ln = ref + n_beams;                        // [beams] ln sum exp(x - ref)
   double *error = ln + n_beams;                      // [beams] of the latter
   double *partial = error + n_beams;                 // [W]
-  uint64_t *found = (uint64_t *)(partial + W) + wave * 64;   // [W][64]
-  int *token = (int *)((uint64_t *)(partial + W) + W * 64);  // [beams][64]
+  float *values = (float *)(partial + W);            // [W][256], and then
+  uint64_t *found = (uint64_t *)(values + wave * 256);   // [W][64]
+  int *groups = (int *)(found + 64);                 // [W][kListCap]
+  int *pool = (int *)(values + W * 256);             // [kPickThreads] the candidates of all beams, if there are so few
+  int *token = pool + kPickThreads;                  // [beams][64]
   int *count = token + n_beams * 64;                 // [beams] -1: candidates of it are looked for
   int *again = count + n_beams;                      // [beams] to be summed again
   int *inside = again + n_beams;                     // [beams] candidates among the k
-  int *order = inside + n_beams;                     // [k] candidate of each place, or -1
+  int *order = inside + n_beams;                     // [k] candidate of each place
   int *pool_size = order + k;
-  int *pool = pool_size + 1;                         // [kPickThreads] the candidates of all beams, if there are so few
-  float *best = (float *)(pool + kPickThreads);      // [W][64]
-  int *groups = (int *)(best + W * 64) + wave * kListCap;    // [W][kListCap]
+  static_assert(64 * 2 + kListCap == 256, "a wave's share of the values");
   if (tid == 0) *pool_size = 0;
   auto put = [&](int i, int n) {   // candidates 0 .. n - 1 of beam i into the pool
     int at = lane == 0 ? atomicAdd(pool_size, n) : 0;
     at = __builtin_amdgcn_readfirstlane(at);
     if (lane < n && at + lane < kPickThreads) pool[at + lane] = i * 64 + lane;
   };
-  GroupTile tile;
-  float most_of_lane = -INFINITY;
+  GroupTile<PickShape<W>::kTile> tile;
+  const bool many = k > 32 && p.chunks >= 4;
+  float most_of_lane[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   for (int i = wave; i < n_beams; i += W) {
     const int row = b * n_beams + i;
     // (All that is needed is loaded at once; for a row out of the search it is not used.)
@@ -474,12 +485,14 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
         if (lane == 0) {
           score[i * 64] = so_far;
           token[i * 64] = p.pad;
-          most_of_lane = fmaxf(most_of_lane, so_far);
+          most_of_lane[0] = fmaxf(most_of_lane[0], so_far);
         }
       } else {
         // (A NaN or +inf among the logits is in the sum.)
-        const float x = largest_of_lane(gm, p.chunks, tile);
-        most = wave_max(x);
+        float x[4];
+        largest_of_lane(gm, p.chunks, tile, x);
+        if (!many) x[0] = fmaxf(max3(x[0], x[1], x[2]), x[3]);
+        most = wave_max(many ? fmaxf(max3(x[0], x[1], x[2]), x[3]) : x[0]);
         double sum = 0.0, lowest = INFINITY;
         for (int w = lane; w < p.waves; w += 64) {
           const DevBeamPart part = w < 64 ? first : parts[w];
@@ -492,7 +505,9 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
           ln_sum = fmax(log(sum), 0.0);   // (of a sum that has the term 1: no token is likelier than certain)
           lowest = wave_min(lowest);
           off = sum_error(p.ln_vocab, ln_sum, fmax(most - lowest, 0.0), most, most > kFarLogit - 1 || lowest < 1 - kFarLogit);
-          most_of_lane = fmaxf(most_of_lane, (float)(so_far + ((double)x - most) - ln_sum));
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i == 0 || many) most_of_lane[i] = fmaxf(most_of_lane[i], (float)(so_far + ((double)x[i] - most) - ln_sum));
         }
       }
       if (lane == 0) {
@@ -508,17 +523,30 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
       if (n == 0) error[i] = 0.0;
     }
   }
-  best[wave * 64 + lane] = most_of_lane;
-  __syncthreads();
-  // (One wave for all: with eight at it the LDS is what they wait for, 1.3 us instead of 0.6.)
-  if (wave == 0) {
+  float *limit = (float *)order;
 #pragma unroll
-    for (int w = 0; w < W; ++w) most_of_lane = fmaxf(most_of_lane, best[w * 64 + lane]);
-    const float t = kth_of_lanes(most_of_lane, lane, k, (uint32_t *)found);
-    if (lane == 0) best[0] = t;
+  for (int i = 0; i < 4; ++i)
+    if (i == 0 || many) values[wave * 256 + i * 64 + lane] = most_of_lane[i];
+  __syncthreads();
+  uint32_t *keys = (uint32_t *)pool;
+  if (many) {
+    float x = values[tid & 255];
+    for (int w = 1; w < W; ++w) x = fmaxf(x, values[w * 256 + (tid & 255)]);
+    const uint32_t key = distinct_key<256>(x, tid & 255);
+    if (tid < 256) keys[tid] = key;
+    __syncthreads();
+    if (tid < 256 && ahead_of<256>(key, keys) == k - 1) *limit = finite_value<256>(key);
+  } else if (wave == 0) {   // (one wave for all: with eight at it the LDS is what they wait for, 1.3 us instead of 0.6)
+    float x = values[lane];
+#pragma unroll
+    for (int w = 1; w < W; ++w) x = fmaxf(x, values[w * 256 + lane]);
+    const uint32_t key = distinct_key<64>(x, lane);
+    keys[lane] = key;
+    wave_lds_fence();
+    if (ahead_of<64>(key, keys) == k - 1) *limit = finite_value<64>(key);
   }
   __syncthreads();
-  const double reached = best[0];
+  const double reached = *limit;
   for (int i = wave; i < n_beams; i += W) {
     if (count[i] >= 0) {
       put(i, count[i]);
@@ -531,7 +559,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
     // (Without k values to go by, whatever a beam has may be wanted.)
     const float least = reached > -FLT_MAX ? fmaxf((float)(bound - slack), -FLT_MAX) : -FLT_MAX;
     BeamList list{0, found, 0, 0, k, least};
-    best_of_row<T>(p, row, lane, groups, tile, list);
+    best_of_row<T, PickShape<W>::kTile, PickShape<W>::kLook>(p, row, lane, groups, tile, list);
     if (lane < list.count) {
       score[i * 64 + lane] = own[i] + ((double)candidate_logit(list.best) - ref[i]) - ln[i];
       token[i * 64 + lane] = candidate_token(list.best);
@@ -614,7 +642,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(BeamSelectParam
     if (round == 1 || !__syncthreads_or(near)) break;
     // exp(d) = 2^n 2^(j/32) exp(r), |r| <= ln 2 / 64: a table and a polynomial of degree 4 (2e-12 off), 16
     // instructions an element. In the order of the tokens, wherever a row begins: rows alike have equal sums.
-    double *table = (double *)found - wave * 64;
+    double *table = (double *)values;
     if (tid < 32) table[tid] = exp2(tid / 32.0);
     __syncthreads();
     for (int i = 0; i < n_beams; ++i) {
@@ -722,11 +750,15 @@ hipError_t launch_beam_scan(const BeamSelectParams &p, DType dt, hipStream_t s) 
 }
 
 hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s) {
-  constexpr int waves = kPickThreads / 64;
-  const size_t lds = (size_t)p.beams * (64 * 12 + 44) + (size_t)waves * (8 + 64 * 8 + 64 * 4 + 4 * kListCap) + ((size_t)p.k + 1 + kPickThreads) * 4;
-  const dim3 grid((unsigned)p.batch), threads(kPickThreads);
-  if (dt == kBF16) hipLaunchKernelGGL(beam_pick_kernel<__bf16>, grid, threads, lds, s, p);
-  else hipLaunchKernelGGL(beam_pick_kernel<float>, grid, threads, lds, s, p);
+  auto launch = [&](auto waves) {
+    constexpr int W = decltype(waves)::value;
+    const size_t lds = (size_t)p.beams * (64 * 12 + 44) + (size_t)W * (8 + 1024) + ((size_t)p.k + 1 + PickShape<W>::kThreads) * 4;
+    const dim3 grid((unsigned)p.batch), threads(PickShape<W>::kThreads);
+    if (dt == kBF16) hipLaunchKernelGGL((beam_pick_kernel<__bf16, W>), grid, threads, lds, s, p);
+    else hipLaunchKernelGGL((beam_pick_kernel<float, W>), grid, threads, lds, s, p);
+  };
+  if (p.beams <= 8) launch(std::integral_constant<int, 8>{});
+  else launch(std::integral_constant<int, 16>{});
   return hipGetLastError();
 }
 
