@@ -138,18 +138,22 @@ struct Row {
       if (piece * N + i >= begin && piece * N + i < end) Piece<T>::put(v, i, base[piece * N + i]);
     return v;
   }
-  // A lane's pieces of chunk c.
+  // A lane's pieces of chunk c, in passing (64 x 8 rows of 131,072 bf16: 27.1 us, and 29.2 when the caches are to keep
+  // them).
+  __device__ __forceinline__ u32x4 load_once(int piece) const {
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + piece * N));
+  }
   __device__ __forceinline__ void load_chunk(int c, int lane, u32x4 *v) const {
     constexpr int J = kBeamPieces;
     const int first = c * 64 * J;
     if (whole(first) && whole(first + 64 * J - 1)) {
 #pragma unroll
-      for (int j = 0; j < J; ++j) v[j] = load(first + 64 * j + lane);
+      for (int j = 0; j < J; ++j) v[j] = load_once(first + 64 * j + lane);
     } else {
 #pragma unroll
       for (int j = 0; j < J; ++j) {
         const int piece = first + 64 * j + lane;
-        v[j] = whole(piece) ? load(piece) : load_partial(piece);
+        v[j] = whole(piece) ? load_once(piece) : load_partial(piece);
       }
     }
   }
@@ -169,8 +173,9 @@ template <typename T>
 __global__ __launch_bounds__(kScanThreads, 4) void beam_scan_kernel(BeamSelectParams p) {
   constexpr int N = Piece<T>::N, J = kBeamPieces;
   const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * (kScanThreads / 64) + (threadIdx.x >> 6);
-  const int row = (int)(id / p.waves), w = (int)(id - (int64_t)row * p.waves);
+  // (Scalar, so that what the wave begins with is scalar work, too.)
+  const unsigned id = blockIdx.x * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = (int)(id / (unsigned)p.waves), w = (int)(id - (unsigned)row * (unsigned)p.waves);
   if (row >= p.batch * p.beams || out_of_search(p, row)) return;
   const Row<T> r(p, row);
   const int c0 = w * p.per_wave, c1 = min(c0 + p.per_wave, p.chunks);
