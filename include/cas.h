@@ -640,8 +640,8 @@ cas_status_t cas_pages_copy(void *const *pools, int32_t n_pools, int64_t num_pag
  * beam leaves the search; the others of the batch entry go on).
  *
  * Candidates are ordered by their exact scores (compared in 64 bits where
- * 32 do not tell them apart), equal ones by beam and then token, lowest first;
- * out_scores are rounded once. Should there be fewer than k above -inf, the
+ * 32 do not tell them apart), equal ones by beam and then token, lowest first.
+ * out_scores are within 6e-6 of the exact ones, and rounded once. Should there be fewer than k above -inf, the
  * others follow in that order with the score -inf: parents and tokens are always
  * in range.
  *
