@@ -621,7 +621,7 @@ cas_status_t cas_page_table_lists(const cas_page_table_t *table, const int64_t *
  * The copies are host memory, read during the call. Up to 240 travel as kernel
  * arguments. The list of more goes through a workspace of the size that
  * cas_pages_copy_workspace_size gives for n copies (0 up to 240, where NULL will
- * do); calls that run at the same time need a workspace each, as do captured
+ * do; no larger from 65,536 on); calls that run at the same time need a workspace each, as do captured
  * graphs that may.
  */
 cas_status_t cas_pages_copy_workspace_size(int32_t n, size_t *bytes);

@@ -921,8 +921,14 @@ class PagePools:
 def _copy_list(copies) -> Tuple[object, int, int]:
     """(what keeps the memory, address, entries) of a list of copies."""
     import numpy as np
-    a = np.ascontiguousarray(copies, dtype=np.int32) if not (isinstance(copies, np.ndarray) and copies.dtype == np.int32
-                                                             and copies.flags.c_contiguous) else copies
+    a = copies
+    if not (isinstance(a, np.ndarray) and a.dtype == np.int32 and a.flags.c_contiguous):
+        b = np.asarray(copies)
+        if b.size and b.dtype.kind not in "iu":
+            raise TypeError("copies must be whole numbers")
+        a = np.ascontiguousarray(b, dtype=np.int32)
+        if (a != b).any():
+            raise ValueError("copies: a number beyond 32 bits")
     if a.size == 0:
         return a, 0, 0
     if a.ndim != 2 or a.shape[1] != 3:

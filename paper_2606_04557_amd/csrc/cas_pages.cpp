@@ -277,7 +277,11 @@ cas_status_t check_copies(const cas_page_copy_t *c, int32_t n, int64_t num_pages
   return CAS_OK;
 }
 
-size_t table_bytes(int32_t n) { return n <= kPageCopyArgs ? 0 : ((size_t)n * sizeof(cas_page_copy_t) + 15) / 16 * 16; }
+constexpr int32_t kTableCopies = 1 << 16;   // of a list at a time (786 KB)
+
+size_t table_bytes(int32_t n) {
+  return n <= kPageCopyArgs ? 0 : ((size_t)std::min(n, kTableCopies) * sizeof(cas_page_copy_t) + 15) / 16 * 16;
+}
 
 // Bytes of a workgroup's piece. Whole pages go fastest with one 16-byte load to a
 // thread (8,192 of 32 KB in two pools: 172 us; with two 187, four 194). Where copies are of
@@ -323,27 +327,32 @@ cas_status_t copy_pages(void *const *pools, int32_t n_pools, int64_t num_pages, 
   if (need) iv.push_back({(uintptr_t)workspace, (uintptr_t)workspace + need, true, 0, "the workspace"});
   std::string msg;
   if (!overlap_free(iv, msg)) return set_error(CAS_ERR_INVALID_ARGUMENT, msg);
-  PageCopyList list;
-  if (need) {
-    s = upload_call_tables(need, workspace, stream, [&](char *h) { std::memcpy(h, c, (size_t)n * sizeof(cas_page_copy_t)); });
-    if (s != CAS_OK) return s;
-  } else {
-    std::memcpy(list.copies, c, (size_t)n * sizeof(cas_page_copy_t));
-  }
   PageCopyParams p;
   p.row_bytes = row_bytes;
   p.page_bytes = row_bytes * page_size;
   p.table = need ? (const cas_page_copy_t *)workspace : nullptr;
   p.piece = piece_bytes(all_rows, rows, n, row_bytes, n_pools);
   p.pieces = (int32_t)((rows * row_bytes + p.piece - 1) / p.piece);
-  const int32_t most = std::max(1, (1 << 23) / p.pieces);   // copies of a launch, of under 2^31 threads
-  for (int32_t pool0 = 0; pool0 < n_pools; pool0 += kPageCopyPools) {
-    const int32_t m = std::min(kPageCopyPools, n_pools - pool0);
-    for (int32_t i = 0; i < m; ++i) p.pools[i] = (char *)pools[pool0 + i];
-    for (p.first = 0; p.first < n; p.first += most) {
-      const int32_t k = std::min(most, n - p.first);
-      const hipError_t e = timed_launch("page_copy", stream, [&] { return launch_page_copy(p, need ? nullptr : &list, k, m, stream); });
-      if (e != hipSuccess) return set_hip_error("page_copy launch", e);
+  const int32_t most = std::max(1, (1 << 21) / p.pieces);   // copies of a launch, of at most 2^31 threads
+  for (int32_t from = 0; from < n; from += kTableCopies) {
+    const int32_t listed = std::min(kTableCopies, n - from);
+    PageCopyList list;
+    if (need) {
+      // (The stream has read the copies before these by then.)
+      const size_t bytes = ((size_t)listed * sizeof(cas_page_copy_t) + 15) / 16 * 16;
+      s = upload_call_tables(bytes, workspace, stream, [&](char *h) { std::memcpy(h, c + from, (size_t)listed * sizeof(cas_page_copy_t)); });
+      if (s != CAS_OK) return s;
+    } else {
+      std::memcpy(list.copies, c, (size_t)n * sizeof(cas_page_copy_t));
+    }
+    for (int32_t pool0 = 0; pool0 < n_pools; pool0 += kPageCopyPools) {
+      const int32_t m = std::min(kPageCopyPools, n_pools - pool0);
+      for (int32_t i = 0; i < m; ++i) p.pools[i] = (char *)pools[pool0 + i];
+      for (p.first = 0; p.first < listed; p.first += most) {
+        const int32_t k = std::min(most, listed - p.first);
+        const hipError_t e = timed_launch("page_copy", stream, [&] { return launch_page_copy(p, need ? nullptr : &list, k, m, stream); });
+        if (e != hipSuccess) return set_hip_error("page_copy launch", e);
+      }
     }
   }
   return CAS_OK;

@@ -60,6 +60,21 @@ def test_copies(gpu_lib, n_pools, num_pages, page, shape, dtype, n, whole):
     assert same(d, ref)
 
 
+def test_very_many_copies(gpu_lib):
+    """More copies than one table has, 65,536, and pages of many pieces."""
+    t = _t()
+    n, num_pages = 150001, 310000
+    x = t.randint(0, 120, (1, num_pages, 16, 16), dtype=t.uint8, generator=t.Generator().manual_seed(1))
+    copies = random_copies(num_pages, 16, n, 2)
+    d = x.cuda()
+    gpu_lib.pages_copy([d[0]], copies)
+    s, e, rows = (t.from_numpy(c).cuda().long() for c in copies.T)
+    ref = x.cuda()
+    ref[0, e] = t.where((t.arange(16, device="cuda") < rows[:, None])[..., None], ref[0, s], ref[0, e])
+    assert t.equal(d, ref)
+    assert int(d[0].long().sum()) != int(x[0].long().sum())
+
+
 def test_copies_in_any_form(gpu_lib):
     """Lists, other integer types, a column-major array; another stream, the caller's workspace."""
     t = _t()
@@ -84,9 +99,11 @@ def test_copy_binding_refusals(gpu_lib):
     for pools in ([d[0], d[1, :5]], [d[0], d[1].float()], [d[0].transpose(0, 1)], [d[0], d[1].cpu()], [d[0, :, 0, 0]]):
         with pytest.raises((ValueError, TypeError)):
             gpu_lib.PagePools(pools)
-    for copies in ([[1, 2]], [1, 2, 3], [[1, 2, 17]], [[1, 10, 1]], [[1, 2, 1], [3, 2, 1]], [[1, 2, 1], [2, 3, 1]]):
+    for copies in ([[1, 2]], [1, 2, 3], [[1, 2, 17]], [[(1 << 32) + 1, 2, 1]], np.array([[1 << 40, 2, 1]]), [[1, 10, 1]], [[1, 2, 1], [3, 2, 1]], [[1, 2, 1], [2, 3, 1]]):
         with pytest.raises((ValueError, gpu_lib.CasError)):
             gpu_lib.pages_copy([d[0]], copies)
+    with pytest.raises(TypeError):
+        gpu_lib.pages_copy([d[0]], [[1.0, 2.0, 1.0]])
     with pytest.raises(gpu_lib.CasError):
         gpu_lib.pages_copy([d[0], d[0]], [[1, 2, 1]])
     with pytest.raises(gpu_lib.CasError):
