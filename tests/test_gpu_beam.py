@@ -194,6 +194,27 @@ def test_select_equal_beams(gpu_lib):
             check(gpu_lib, flat, x, scores, 32)
 
 
+@pytest.mark.parametrize("N,V,k", [(9, 700, 30), (12, 20011, 50), (40, 5001, 64), (64, 300, 64), (64, 20000, 64)])
+def test_select_many_equal_beams(gpu_lib, N, V, k):
+    """Many beams alike, with random logits and with constant ones (masses of equal candidates), some of them a little better."""
+    t = _t()
+    for dtype in ("fp32", "bf16"):
+        flat, x = logits_of(2, N, V, dtype, seed=V, shift=1)
+        x[:] = x[:, 2:3].clone()
+        x[1] = 0.25
+        scores = t.full((2, N), -2.5)
+        scores[0, N // 2] = t.nextafter(t.tensor(-2.5), t.tensor(0.0))
+        scores[1, 3] = t.nextafter(t.tensor(-2.5), t.tensor(-9.0))
+        check(gpu_lib, flat, x, scores, k)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,V,k", [(20, 20000, 50), (33, 8191, 33), (64, 40000, 64), (17, 100000, 40), (8, 300000, 64)])
+def test_select_many_beams(gpu_lib, dtype, N, V, k):
+    flat, x = logits_of(2, N, V, dtype, seed=V + k, shift=2)
+    check(gpu_lib, flat, x, some_scores(2, N, V), k)
+
+
 @pytest.mark.parametrize("seed", range(6))
 def test_select_random(gpu_lib, seed):
     t = _t()
