@@ -114,9 +114,15 @@ cas_status_t select(const cas_beam_problem_t *p, const void *logits, const float
   a.group_max = (float *)ws;
   a.parts = (DevBeamPart *)(ws + l.parts);
   const DType dt = p->dtype == CAS_DTYPE_BF16 ? kBF16 : kFP32;
-  hipError_t e = timed_launch("beam_scan", stream, [&] { return launch_beam_scan(a, dt, stream); });
-  if (e != hipSuccess) return set_hip_error("beam_scan launch", e);
-  e = timed_launch("beam_pick", stream, [&] { return launch_beam_pick(a, dt, stream); });
+  // Where a batch entry has no more chunks than its workgroup has waves, that scans them itself: 4 beams of 8,000 tokens
+  // 11.5 us instead of 12.7 (a call without a graph 11.9 instead of 14.5), 200 x 8 of 4,000 15.0 instead of 19.0. With two
+  // rounds of chunks it takes longer, 4 beams of 32,000 17.1 instead of 12.6.
+  const bool one_launch = p->batch <= device_topology().cus && (int64_t)p->beams * l.waves <= kBeamPickWaves;
+  if (!one_launch) {
+    const hipError_t e = timed_launch("beam_scan", stream, [&] { return launch_beam_scan(a, dt, stream); });
+    if (e != hipSuccess) return set_hip_error("beam_scan launch", e);
+  }
+  const hipError_t e = timed_launch("beam_pick", stream, [&] { return launch_beam_pick(a, dt, one_launch, stream); });
   return e == hipSuccess ? CAS_OK : set_hip_error("beam_pick launch", e);
 }
 

@@ -172,13 +172,8 @@ struct Row {
 // 7.5 operations of full rate, four of them its exponential's). A wave has 8 KB in
 // flight and four waves a SIMD; five, which spill, took 40 us.
 template <typename T>
-__global__ __launch_bounds__(kScanThreads, 4) void beam_scan_kernel(BeamSelectParams p) {
+__device__ __forceinline__ void scan(const BeamSelectParams &p, int row, int w, int lane) {
   constexpr int N = Piece<T>::N, J = kBeamPieces;
-  const int lane = threadIdx.x & 63;
-  // (Scalar, so that what the wave begins with is scalar work, too.)
-  const unsigned id = blockIdx.x * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = (int)(id / (unsigned)p.waves), w = (int)(id - (unsigned)row * (unsigned)p.waves);
-  if (row >= p.batch * p.beams || out_of_search(p, row)) return;
   const Row<T> r(p, row);
   const int c0 = w * p.per_wave, c1 = min(c0 + p.per_wave, p.chunks);
   float *group_max = p.group_max + (int64_t)row * p.chunks * 64 + lane;
@@ -234,6 +229,15 @@ __global__ __launch_bounds__(kScanThreads, 4) void beam_scan_kernel(BeamSelectPa
   }
   sum = wave_sum(sum);
   if (lane == 0) p.parts[(int64_t)row * p.waves + w] = DevBeamPart{sum, base};
+}
+
+template <typename T>
+__global__ __launch_bounds__(kScanThreads, 4) void beam_scan_kernel(BeamSelectParams p) {
+  // (Scalar, so that what the wave begins with is scalar work, too.)
+  const unsigned id = blockIdx.x * (kScanThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = (int)(id / (unsigned)p.waves), w = (int)(id - (unsigned)row * (unsigned)p.waves);
+  if (row >= p.batch * p.beams || out_of_search(p, row)) return;
+  scan<T>(p, row, w, threadIdx.x & 63);
 }
 
 // 32-bit keys in the order of the floats.
@@ -449,7 +453,7 @@ __device__ __forceinline__ double sum_error(double ln_vocab, double ln_sum, doub
 // Bound by latency: 64 x 8 beams in 12 us, of which the first loads take 2.3, the
 // sums 1.1, the bound 1.6, listing groups 0.7, their logits 1.2, sorting them 0.6, waiting for
 // the wave with most of them 1.5, places and what is close 1.3, the results 0.4.
-template <typename T, int W>
+template <typename T, int W, bool SCAN>
 __global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamSelectParams p) {
   constexpr int kPickThreads = PickShape<W>::kThreads;
   extern __shared__ char smem[];
@@ -477,6 +481,15 @@ __global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamS
     at = __builtin_amdgcn_readfirstlane(at);
     if (lane < n && at + lane < kPickThreads) pool[at + lane] = i * 64 + lane;
   };
+  if (SCAN) {   // (otherwise beam_scan_kernel has done it)
+    const unsigned items = (unsigned)(n_beams * p.waves);
+#pragma unroll 1
+    for (unsigned id = __builtin_amdgcn_readfirstlane(wave); id < items; id += W) {
+      const int i = (int)(id / (unsigned)p.waves), row = b * n_beams + i;
+      if (!out_of_search(p, row)) scan<T>(p, row, (int)(id - (unsigned)i * (unsigned)p.waves), lane);
+    }
+    __syncthreads();
+  }
   GroupTile<PickShape<W>::kTile> tile;
   const bool many = k > 32 && p.chunks >= 4;
   float most_of_lane[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -764,16 +777,19 @@ hipError_t launch_beam_scan(const BeamSelectParams &p, DType dt, hipStream_t s) 
   return hipGetLastError();
 }
 
-hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s) {
-  auto launch = [&](auto waves) {
+hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, bool scan, hipStream_t s) {
+  auto launch = [&](auto waves, auto scans) {
     constexpr int W = decltype(waves)::value;
+    constexpr bool SCAN = decltype(scans)::value;
     const size_t lds = (size_t)p.beams * (64 * 12 + 44) + (size_t)W * (8 + 1024) + ((size_t)p.k + 1 + PickShape<W>::kThreads) * 4;
     const dim3 grid((unsigned)p.batch), threads(PickShape<W>::kThreads);
-    if (dt == kBF16) hipLaunchKernelGGL((beam_pick_kernel<__bf16, W>), grid, threads, lds, s, p);
-    else hipLaunchKernelGGL((beam_pick_kernel<float, W>), grid, threads, lds, s, p);
+    if (dt == kBF16) hipLaunchKernelGGL((beam_pick_kernel<__bf16, W, SCAN>), grid, threads, lds, s, p);
+    else hipLaunchKernelGGL((beam_pick_kernel<float, W, SCAN>), grid, threads, lds, s, p);
   };
-  if (p.beams <= 8) launch(std::integral_constant<int, 8>{});
-  else launch(std::integral_constant<int, 16>{});
+  using Many = std::integral_constant<int, kBeamPickWaves>;
+  if (scan) launch(Many{}, std::true_type{});
+  else if (p.beams > 8) launch(Many{}, std::false_type{});
+  else launch(std::integral_constant<int, 8>{}, std::false_type{});
   return hipGetLastError();
 }
 

@@ -468,7 +468,9 @@ hipError_t launch_table_flags(void *dst, const void *src, size_t bytes, uint32_t
 // copies: a list of at most kPageCopyArgs, or null where p.table has them.
 hipError_t launch_page_copy(const PageCopyParams &p, const PageCopyList *copies, int n, int n_pools, hipStream_t s);
 hipError_t launch_beam_scan(const BeamSelectParams &p, DType dt, hipStream_t s);
-hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, hipStream_t s);
+// scan: instead of launch_beam_scan before it, with kBeamPickWaves waves for a batch entry.
+constexpr int kBeamPickWaves = 16;
+hipError_t launch_beam_pick(const BeamSelectParams &p, DType dt, bool scan, hipStream_t s);
 hipError_t launch_beam_reorder(const BeamReorderParams &p, int n, hipStream_t s);
 hipError_t launch_append(const AppendParams &p, int D, int units, int head_groups, hipStream_t s);
 
