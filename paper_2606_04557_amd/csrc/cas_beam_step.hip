@@ -159,13 +159,19 @@ struct Row {
   }
 };
 
+// What a wave's terms are relative to, see scan().
+__device__ __forceinline__ double base_of(float ref) {
+  return fabsf(ref) > kFarLogit ? (double)ref : (double)(ref * kLog2e) * 0.6931471805599453;
+}
+
 // A wave's chunks of one row: the largest logit of every group, and sum exp(x -
 // base). With ref the largest logit of the wave's first 64 pieces, a term is
 // 2^(x log2 e - c), one multiply-add and the exponential, where c is ref log2 e
 // rounded to fp32 and base = c ln 2. Where ref is beyond +-kFarLogit, so that
 // rounding log2 e would count, base = ref and a term is 2^((x - base) log2 e). Eight terms
 // (fp32: four) and J / 2 of such sums are added in fp32, the chunks in fp64. A chunk
-// with a logit over ref + 16 is done again, with another ref.
+// with a logit over ref + 16 is done again, with another ref; terms from before keep
+// the rounding of the ref that they were made with.
 //
 // Bound by HBM: 64 x 8 rows of 131,072 bf16 (134 MB) in 27 us, 5.0 TB/s (without the
 // exponentials 26; on data in the cache, so its arithmetic alone, 17.5: an element is
@@ -177,8 +183,8 @@ __device__ __forceinline__ void scan(const BeamSelectParams &p, int row, int w, 
   const Row<T> r(p, row);
   const int c0 = w * p.per_wave, c1 = min(c0 + p.per_wave, p.chunks);
   float *group_max = p.group_max + (int64_t)row * p.chunks * 64 + lane;
-  float ref = 0.0f, shift = 0.0f;
-  double base = 0.0, sum = 0.0;
+  float ref = 0.0f, low = 0.0f, shift = 0.0f;
+  double sum = 0.0;
   bool fresh = true;
   for (int c = c0; c < c1; ++c) {
     u32x4 v[J];
@@ -193,11 +199,11 @@ __device__ __forceinline__ void scan(const BeamSelectParams &p, int row, int w, 
 #pragma unroll
           for (int i = 1; i < N; ++i) m = fmaxf(m, x[i]);
         }
+        const double was = base_of(ref);
         ref = fmaxf(wave_max(m), -FLT_MAX);
         shift = ref * kLog2e;
-        const double was = base;
-        base = fabsf(ref) > kFarLogit ? (double)ref : (double)shift * 0.6931471805599453;
-        sum *= sum > 0.0 ? exp(was - base) : 0.0;
+        sum *= sum > 0.0 ? exp(was - base_of(ref)) : 0.0;
+        if (!(__any(sum > 1e-12))) low = ref;   // (its own term is 1)
         fresh = false;
       }
       float parts[2] = {0.0f, 0.0f};
@@ -221,14 +227,14 @@ __device__ __forceinline__ void scan(const BeamSelectParams &p, int row, int w, 
       if (fabsf(ref) <= kFarLogit) add([&](float x) { return fmaf(x, kLog2e, -shift); });
       else add([&](float x) { return (x - ref) * kLog2e; });   // (inf - inf: a NaN)
       part = parts[0] + parts[1];
-      fresh = __any(m > ref + 16.0f);
+      fresh = __any(m - ref > 16.0f);
       if (!fresh) break;
     }
     group_max[c * 64] = m;
     sum += (double)part;
   }
   sum = wave_sum(sum);
-  if (lane == 0) p.parts[(int64_t)row * p.waves + w] = DevBeamPart{sum, base};
+  if (lane == 0) p.parts[(int64_t)row * p.waves + w] = DevBeamPart{sum, ref, low};
 }
 
 template <typename T>
@@ -435,8 +441,9 @@ __device__ __forceinline__ void best_of_row(const BeamSelectParams &p, int row, 
 // term is off by its argument's rounding, |d| 2^-24 for d = x - base, by that of
 // log2 e (|x| 2^-24 / 4, or |d| 2^-24 / 4 and a second rounding of the argument for a far base), by
 // the exponential's unit (2 x 2^-24) and by eleven additions at most. Weighted
-// by their share of the sum, the terms have at most ln V - ln sum + above for |d|, with
-// above = most - base (the entropy of V tokens is at most ln V), and |most| more for |x|.
+// by their share of the sum, most - x is ln V - ln sum at most (the entropy of V tokens is at most ln V), and
+// with it what d is below 0; above 0 it is `above` = most - the lowest ref at most, and 16. |x| is at most |most| more
+// than most - x. All in all under 6e-6.
 __device__ __forceinline__ double sum_error(double ln_vocab, double ln_sum, double above, double most, bool far) {
   const double d = ln_vocab - ln_sum + above;
   return ((far ? 2.25 * d : 1.25 * d + 0.25 * fabs(most)) + 13.0) * 0x1p-24;
@@ -521,15 +528,15 @@ __global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamS
         double sum = 0.0, lowest = INFINITY;
         for (int w = lane; w < p.waves; w += 64) {
           const DevBeamPart part = w < 64 ? first : parts[w];
-          sum += part.sum > 0.0 ? part.sum * exp(part.base - most) : part.sum;
-          if (part.sum > 0.0 && part.base > most - 60.0) lowest = fmin(lowest, part.base);   // (the others' share is under 1e-10)
+          sum += part.sum > 0.0 ? part.sum * exp(base_of(part.ref) - most) : part.sum;
+          if (part.sum > 0.0 && part.ref > most - 60.0) lowest = fmin(lowest, (double)part.low);   // (the others' share is under 1e-10)
         }
         sum = wave_sum(sum);
         if (sum > 0.0 && sum < INFINITY) {
           n = -1;
           ln_sum = fmax(log(sum), 0.0);   // (of a sum that has the term 1: no token is likelier than certain)
           lowest = wave_min(lowest);
-          off = sum_error(p.ln_vocab, ln_sum, fmax(most - lowest, 0.0), most, most > kFarLogit - 1 || lowest < 1 - kFarLogit);
+          off = sum_error(p.ln_vocab, ln_sum, fmin(fmax(most - lowest, 0.0), 16.0), most, most > kFarLogit - 1 || lowest < 1 - kFarLogit);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (i == 0 || many) most_of_lane[i] = fmaxf(most_of_lane[i], (float)(so_far + ((double)x[i] - most) - ln_sum));
@@ -579,7 +586,8 @@ __global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamS
     }
     const int row = b * n_beams + i;
     if (n_beams > W) tile.load(p.group_max + (int64_t)row * p.chunks * 64 + lane, p.chunks);
-    // (Lower by what the scores and their rounding to fp32 may be off, and by a step of fp32 for the rounding here.)
+    // (Lower by what the scores, those behind the bound among them, and their rounding to fp32 may be off, and by a step of
+    // fp32 for the rounding here.)
     const double bound = reached - own[i] + ref[i] + ln[i], slack = 2.0 * error[i] + 1e-5 + 0x1p-22 * (fabs(reached) + fabs(bound));
     // (Without k values to go by, whatever a beam has may be wanted.)
     const float least = reached > -FLT_MAX ? fmaxf((float)(bound - slack), -FLT_MAX) : -FLT_MAX;

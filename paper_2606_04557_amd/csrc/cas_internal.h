@@ -385,8 +385,9 @@ static_assert(sizeof(PageCopyParams) + sizeof(PageCopyList) <= 4096, "kernel arg
 // `lane` in chunk c. A group is what one lane has of one chunk: 8 pieces.
 constexpr int kBeamPieces = 8;
 struct DevBeamPart {
-  double sum;   // of exp(x - base) over a wave's chunks
-  double base;
+  double sum;   // of exp(x - base) over a wave's chunks, base being about ref
+  float ref;
+  float low;    // the lowest ref that terms of the sum were made with
 };
 struct BeamSelectParams {
   const void *logits;

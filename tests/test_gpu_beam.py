@@ -183,6 +183,42 @@ def test_select_tells_near_scores_apart(gpu_lib):
             check(gpu_lib, flat, x, scores, 16)
 
 
+def test_select_near_scores_of_rising_rows(gpu_lib):
+    """Logits that rise along the row, as far as the sums keep what they began with and a little further, in beams that
+    differ by a constant and a few steps of fp32 in their scores."""
+    t = _t()
+    for dtype, chunk in (("fp32", 2048), ("bf16", 4096)):
+        for rise in (15.5, 16.0, 16.5, 40.0):
+            flat, x = logits_of(6, 4, 3 * chunk, dtype, seed=chunk)
+            x[:, 0, :512] = 0.0
+            x[:, 0, 512: chunk] = 15.5
+            x[:, 0, chunk: 2 * chunk] = rise
+            x[:, 0, 2 * chunk:] = rise + 16.5
+            x[:, 0, 7 * chunk // 3:] = rise + 0.5
+            x[:] = (x[:, :1].float() + t.tensor([0.0, 64.0, -32.0, 8.0])[None, :, None]).to(x.dtype)
+            scores = t.tensor([-0.01, -0.3, -1.0, -5.0, -20.0, -0.002])[:, None].repeat(1, 4)
+            for i in range(4):
+                for _ in range((3 * i) % 4):
+                    scores[:, i] = t.nextafter(scores[:, i], t.tensor(0.0 if i % 2 else -100.0))
+            check(gpu_lib, flat, x, scores, 12)
+
+
+@pytest.mark.parametrize("rise", [15.5, 16.5, 40.0])
+def test_select_near_scores_of_long_rising_rows(gpu_lib, rise):
+    """As above in rows so long that a wave has several chunks of them."""
+    t = _t()
+    flat, x = logits_of(2, 4, 2048 * 2048, "fp32", seed=9, std=0.0)
+    row = x[0, 0].view(1024, 2, 2048)   # (of the chunks, every second one)
+    row[:, 0, 512:] = 15.5
+    row[:, 1] = rise
+    x[:] = row.reshape(-1) + t.tensor([0.0, 64.0, -32.0, 8.0])[None, :, None]
+    scores = t.tensor([[-0.3], [-5.0]]).repeat(1, 4)
+    for i in range(4):
+        for _ in range((3 * i) % 4):
+            scores[:, i] = t.nextafter(scores[:, i], t.tensor(0.0 if i % 2 else -100.0))
+    check(gpu_lib, flat, x, scores, 12)
+
+
 def test_select_equal_beams(gpu_lib):
     """Beams alike in every bit: equal scores go by beam, then token. Rows of odd length begin at different alignments."""
     t = _t()
