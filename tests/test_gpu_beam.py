@@ -343,6 +343,19 @@ def test_select_rows_past_four_gib(gpu_lib):
     compare(gpu_lib.beam_select(d, scores.cuda(), 8), x, scores, 8)
 
 
+@pytest.mark.parametrize("B,N,V", [(70001, 2, 9), (1 << 18, 4, 3), (300, 1, 4099)])
+def test_select_many_entries(gpu_lib, B, N, V):
+    """More batch entries than a grid's second dimension has, up to the most rows."""
+    t = _t()
+    flat, x = logits_of(B, N, V, "fp32", seed=B, shift=1)
+    scores = some_scores(B, N, 4)
+    s, p, v = (a.cpu() for a in gpu_lib.beam_select(on_gpu(flat, x), scores.cuda(), 3))
+    ref = (scores.double()[..., None] + t.log_softmax(x.double(), -1)).view(B, N * V)
+    best, at = ref.sort(dim=1, descending=True, stable=True)
+    assert t.equal(p, (at[:, :3] // V).int()) and t.equal(v, (at[:, :3] % V).int())
+    assert bool(((s - best[:, :3]).abs() <= 2.0 ** -24 * best[:, :3].abs() + LSE_TOL).all())
+
+
 # -- reordering ---------------------------------------------------------------
 def states(B, N, shape, dtype, seed):
     """Integers that every type holds."""
@@ -355,6 +368,7 @@ def states(B, N, shape, dtype, seed):
 @pytest.mark.parametrize("B,N,shape,dtype", [(1, 1, (1,), "uint8"), (2, 4, (), "int32"), (3, 8, (777,), "int32"), (2, 3, (5,), "uint8"),
                                              (2, 5, (31,), "int16"), (1, 16, (8, 3, 64), "bf16"), (4, 17, (40,), "float64"),
                                              (2, 64, (1000,), "bf16"), (70, 2, (9,), "float64"), (2, 33, (3, 7), "uint8"), (0, 4, (5,), "int32"),
+                                             (70001, 2, (9,), "uint8"), (1 << 18, 4, (3,), "int32"),
                                              (2, 4, (0,), "int32"), (1, 6, (200003,), "uint8")])
 def test_reorder(gpu_lib, B, N, shape, dtype, in_place):
     t = _t()
