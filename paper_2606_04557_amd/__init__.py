@@ -1028,7 +1028,10 @@ def beam_select(logits, scores, k: Optional[int] = None, finished=None, pad_toke
     if workspace is None:
         n = ctypes.c_size_t(0)
         _check(lib.cas_beam_select_workspace_size(packed, ctypes.byref(n)))
-        workspace = _empty(stream, (max(n.value, 1),), torch.uint8, device)
+        if stream is None:
+            workspace = scores.new_empty((max(n.value, 1),), dtype=torch.uint8)
+        else:
+            workspace = _empty(stream, (max(n.value, 1),), torch.uint8, device)
     elif workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous and on the tensors' device")
     s, p, t = outs
