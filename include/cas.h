@@ -621,8 +621,8 @@ cas_status_t cas_page_table_lists(const cas_page_table_t *table, const int64_t *
  * The copies are host memory, read during the call. Up to 240 travel as kernel
  * arguments. The list of more goes through a workspace of the size that
  * cas_pages_copy_workspace_size gives for n copies (0 up to 240, where NULL will
- * do; no larger from 65,536 on); calls that run at the same time need a workspace each, as do captured
- * graphs that may.
+ * do; no larger from 65,536 on); calls that run at the same time need a workspace
+ * each, as do captured graphs that may.
  */
 cas_status_t cas_pages_copy_workspace_size(int32_t n, size_t *bytes);
 cas_status_t cas_pages_copy(void *const *pools, int32_t n_pools, int64_t num_pages, int32_t page_size, int64_t row_bytes,
@@ -641,9 +641,9 @@ cas_status_t cas_pages_copy(void *const *pools, int32_t n_pools, int64_t num_pag
  *
  * Candidates are ordered by their exact scores (compared in 64 bits where
  * 32 do not tell them apart), equal ones by beam and then token, lowest first.
- * out_scores are within 6e-6 of the exact ones, and rounded once. Should there be fewer than k above -inf, the
- * others follow in that order with the score -inf: parents and tokens are always
- * in range.
+ * out_scores are within 6e-6 of the exact ones, and rounded once. Should there be
+ * fewer than k above -inf, the others follow in that order with the score -inf:
+ * parents and tokens are always in range.
  *
  * logits: [batch, beams, vocab] bf16 or fp32, device memory, aligned to its type,
  *   rows row_stride >= vocab elements apart (any number: columns behind vocab are not read).

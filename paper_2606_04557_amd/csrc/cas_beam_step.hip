@@ -452,10 +452,11 @@ __device__ __forceinline__ double sum_error(double ln_vocab, double ln_sum, doub
 // One batch entry, a wave to a beam. The largest score of any group with index l mod
 // 64 (or 256) is the l-th of 64 (256) values: k groups reach the k-th largest of these,
 // and only logits that reach it are looked for. Of k random ones among 64 values that
-// is hardly more than k in all while k is small, 44 for 32, but 300 for 64; among 256, 74. Then a candidate's place is the number of those
-// ahead of it. Where two beams' candidates are closer than their sums are exact,
-// those sums are made again in fp64 and the places counted again (3 % of the calls for 64 x 8
-// beams of 131,072 bf16 with random logits; a pair takes 48 us then).
+// is hardly more than k in all while k is small, 44 for 32, but 300 for 64; among 256,
+// 74. Then a candidate's place is the number of those ahead of it. Where two beams'
+// candidates are closer than their sums are exact, those sums are made again in fp64
+// and the places counted again (3 % of the calls for 64 x 8 beams of 131,072 bf16 with
+// random logits; a pair takes 48 us then).
 //
 // Bound by latency: 64 x 8 beams in 12 us, of which the first loads take 2.3, the
 // sums 1.1, the bound 1.6, listing groups 0.7, their logits 1.2, sorting them 0.6, waiting for
