@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "cas_beam_error.h"
 #include "cas_device.h"
 
 namespace cas {
@@ -17,7 +18,6 @@ namespace cas {
 namespace {
 
 constexpr int kScanThreads = 256;
-constexpr float kFarLogit = 64.0f;
 constexpr int kReorderThreads = 256;
 constexpr int kListCap = 128;    // groups that a wave has found and not looked at yet
 
@@ -437,18 +437,6 @@ __device__ __forceinline__ void best_of_row(const BeamSelectParams &p, int row, 
   }
 }
 
-// How far ln sum exp(x - most) may be off by what the scan rounds. Relative to itself each
-// term is off by its argument's rounding, |d| 2^-24 for d = x - base, by that of
-// log2 e (|x| 2^-24 / 4, or |d| 2^-24 / 4 and a second rounding of the argument for a far base), by
-// the exponential's unit (2 x 2^-24) and by eleven additions at most. Weighted
-// by their share of the sum, most - x is ln V - ln sum at most (the entropy of V tokens is at most ln V), and
-// with it what d is below 0; above 0 it is `above` = most - the lowest ref at most, and 16. |x| is at most |most| more
-// than most - x. All in all under 6e-6.
-__device__ __forceinline__ double sum_error(double ln_vocab, double ln_sum, double above, double most, bool far) {
-  const double d = ln_vocab - ln_sum + above;
-  return ((far ? 2.25 * d : 1.25 * d + 0.25 * fabs(most)) + 13.0) * 0x1p-24;
-}
-
 // One batch entry, a wave to a beam. The largest score of any group with index l mod
 // 64 (or 256) is the l-th of 64 (256) values: k groups reach the k-th largest of these,
 // and only logits that reach it are looked for. Of k random ones among 64 values that
@@ -530,14 +518,13 @@ __global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamS
         for (int w = lane; w < p.waves; w += 64) {
           const DevBeamPart part = w < 64 ? first : parts[w];
           sum += part.sum > 0.0 ? part.sum * exp(base_of(part.ref) - most) : part.sum;
-          if (part.sum > 0.0 && part.ref > most - 60.0) lowest = fmin(lowest, (double)part.low);   // (the others' share is under 1e-10)
+          if (part.sum > 0.0 && most - part.ref < 60.0) lowest = fmin(lowest, (double)part.low);   // (the others' share is under 1e-10)
         }
         sum = wave_sum(sum);
         if (sum > 0.0 && sum < INFINITY) {
           n = -1;
           ln_sum = fmax(log(sum), 0.0);   // (of a sum that has the term 1: no token is likelier than certain)
-          lowest = wave_min(lowest);
-          off = sum_error(p.ln_vocab, ln_sum, fmin(fmax(most - lowest, 0.0), 16.0), most, most > kFarLogit - 1 || lowest < 1 - kFarLogit);
+          off = sum_error(p.ln_vocab, ln_sum, wave_min(lowest), most);
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (i == 0 || many) most_of_lane[i] = fmaxf(most_of_lane[i], (float)(so_far + ((double)x[i] - most) - ln_sum));

@@ -183,6 +183,24 @@ def test_select_tells_near_scores_apart(gpu_lib):
             check(gpu_lib, flat, x, scores, 16)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("V", [1, 2048, 32000])
+def test_select_equal_scores_around_64(gpu_lib, dtype, V):
+    """Constant rows and random ones that differ by a constant, around logits of +-64, where the sums' terms change their
+    form: equal scores go by beam, whatever the sums are off by."""
+    t = _t()
+    shifts = t.tensor([[-64.0, 64.0], [64.0, -64.0], [-63.5, 63.5], [-64.0, 63.5], [-65.0, 64.0], [64.0, 65.0], [-64.5, -63.5],
+                       [62.0, -66.0]])[..., None]
+    k = min(40, 2 * V)
+    flat, x = logits_of(8, 2, V, dtype, seed=V)
+    x[:] = shifts.to(x.dtype)
+    check(gpu_lib, flat, x, t.full((8, 2), -2.5), k)
+    step = 1.0 if dtype == "bf16" else 2.0 ** -10   # (both types hold such sums)
+    base = (3 * t.randn((8, 1, V), generator=t.Generator().manual_seed(V)) / step).round() * step
+    x[:] = (base + shifts.round()).to(x.dtype)
+    check(gpu_lib, flat, x, t.full((8, 2), -2.5), k)
+
+
 def test_select_near_scores_of_rising_rows(gpu_lib):
     """Logits that rise along the row, as far as the sums keep what they began with and a little further, in beams that
     differ by a constant and a few steps of fp32 in their scores."""
