@@ -639,8 +639,11 @@ cas_status_t cas_pages_copy(void *const *pools, int32_t n_pools, int64_t num_pag
  * finite, whose logits are all -inf, or among whose logits is a NaN or +inf (such a
  * beam leaves the search; the others of the batch entry go on).
  *
- * Candidates are ordered by their exact scores (compared in 64 bits where
- * 32 do not tell them apart), equal ones by beam and then token, lowest first.
+ * Candidates are ordered by their exact scores, equal ones by beam and then token,
+ * lowest first. Those of one beam are ordered by its logits. Where sums in 32 bits
+ * do not tell two beams apart 64 bits do, if their scores differ by more than 2^-52 (vocab /
+ * 512 + 140) (1e-13 for 131,072 tokens) and a few units of 64 bits of the scores;
+ * equal rows have equal sums.
  * out_scores are within 6e-6 of the exact ones, and rounded once. Should there be
  * fewer than k above -inf, the others follow in that order with the score -inf:
  * parents and tokens are always in range.

@@ -201,6 +201,26 @@ def test_select_equal_scores_around_64(gpu_lib, dtype, V):
     check(gpu_lib, flat, x, t.full((8, 2), -2.5), k)
 
 
+@pytest.mark.parametrize("V", [2, 1000])
+def test_select_scores_a_few_1e_13_apart(gpu_lib, V):
+    """Beam 0's logits are all 0; beam 1 has 0 and V - 1 times d, and a score that puts it 2e-13 to 4e-13 ahead by the
+    definition. The sums of the second pass are to be exact enough for that."""
+    t = _t()
+    found = {2: ["-0x1.4394a4p-7 -0x1.42c824p-8", "-0x1.5d1d2ep-7 -0x1.5c2f22p-8", "-0x1.3cc734p-7 -0x1.3c0336p-8",
+                 "-0x1.479916p-7 -0x1.46c77ap-8", "-0x1.58801cp-7 -0x1.579850p-8", "-0x1.5ab608p-7 -0x1.59cb40p-8"],
+             1000: ["-0x1.53b9eep-7 -0x1.536282p-7", "-0x1.47dab4p-7 -0x1.47865ap-7", "-0x1.5822bap-7 -0x1.57ca2ap-7",
+                    "-0x1.3d2fe0p-7 -0x1.3cde48p-7", "-0x1.46fa64p-7 -0x1.46a644p-7", "-0x1.52ca3cp-7 -0x1.52730ep-7"]}[V]
+    d, own = t.tensor([[float.fromhex(h) for h in pair.split()] for pair in found], dtype=t.float64).unbind(1)
+    flat, x = logits_of(len(found), 2, V, "fp32", seed=V)
+    x[:, 0] = 0.0
+    x[:, 1, 0], x[:, 1, 1:] = 0.0, d[:, None].float()
+    ahead = own - (((V - 1) * d.exp() + 1) / V).log()   # (64 bits hold these to 1e-15)
+    assert bool((x[:, 1, 1].double() == d).all()) and bool(((ahead > 2e-13) & (ahead < 4e-13)).all())
+    scores = t.stack([t.zeros_like(own), own], 1).float()
+    got = check(gpu_lib, flat, x, scores, 2)
+    assert got[1][:, 0].tolist() == [1] * len(found)
+
+
 def test_select_near_scores_of_rising_rows(gpu_lib):
     """Logits that rise along the row, as far as the sums keep what they began with and a little further, in beams that
     differ by a constant and a few steps of fp32 in their scores."""
