@@ -52,8 +52,8 @@ class BeamSearch:
 
     def step(self, logits):
         """Chooses each request's next beams; returns their tokens, int32 [batch,
-        beams]. Where too few pages are free the search ends as it is, with a
-        CasError."""
+        beams]. Where too few pages are free (a CasError), or anything else fails once
+        the beams are chosen, the search ends as it is: results() and close() are left."""
         import torch
         if self._over or self.done or self.steps == self._history.shape[2]:
             raise RuntimeError("the search is over")
@@ -63,14 +63,15 @@ class BeamSearch:
         scores, parents, tokens = beam_select(logits, self.scores, self.beams, finished=None if first else self.finished,
                                               pad_token=self.end_token)
         t = self.steps
+        self._over = True   # (until histories, pages and copies belong together again)
         if not first:
             states = [self._history[:, :, :t], self.finished]
             beam_reorder(states, parents, outs=states)
         self._history[:, :, t] = tokens
         self.finished |= tokens == self.end_token
+        self.scores, self.steps = scores, t + 1
         # A beam at -inf (there were fewer candidates than beams) goes no further, either.
         host = torch.stack((parents, (self.finished | (scores == float("-inf"))).int())).cpu()
-        self.scores, self.steps = scores, t + 1
         if not first:
             base = torch.arange(self.batch, dtype=torch.int32)[:, None] * self.beams
             self.table.reorder(self.seqs, (host[0] + base).flatten().tolist())
@@ -80,16 +81,14 @@ class BeamSearch:
                 self.table.truncate(seq, 0)
         self.done = all(ended) or self.steps == self._history.shape[2]
         if not self.done:
-            try:
-                copies = self.table.extend(self.seqs, [1] * len(self.seqs))
-            except BaseException:
-                self._over = True
-                raise
-            pages_copy(self.pools, copies)
+            pages_copy(self.pools, self.table.extend(self.seqs, [1] * len(self.seqs)))
+        self._over = False
         return tokens
 
     def problem(self, num_kv_heads: int, group_size: int, head_dim: int, softmax_scale: float) -> DecodeProblem:
         """The tables of the next token: one row per beam, request by request."""
+        if self._over:
+            raise RuntimeError("the search is over")
         return self.table.problem(self.seqs, [1] * len(self.seqs), num_kv_heads, group_size, head_dim, softmax_scale)
 
     def results(self):
