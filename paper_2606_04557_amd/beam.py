@@ -89,7 +89,9 @@ class BeamSearch:
         """The tables of the next token: one row per beam, request by request."""
         if self._over:
             raise RuntimeError("the search is over")
-        return self.table.problem(self.seqs, [1] * len(self.seqs), num_kv_heads, group_size, head_dim, softmax_scale)
+        # (The pools may have more pages than the table gives out; the paged calls go by the pools.)
+        return DecodeProblem.from_tables([1] * len(self.seqs), *self.table.lists(self.seqs), self.pools.num_pages,
+                                         self.table.page_size, num_kv_heads, group_size, head_dim, softmax_scale)
 
     def results(self):
         """(tokens int32 [batch, beams, steps], scores fp32 [batch, beams]), best first; behind a beam's end its end_token."""

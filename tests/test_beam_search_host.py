@@ -103,3 +103,15 @@ def test_a_selection_that_fails_can_be_made_again(made):
         results.append((search.results(), table.info()))
     (a, i), (b, j) = results
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and i == j
+
+
+def test_pools_with_more_pages_than_the_table(made):
+    """The problem is one on the pools, as the paged calls ask for."""
+    for pages in (100, 150):
+        table = made.cas.PageTable(100, PAGE)
+        search = made.cas.BeamSearch(table, pools_of(pages), [table.add(tokens=20)], 3, 0, 4)
+        search.step(logits_of(1, 1, 50, 1))
+        p = search.problem(2, 4, 64, 0.125)
+        lens, offsets, ids = table.lists(search.seqs)
+        assert (p.c.num_pages, p.c.page_size, p.c.num_kv_heads, p.c.group_size, p.c.head_dim) == (pages, PAGE, 2, 4, 64)
+        assert list(p._qo) == [0, 1, 2, 3] and list(p._kv) == lens[:] == [21] * 3 and list(p._po) == offsets[:] and list(p._ids) == ids[:]

@@ -159,3 +159,31 @@ def test_beam_search_refusals(gpu_lib):
     search = gpu_lib.BeamSearch(table, pools, [prompt], 2, 0, 4)
     assert search.step(x).cpu()[0, 0] == 9 and not search.done
     assert search.scores.cpu()[0].tolist() == [0.0, float("-inf")] and search.table.lists(search.seqs)[0][:] == [4, 1]
+
+
+def test_beam_search_in_pools_larger_than_the_table(gpu_lib):
+    """The documented loop where the pools have pages that the table does not give out: those stay as they are."""
+    import torch
+    table = gpu_lib.PageTable(20, PAGE)
+    kp, vp = (torch.full((33, PAGE, Hkv, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    pools, scale = gpu_lib.PagePools([kp, vp]), D ** -0.5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    prompt = table.add(tokens=21)
+    k, v = rand(21, Hkv, D), rand(21, Hkv, D)
+    gpu_lib.paged_append(k, v, kp, vp, gpu_lib.DecodeProblem.from_tables([21], *table.lists([prompt]), 33, PAGE, Hkv, G, D, scale))
+    search = gpu_lib.BeamSearch(table, pools, [prompt], 3, 0, 4)
+    search.step(rand(1, 1, 50))
+    while not search.done:
+        k1, v1 = rand(3, Hkv, D), rand(3, Hkv, D)
+        problem = search.problem(Hkv, G, D, scale)
+        gpu_lib.paged_append(k1, v1, kp, vp, problem)
+        o = gpu_lib.paged_chunk_fwd(rand(3, Hkv * G, D), kp, vp, problem)[0]
+        assert bool(torch.isfinite(o).all())
+        lens, offs, ids = table.lists(search.seqs)
+        for i in range(3):
+            at = torch.tensor(ids[offs[i]:offs[i + 1]], device="cuda")
+            mine = kp[at].reshape(-1, Hkv, D)[:lens[i]]
+            assert torch.equal(mine[-1], k1[i]) and (lens[i] == 1 or torch.equal(mine[:21], k))
+        search.step(rand(1, 3, 50))
+    assert bool((kp[20:] == 7.0).all()) and bool((vp[20:] == 7.0).all())
