@@ -898,8 +898,9 @@ class PageTable:
 
 class PagePools:
     """The page pools of a model's layers for pages_copy: tensors [num_pages,
-    page_size, ..] of one shape, dtype and GPU, contiguous (K and V of every layer).
-    The object keeps them; their memory must not be exchanged while it is in use."""
+    page_size, ..] of one shape, dtype and GPU, contiguous (K and V of every layer), a
+    token's row a multiple of 16 bytes. The object keeps them; their memory must not
+    be exchanged while it is in use."""
 
     def __init__(self, pools: Sequence[object]):
         pools = list(pools)

@@ -34,6 +34,8 @@ class BeamSearch:
             raise ValueError("beams and max_tokens must be >= 1")
         if pools.num_pages < table.num_pages or pools.page_size != table.page_size:
             raise ValueError("the pools must have the table's pages")
+        if pools.row_bytes % 16:
+            raise ValueError("a token's row in the pools must be a multiple of 16 bytes (see pages_copy)")
         self.table, self.pools, self.beams, self.end_token = table, pools, int(beams), int(end_token)
         self.batch, self.steps, self._over = len(prompts), 0, False
         self.seqs: List[int] = []

@@ -115,3 +115,13 @@ def test_pools_with_more_pages_than_the_table(made):
         lens, offsets, ids = table.lists(search.seqs)
         assert (p.c.num_pages, p.c.page_size, p.c.num_kv_heads, p.c.group_size, p.c.head_dim) == (pages, PAGE, 2, 4, 64)
         assert list(p._qo) == [0, 1, 2, 3] and list(p._kv) == lens[:] == [21] * 3 and list(p._po) == offsets[:] and list(p._ids) == ids[:]
+
+
+@pytest.mark.parametrize("row_bytes", [8, 24, 250])
+def test_pools_whose_rows_cannot_be_copied(made, row_bytes):
+    table = made.cas.PageTable(100, PAGE)
+    prompt = table.add(tokens=20)
+    before = table.info()
+    with pytest.raises(ValueError):
+        made.cas.BeamSearch(table, pools_of(100, row_bytes), [prompt], 3, 0, 4)
+    assert table.info() == before
