@@ -835,7 +835,14 @@ class PageTable:
 
     def fork(self, seq: int, n: int = 1) -> List[int]:
         """n new sequences of the keys of one."""
-        return [self.add([seq]) for _ in range(n)]
+        made: List[int] = []
+        try:
+            for _ in range(n):
+                made.append(self.add([seq]))
+        except BaseException:
+            self.free(made)
+            raise
+        return made
 
     def extend(self, seqs: Sequence[int], counts: Sequence[int]):
         """Room for counts[i] more keys at the end of each sequence; returns the copies

@@ -39,17 +39,18 @@ class BeamSearch:
         self.table, self.pools, self.beams, self.end_token = table, pools, int(beams), int(end_token)
         self.batch, self.steps, self._over = len(prompts), 0, False
         self.seqs: List[int] = []
+        device = pools.pools[0].device
+        shape = (self.batch, self.beams)
+        self.scores = torch.zeros((self.batch, 1), dtype=torch.float32, device=device)
+        self.finished = torch.zeros(shape, dtype=torch.bool, device=device)
+        self._history = torch.full((*shape, int(max_tokens)), self.end_token, dtype=torch.int32, device=device)
+        # (Last: what fails has taken no pages.)
         try:
             for p in prompts:
                 self.seqs += table.fork(p, self.beams)
         except BaseException:
             table.free(self.seqs)
             raise
-        device = pools.pools[0].device
-        shape = (self.batch, self.beams)
-        self.scores = torch.zeros((self.batch, 1), dtype=torch.float32, device=device)
-        self.finished = torch.zeros(shape, dtype=torch.bool, device=device)
-        self._history = torch.full((*shape, int(max_tokens)), self.end_token, dtype=torch.int32, device=device)
         self.done = self.batch == 0
 
     def step(self, logits):

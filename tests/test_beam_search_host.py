@@ -125,3 +125,36 @@ def test_pools_whose_rows_cannot_be_copied(made, row_bytes):
     with pytest.raises(ValueError):
         made.cas.BeamSearch(table, pools_of(100, row_bytes), [prompt], 3, 0, 4)
     assert table.info() == before
+
+
+def test_a_search_that_cannot_be_made_leaves_the_table_as_it_was(made, monkeypatch):
+    """Memory for the histories, or for the last of the forks, is not there."""
+    table = made.cas.PageTable(100, PAGE)
+    prompts = [table.add(tokens=20), table.add(tokens=5)]
+    before, add, full, left = table.info(), made.cas.PageTable.add, torch.full, []
+
+    def no_memory(*a, **kw):
+        raise MemoryError
+
+    def few(self, parts=(), tokens=0):
+        if not left:
+            raise MemoryError
+        left.pop()
+        return add(self, parts, tokens)
+
+    monkeypatch.setattr(torch, "full", no_memory)
+    with pytest.raises(MemoryError):
+        made.cas.BeamSearch(table, pools_of(100), prompts, 3, 0, 4)
+    monkeypatch.setattr(torch, "full", full)
+    assert table.info() == before
+    monkeypatch.setattr(made.cas.PageTable, "add", few)
+    for n in range(6):
+        left[:] = [0] * n
+        with pytest.raises(MemoryError):
+            made.cas.BeamSearch(table, pools_of(100), prompts, 3, 0, 4)
+        assert table.info() == before
+    for n in range(3):
+        left[:] = [0] * n
+        with pytest.raises(MemoryError):
+            table.fork(prompts[0], 3)
+        assert table.info() == before
