@@ -16,7 +16,7 @@ def made(monkeypatch):
     """The search's GPU calls on CPU tensors. What is in `fail` raises instead."""
     import paper_2606_04557_amd as cas
     import paper_2606_04557_amd.beam as beam
-    m = types.SimpleNamespace(cas=cas, copies=[], fail=set())
+    m = types.SimpleNamespace(cas=cas, copies=[], parents=[], fail=set())
 
     def fails(name):
         if name in m.fail:
@@ -26,6 +26,7 @@ def made(monkeypatch):
         fails("beam_select")
         s, p, v = oracle.beam.select(logits.double().numpy(), scores.double().numpy(), k,
                                      None if finished is None else finished.numpy(), pad_token)
+        m.parents.append(p)
         return torch.from_numpy(s).float(), torch.from_numpy(p).int(), torch.from_numpy(v).int()
 
     def reorder(xs, parents, outs):
@@ -158,3 +159,46 @@ def test_a_search_that_cannot_be_made_leaves_the_table_as_it_was(made, monkeypat
         with pytest.raises(MemoryError):
             table.fork(prompts[0], 3)
         assert table.info() == before
+
+
+@pytest.mark.parametrize("beams,prompts,steps,end", [(4, [20, 48], 40, -9.0), (3, [16, 1, 31], 36, 1.5), (6, [15], 20, -9.0), (1, [40], 20, -9.0)])
+def test_beams_share_the_pages_that_they_have_in_common(made, beams, prompts, steps, end):
+    """After every step a full page is there once for all beams that descend from the token in its last row, its
+    prompt's full pages once for all beams of a request; every beam has a last page of its own, and nothing else is in use."""
+    table = made.cas.PageTable(400, PAGE)
+    seqs = [table.add(tokens=n) for n in prompts]
+    search = made.cas.BeamSearch(table, pools_of(400), seqs, beams, 0, steps)
+    B, step, shared = len(prompts), 0, 0
+    paths = [[[] for _ in range(beams)] for _ in prompts]   # the steps' beams that each beam descends from
+    while not search.done:
+        x = logits_of(B, 1 if step == 0 else beams, 60, step)
+        x[..., 0] += end
+        search.step(x)
+        par = made.parents[-1]
+        paths = [[paths[b][par[b, i]] + [(step, i)] for i in range(beams)] for b in range(B)]
+        step += 1
+        if search.done:
+            break
+        ended = search.finished | (search.scores == -np.inf)
+        want = {}   # page of the cache -> what it is
+        for b, n in enumerate(prompts):
+            lens, offs, ids = table.lists([seqs[b]] + search.seqs[b * beams:(b + 1) * beams])
+            assert lens[0] == n
+            for i in range(-1, beams):
+                pages, dead = ids[offs[i + 1]:offs[i + 2]], i >= 0 and bool(ended[b, i])
+                length = n if i < 0 else 1 if dead else n + step
+                assert lens[i + 1] == length and len(pages) == -(-length // PAGE)
+                for j, page in enumerate(pages):
+                    last = (j + 1) * PAGE - 1
+                    if dead or last >= length:
+                        key = (b, i, "own")
+                    elif last < n:
+                        key = (b, j, "prompt")
+                    else:
+                        key = (b, j, paths[b][i][last - n])
+                        shared += key in want.values()
+                    assert want.setdefault(page, key) == key
+        assert len(set(want.values())) == len(want) == table.info()["pages_used"]
+    assert shared or beams == 1 or step < 2 * PAGE
+    copies = [c for call in made.copies for c in call]
+    assert copies or beams == 1
