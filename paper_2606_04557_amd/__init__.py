@@ -401,8 +401,12 @@ class DecodeProblem:
                     num_kv_heads: int, group_size: int, head_dim: int, softmax_scale: float) -> DecodeProblem:
         """A problem on C int32 arrays as PageTable.lists returns them, which it keeps."""
         B = len(q_counts)
+        if any(getattr(t, "_type_", None) is not ctypes.c_int32 for t in (kv_lens, page_offsets, page_ids)):
+            raise TypeError("the tables must be ctypes arrays of c_int32")
         if len(page_offsets) != B + 1:
             raise ValueError("one query count per sequence")
+        if len(kv_lens) < B or len(page_ids) < page_offsets[B]:   # (what the library reads)
+            raise ValueError("a length per sequence, and page_offsets[-1] page ids")
         self = cls.__new__(cls)
         self._qo = (ctypes.c_int32 * (B + 1))(0, *itertools.accumulate(int(n) for n in q_counts))
         self.Tq, self._kv, self._po, self._ids = self._qo[B], kv_lens, page_offsets, page_ids

@@ -221,6 +221,23 @@ def test_problem_of_a_table(cas):
         t.problem(q, [1], 2, 4, 64, 0.125)
 
 
+def test_problem_of_tables_that_do_not_fit(cas):
+    """Arrays shorter than what the library would read of them, or of another type, are refused."""
+    t = cas.PageTable(64, 16)
+    q = [t.add(tokens=40), t.add(tokens=20)]
+    lens, offs, ids = t.lists(q)
+    ints = lambda *v: (ctypes.c_int32 * len(v))(*v)
+    rest = (64, 16, 2, 4, 64, 0.125)
+    assert cas.DecodeProblem.from_tables([1, 1], lens, offs, ids, *rest).Tq == 2
+    for counts, tables in (([1, 1], (ints(40), offs, ids)), ([1, 1], (lens, offs, ints(*ids[:4]))), ([1, 1], (lens, ints(0, 3), ids)),
+                           ([1], (lens, offs, ids)), ([1, 1], (lens, ints(0, 3, 1 << 30), ids))):
+        with pytest.raises(ValueError):
+            cas.DecodeProblem.from_tables(counts, *tables, *rest)
+    for tables in (((ctypes.c_int64 * 2)(40, 20), offs, ids), (lens, list(offs), ids), (lens, offs, np.array(ids[:], dtype=np.int32))):
+        with pytest.raises(TypeError):
+            cas.DecodeProblem.from_tables([1, 1], *tables, *rest)
+
+
 # -- copies of pages ----------------------------------------------------------
 def _copy(cas, copies, pools=(A, A + (1 << 30)), num_pages=100, page=16, row=256, ws=0, ws_bytes=0, n=None, at=True):
     a = (ctypes.c_int32 * (3 * max(len(copies), 1)))(*[x for c in copies for x in c])
