@@ -640,10 +640,11 @@ cas_status_t cas_pages_copy(void *const *pools, int32_t n_pools, int64_t num_pag
  * beam leaves the search; the others of the batch entry go on).
  *
  * Candidates are ordered by their exact scores, equal ones by beam and then token,
- * lowest first. Those of one beam are ordered by its logits. Where sums in 32 bits
- * do not tell two beams apart 64 bits do, if their scores differ by more than 2^-52 (vocab /
- * 512 + 140) (1e-13 for 131,072 tokens) and a few units of 64 bits of the scores;
- * equal rows have equal sums.
+ * lowest first. Those of one beam are ordered by its logits. Two beams' that sums in
+ * 32 bits do not tell apart are compared with sums in 64, which do if their scores
+ * differ by more than 2^-52 (vocab / 512 + 140) (1e-13 for 131,072 tokens) and a few
+ * units of 64 bits of the scores; rows that are equal, or so but for a constant, have
+ * equal sums.
  * out_scores are within 6e-6 of the exact ones, and rounded once. Should there be
  * fewer than k above -inf, the others follow in that order with the score -inf:
  * parents and tokens are always in range.
@@ -681,9 +682,11 @@ cas_status_t cas_beam_select(const cas_beam_problem_t *p, const void *logits, co
  * for 1 to 8 tensors in one launch. parents: device array [batch, beams_out] of
  * beams of the same batch entry, 0 .. beams_in - 1; a row with any other parent is
  * left as it was. A row is row_bytes bytes (0 allowed) in a row; strides are
- * bytes, of any alignment (16 is the fastest; the rest of a row goes byte by byte). beams_in
- * and beams_out are at most 64. y == x with equal strides and beams_in ==
- * beams_out reorders in place; any other overlap is refused.
+ * bytes, of any alignment (16 is the fastest: a tensor whose addresses and strides
+ * are multiples of 4 only takes twice as long, any other five times; the bytes of a
+ * row behind its last 16 or 4 go one by one). beams_in and beams_out are at most
+ * 64. y == x with equal strides and beams_in == beams_out reorders in place; any
+ * other overlap is refused.
  */
 typedef struct {
   const void *x;

@@ -57,7 +57,7 @@ struct BeamLayout {
 
 BeamLayout beam_layout(const cas_beam_problem_t &p) {
   // Chunks of a wave: as many as leave 8,192 waves, twice what is on the GPU at a time (64 x 8 rows of 131,072
-  // bf16: 30 us, with half or a quarter as many waves 33).
+  // bf16 before the loads passed by the caches: 30 us, with half or a quarter as many waves 33).
   constexpr int64_t kWaves = 8192;
   const int64_t rows = (int64_t)p.batch * p.beams, piece = p.dtype == CAS_DTYPE_BF16 ? 8 : 4, chunk = 64 * kBeamPieces * piece;
   BeamLayout l;
@@ -114,7 +114,7 @@ cas_status_t select(const cas_beam_problem_t *p, const void *logits, const float
   a.group_max = (float *)ws;
   a.parts = (DevBeamPart *)(ws + l.parts);
   const DType dt = p->dtype == CAS_DTYPE_BF16 ? kBF16 : kFP32;
-  // Where a batch entry has no more chunks than its workgroup has waves, that scans them itself: 4 beams of 8,000 tokens
+  // Where the scan of a batch entry has no more waves than its workgroup, that does it itself: 4 beams of 8,000 tokens
   // 11.5 us instead of 12.7 (a call without a graph 11.9 instead of 14.5), 200 x 8 of 4,000 15.0 instead of 19.0. With two
   // rounds of chunks it takes longer, 4 beams of 32,000 17.1 instead of 12.6.
   const bool one_launch = p->batch <= device_topology().cus && (int64_t)p->beams * l.waves <= kBeamPickWaves;

@@ -138,8 +138,8 @@ struct Row {
       if (piece * N + i >= begin && piece * N + i < end) Piece<T>::put(v, i, base[piece * N + i]);
     return v;
   }
-  // A lane's pieces of chunk c, in passing (64 x 8 rows of 131,072 bf16: 27.1 us, and 29.2 when the caches are to keep
-  // them).
+  // A lane's pieces of chunk c, in passing (64 x 8 rows of 131,072 bf16: 27.1 us between events, and 29.2 when the
+  // caches are to keep them).
   __device__ __forceinline__ u32x4 load_once(int piece) const {
     return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + piece * N));
   }
@@ -173,7 +173,7 @@ __device__ __forceinline__ double base_of(float ref) {
 // with a logit over ref + 16 is done again, with another ref; terms from before keep
 // the rounding of the ref that they were made with.
 //
-// Bound by HBM: 64 x 8 rows of 131,072 bf16 (134 MB) in 27 us, 5.0 TB/s (without the
+// Bound by HBM: 64 x 8 rows of 131,072 bf16 (134 MB) in 25.5 us, 5.3 TB/s (between events 27, without the
 // exponentials 26; on data in the cache, so its arithmetic alone, 17.5: an element is
 // 7.5 operations of full rate, four of them its exponential's). A wave has 8 KB in
 // flight and four waves a SIMD; five, which spill, took 40 us.
@@ -444,11 +444,13 @@ __device__ __forceinline__ void best_of_row(const BeamSelectParams &p, int row, 
 // 74. Then a candidate's place is the number of those ahead of it. Where two beams'
 // candidates are closer than their sums are exact, those sums are made again in fp64
 // and the places counted again (3 % of the calls for 64 x 8 beams of 131,072 bf16 with
-// random logits; a pair takes 48 us then).
+// random logits; 21 us for each such beam, one after the other).
 //
-// Bound by latency: 64 x 8 beams in 12 us, of which the first loads take 2.3, the
-// sums 1.1, the bound 1.6, listing groups 0.7, their logits 1.2, sorting them 0.6, waiting for
-// the wave with most of them 1.5, places and what is close 1.3, the results 0.4.
+// Bound by latency: 64 x 8 beams in 13 us, of which the first loads take a sixth, the
+// sums a tenth, the bounds a fifth, listing groups 6 %, their logits 8, sorting them 11, waiting for
+// the wave with most of them 8, places and what is close 15, the results 4. 184 scalar
+// registers are spilled (8 waves, bf16), in all of these. Equal logits are all looked at, since
+// all of them reach the bound: a row of 131,072 takes 7 ms.
 template <typename T, int W, bool SCAN>
 __global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamSelectParams p) {
   constexpr int kPickThreads = PickShape<W>::kThreads;
@@ -719,7 +721,8 @@ __global__ __launch_bounds__(PickShape<W>::kThreads) void beam_pick_kernel(BeamS
 // copy. Bound by HBM: every row that is a parent is read once (its further children
 // find it in the cache), every one written that is not its own parent in place. Two tensors of
 // 32 x 8 rows of 400 KB (329 MB, 120 of the 256 rows parents): 66 us, 4.9 TB/s; with 64 beams, whose
-// 64 pieces leave two waves to a SIMD, 3.7 TB/s. Addresses by scalars: with a branch around each
+// 64 pieces leave one wave to a SIMD and spill 442 scalar registers, 2.5 TB/s. Rows that are 4 or 1 bytes
+// aligned go by such units: 128 x 8 rows of 400 KB in 126, 266 and 624 us (660 MB). Addresses by scalars: with a branch around each
 // load and vector addresses the same took 218 us.
 template <typename U, int N>
 __device__ __forceinline__ void move(const char *x, int64_t xi, char *y, int64_t yi, int parent_of_lane, int n, int n_in, uint32_t at) {
